@@ -413,6 +413,38 @@ int nm_linear_forward(const void *x, int64_t ldx, const void *w, const void *bia
                       void *y, void *hip_stream);
 int nm_linear_input_grad(const void *g, int64_t ldg, const void *w, int64_t T, int64_t O, int64_t I, void *dx, void *hip_stream);
 
+/*
+ * One AdamW step over many tensors (decoupled weight decay), one launch for every 48 of them:
+ *     g <- g * grad_scale * (grad_scale_dev ? *grad_scale_dev : 1)
+ *     m <- beta1 m + (1 - beta1) g      v <- beta2 v + (1 - beta2) g^2
+ *     p <- p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * binary32 throughout.  tensors: a HOST array of `count` entries, read before the call returns; arrays contiguous, n elements each:
+ *   param, grad    of param_dtype and grad_dtype (NM_F32 or NM_BF16, one for all tensors of a call)
+ *   master         binary32 copy of a bf16 parameter that takes the step in its place, the parameter is then its rounding; NULL = none,
+ *                  for all tensors of a call
+ *   m, v           NM_STATE_F32: binary32.  NM_STATE_Q8: e4m3 codes of m and of sqrt(v), with m_scale and v_scale [(n + 255) / 256]:
+ *                  a value is its code's times the scale of its block of 256 elements (all-zero codes stand for zeros under any finite scale)
+ *   number         of the tensor, in the counter of its random words
+ * NM_STATE_Q8 writes a block's scale as the smallest power of two that brings its largest finite magnitude to 448 or below (1 for a block of zeros,
+ * exponents kept in [-126, 126]), and rounds a magnitude y / scale to one of its two e4m3 neighbours: up where its fraction of the
+ * step plus r / 2^16 reaches 1 (below 2^-6 the step is 2^-9 and y / scale + 2^-6 is rounded to binary32 first).  r is half a word of
+ * Philox4x32-10: key = seed, counter = (e/4 low, e/4 high, number, 2^31 + step), word e % 4 for element e, its low half for m and
+ * its high half for sqrt(v).  sqrt(v) > 0 gets code 1 at least; what is not finite gets the NaN code.
+ * Bases on their elements' boundary; on 16-byte boundaries they are read in vectors.  The arrays of a tensor, and those of different
+ * tensors, must not overlap (checked within a tensor).
+ */
+typedef enum { NM_STATE_F32 = 0, NM_STATE_Q8 = 1 } nm_state;
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale, *master;
+    int64_t n;
+    uint32_t number;
+} nm_adamw_tensor;
+int nm_adamw(const nm_adamw_tensor *tensors, int count, int param_dtype, int grad_dtype, int state, double lr, double beta1, double beta2,
+             double eps, double weight_decay, int64_t step, float grad_scale, const float *grad_scale_dev, uint64_t seed, void *hip_stream);
+
 /* Message of the last error on this thread ("" if none).  Static storage; do not free. */
 const char *nm_last_error(void);
 

@@ -102,6 +102,8 @@ def load():
     lib.nm_linear_forward.restype = i32
     lib.nm_linear_input_grad.argtypes = [vp, i64, vp, i64, i64, i64, vp, vp]
     lib.nm_linear_input_grad.restype = i32
+    lib.nm_adamw.argtypes = [vp, i32, i32, i32, i32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, i64, f32, vp, u64, vp]
+    lib.nm_adamw.restype = i32
     for f in (lib.mvue_prune_1of2, lib.mvue_prune_2of4, lib.nm_compress, lib.nm_update_gemm, lib.mvue_prune_2of4_q8,
               lib.nm_update_gemm_q8):
         f.restype = i32
@@ -113,7 +115,7 @@ def load():
         from . import _nm_torch as native
         native.bind({f: C.cast(getattr(lib, f), vp).value for f in (
             "mvue_prune_1of2", "mvue_prune_2of4", "nm_update_gemm", "nm_update_gemm_workspace", "nm_linear_update", "nm_linear_update_workspace",
-            "nm_linear_forward", "nm_linear_input_grad")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
+            "nm_linear_forward", "nm_linear_input_grad", "nm_adamw")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
     except ImportError as e:
         warnings.warn(f"_nm_torch.so is not built for this torch ({e}): every call takes the slower way through ctypes and linear layers take the "
                       "framework's products until `python -m paper_2203_10991_amd.build` has run")
@@ -125,7 +127,7 @@ def load():
 
 class _NoNative:
     """In the place of _nm_torch: no call is its own."""
-    prune = update_gemm = linear_update = linear_forward = linear_input_grad = staticmethod(lambda *a: None)
+    prune = update_gemm = linear_update = linear_forward = linear_input_grad = adamw = staticmethod(lambda *a: None)
 
 
 def _native_result(r):
@@ -691,3 +693,95 @@ def own_linear_input_grad(g: torch.Tensor, weight: torch.Tensor) -> Optional[tor
         return None
     load()
     return _native_result(_native.linear_input_grad(g, weight))
+
+
+# ---- the optimizer's step
+
+class _AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("master", C.c_void_p), ("n", C.c_int64), ("number", C.c_uint32)]
+
+
+STATE_BLOCK = 256         # elements of an 8-bit state that share a scale
+
+
+def alloc_adamw_state(param: torch.Tensor, q8: bool = False):
+    """Zero state of nm_adamw for one of m and v: a binary32 tensor, or (q8) a pair of e4m3 codes and scales."""
+    if not q8:
+        return torch.zeros_like(param, dtype=torch.float32, memory_format=torch.preserve_format)
+    codes = torch.empty_like(param, dtype=torch.float8_e4m3fn, memory_format=torch.preserve_format)
+    codes.view(torch.uint8).zero_()
+    return codes, torch.ones(-(-param.numel() // STATE_BLOCK), dtype=torch.float32, device=param.device)
+
+
+def _adamw_state(what: str, state, p: torch.Tensor):
+    """(values, scale or None) of a state that fits its parameter."""
+    if isinstance(state, torch.Tensor):
+        values, scale, want = state, None, torch.float32
+    else:
+        (values, scale), want = state, torch.float8_e4m3fn
+        if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != -(-p.numel() // STATE_BLOCK) or scale.device != p.device:
+            raise ValueError(f"{what}: scales are contiguous float32, one for every {STATE_BLOCK} elements")
+    if values.dtype != want:
+        raise TypeError(f"{what} is float32, or a pair of float8_e4m3fn codes and float32 scales; got {values.dtype}")
+    if values.shape != p.shape or values.stride() != p.stride() or values.device != p.device:
+        raise ValueError(f"{what} has another shape, layout or device than its parameter")
+    return values, scale
+
+
+def nm_adamw(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
+             masters=None, grad_scale=1.0, seed: int = 0, numbers=None) -> None:
+    """One AdamW step (number `step`, from 1) over lists of tensors, in place; tensors of one set of types share a launch.
+
+    params and grads: float32 or bfloat16.  exp_avgs, exp_avg_sqs: of each tensor a float32 tensor, or for 8-bit states a pair
+    (float8_e4m3fn codes, float32 scales) as alloc_adamw_state makes them; that of exp_avg_sqs then stands for its square
+    root.  masters: float32 copies of bfloat16 parameters that take the step, None in the place of one without.  grad_scale: a
+    factor on the gradients, a number or a float32 tensor of one element on the GPU.  numbers: each tensor's number in the counter of its random words
+    (8-bit states), its place in the list by default."""
+    lib = load()
+    params, grads, exp_avgs, exp_avg_sqs = list(params), list(grads), list(exp_avgs), list(exp_avg_sqs)
+    masters = None if masters is None else list(masters)
+    numbers = None if numbers is None else list(numbers)
+    dev_scale = grad_scale if isinstance(grad_scale, torch.Tensor) else None
+    args = (step, float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), 1.0 if dev_scale is not None else float(grad_scale))
+    if _native_result(_native.adamw(params, grads, exp_avgs, exp_avg_sqs, masters, numbers, *args, dev_scale, seed)):
+        return
+    n = len(params)
+    if any(len(x) != n for x in (grads, exp_avgs, exp_avg_sqs, masters or params, numbers or params)):
+        raise ValueError("nm_adamw takes lists of one length")
+    if dev_scale is not None and (not dev_scale.is_cuda or dev_scale.dtype != torch.float32 or dev_scale.numel() != 1):
+        raise TypeError("grad_scale is a number or a float32 tensor of one element on the GPU")
+    groups, keep = {}, []
+    for k, (p, g) in enumerate(zip(params, grads)):
+        w = None if masters is None else masters[k]
+        if not p.is_cuda or g.device != p.device or (dev_scale is not None and dev_scale.device != p.device):
+            raise ValueError("nm_adamw takes tensors on the GPU, a parameter's arrays on one device")
+        if g.shape != p.shape:
+            raise ValueError(f"gradient {tuple(g.shape)} of a parameter {tuple(p.shape)}")
+        if p.numel() and _dense_strides(p) is None:
+            raise ValueError("a parameter's memory has gaps or overlaps")
+        if g.stride() != p.stride():
+            g = torch.empty_strided(p.shape, p.stride(), dtype=g.dtype, device=g.device).copy_(g)
+            keep.append(g)
+        (m, ms), (v, vs) = _adamw_state("exp_avg", exp_avgs[k], p), _adamw_state("exp_avg_sq", exp_avg_sqs[k], p)
+        if (ms is None) != (vs is None):
+            raise TypeError("exp_avg and exp_avg_sq are both float32 or both 8 bits")
+        if w is not None and (w.dtype != torch.float32 or w.shape != p.shape or w.stride() != p.stride() or w.device != p.device):
+            raise ValueError("a master copy is float32 and laid out as its parameter")
+        key = (p.device, _dtype_code(p), _dtype_code(g), ms is not None, w is not None)
+        groups.setdefault(key, []).append(_AdamwTensor(_ptr(p), _ptr(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), _ptr(w), p.numel(), k if numbers is None else numbers[k]))
+    for (device, pt, gt, q8, _), tensors in groups.items():
+        with torch.cuda.device(device):
+            _check(lib.nm_adamw((_AdamwTensor * len(tensors))(*tensors), len(tensors), pt, gt, int(q8), *args[1:6], step, args[6], _ptr(dev_scale), seed,
+                                torch.cuda.current_stream(device).cuda_stream))
+    torch.autograd.graph.increment_version([t for t in params + (masters or []) if t is not None and not t.is_inference()])
+
+
+def _dense_strides(t: torch.Tensor) -> Optional[Tuple[int, ...]]:
+    """The strides of a tensor whose elements fill its memory without gaps or overlaps, in any order of dimensions; None of another."""
+    need = 1
+    for size, stride in sorted((x for x in zip(t.shape, t.stride()) if x[0] != 1), key=lambda x: x[1]):
+        if stride != need:
+            return None
+        need *= size
+    return t.stride()

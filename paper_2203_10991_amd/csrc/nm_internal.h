@@ -163,6 +163,46 @@ hipError_t launch_finish_linear(const float *part, int slabs, int64_t O, int64_t
 hipError_t launch_dense_gemm(bool nn, const void *x, int64_t ldx, const void *w, const void *bias, void *y, int64_t ldy, int64_t M, int64_t N, int64_t K,
                              bool relu, hipStream_t st);
 
+// ---- 8-bit integer products of a linear layer
+// Rows of x [R x C] as 8-bit integers and a scale: a = max |x|, q = the integer nearest to x * (127 / a), ties to even, scale = a / 127.  Columns C .. ldq - 1 of q
+// become zeros.  ..._t: the columns of x instead, transposed: q [C x R]; part: C * quant_i8_slabs(R, C) words of workspace.
+hipError_t launch_quant_i8(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, hipStream_t st);
+int quant_i8_slabs(int64_t R, int64_t C);
+hipError_t launch_quant_i8_t(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, uint32_t *part, hipStream_t st);
+// y [M x N] = act((x w^T) xs ws + bias): x [M x K], row stride ldx, zeros from K to the next multiple of I8_K; w [N x K], row stride ldw (a multiple of 16)
+constexpr int I8_K = 128;
+struct I8Arg {
+    const int8_t *x, *w;
+    const float *xs, *ws;
+    const void *bias;
+    void *y;
+    int64_t ldx, ldw, ldy, M, N, K;
+    int bias_dt, y_dt, relu;
+};
+hipError_t launch_gemm_i8(const I8Arg &p, hipStream_t st);
+
+// ---- embedding (embed.hip).  ids: 32 or 64 bits wide
+hipError_t launch_embed(int table_dt, int out_dt, const void *table, int64_t V, int64_t D, int64_t ldt, const void *ids, bool wide, int64_t N, float scale, void *out,
+                        int64_t ldo, hipStream_t st);
+size_t embed_grad_workspace(int64_t N, int64_t V, int64_t D);
+hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, const void *ids, bool wide, int64_t N, int64_t V, int64_t D, float scale,
+                             int64_t padding, bool accumulate, void *out, int64_t ldo, void *workspace, hipStream_t st);
+
+// ---- AdamW (adamw.hip)
+struct AdamwTensor {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale, *master;
+    int64_t n;
+    uint32_t number;                          // in the counter of the random words
+    int aligned;                              // every base on a 16-byte boundary
+};
+constexpr int ADAMW_MOST = 48;                // tensors of a launch: they travel in the kernel's arguments, which hold 4 KB
+struct AdamwRates { double lr, beta1, beta2, eps, weight_decay; int64_t step; float grad_scale; const float *grad_scale_dev; };
+hipError_t launch_adamw(const AdamwTensor *tensors, int count, int param_dt, int grad_dt, bool q8, bool master, const AdamwRates &r, uint64_t seed,
+                        hipStream_t st);
+
 // The library's static device scratch array (nm_static.hip): its size, and its address on the current device
 // (looked up once per device; no allocation).
 size_t static_scratch_bytes();

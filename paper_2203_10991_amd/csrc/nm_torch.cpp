@@ -18,6 +18,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <vector>
 
 #include "../../include/nm_mvue.h"
 
@@ -33,6 +34,7 @@ decltype(&nm_linear_update) p_linear_update;
 decltype(&nm_linear_update_workspace) p_linear_update_workspace;
 decltype(&nm_linear_forward) p_linear_forward;
 decltype(&nm_linear_input_grad) p_linear_input_grad;
+decltype(&nm_adamw) p_adamw;
 PyObject *stream_of = nullptr;
 
 struct NoGil {                                                       // as a ctypes call does: a launch may wait for the queue
@@ -270,6 +272,93 @@ PyObject *linear_input_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- adamw(params, grads, ms, vs, masters or None, numbers or None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, grad_scale tensor or None, seed) -> True:
+// the step has been taken.  Lists of one length; one type of parameters, gradients and states, all on one device, a tensor's arrays with one dense layout.
+// A state is a binary32 tensor, or a pair of e4m3 codes and binary32 scales.
+bool same_layout(const at::Tensor &p, const at::Tensor &t) { return t.sizes() == p.sizes() && t.strides() == p.strides(); }
+// an array of a tensor's state: 0 binary32, 1 codes and scales, -1 neither
+int state_of(PyObject *o, const at::Tensor &p, void *&values, float *&scale)
+{
+    if (const at::Tensor *t = gpu_tensor(o)) {
+        if (t->scalar_type() != at::kFloat || t->device() != p.device() || !same_layout(p, *t)) return -1;
+        values = t->data_ptr();
+        scale = nullptr;
+        return 0;
+    }
+    if (!(PyTuple_CheckExact(o) || PyList_CheckExact(o)) || PySequence_Fast_GET_SIZE(o) != 2) return -1;
+    const at::Tensor *c = gpu_tensor(PySequence_Fast_GET_ITEM(o, 0)), *s = gpu_tensor(PySequence_Fast_GET_ITEM(o, 1));
+    if (!c || !s || c->scalar_type() != at::kFloat8_e4m3fn || s->scalar_type() != at::kFloat || c->device() != p.device() || s->device() != p.device() ||
+        !same_layout(p, *c) || !s->is_contiguous() || s->numel() != (p.numel() + 255) / 256)
+        return -1;
+    values = c->data_ptr();
+    scale = (float *)s->data_ptr();
+    return 1;
+}
+
+PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 15) return none();
+    for (int i = 0; i < 6; ++i)
+        if (!(PyList_CheckExact(a[i]) || PyTuple_CheckExact(a[i])) && !(i >= 4 && a[i] == Py_None)) return none();
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[0]);
+    for (int i = 1; i < 6; ++i)
+        if (a[i] != Py_None && PySequence_Fast_GET_SIZE(a[i]) != count) return none();
+    if (!count || !PyLong_Check(a[6]) || !whole_number(a[14])) return none();
+    std::vector<nm_adamw_tensor> all(count);
+    std::vector<const at::Tensor *> changed;
+    const at::Tensor *first = nullptr;
+    int state = -1;
+    at::ScalarType pt = at::kFloat, gt = at::kFloat;
+    for (Py_ssize_t k = 0; k < count; ++k) {
+        const at::Tensor *p = gpu_tensor(PySequence_Fast_GET_ITEM(a[0], k)), *g = gpu_tensor(PySequence_Fast_GET_ITEM(a[1], k));
+        if (!p || !g || !p->is_non_overlapping_and_dense() || !same_layout(*p, *g)) return none();
+        if (!first) { first = p; pt = p->scalar_type(); gt = g->scalar_type(); }
+        if (p->device() != first->device() || g->device() != first->device() || p->scalar_type() != pt || g->scalar_type() != gt) return none();
+        nm_adamw_tensor &t = all[k];
+        changed.push_back(p);
+        t.param = p->data_ptr();
+        t.grad = g->data_ptr();
+        t.n = p->numel();
+        t.number = a[5] == Py_None ? (uint32_t)k : (uint32_t)PyLong_AsUnsignedLongMask(PySequence_Fast_GET_ITEM(a[5], k));
+        t.master = nullptr;
+        const int ms = state_of(PySequence_Fast_GET_ITEM(a[2], k), *p, t.m, t.m_scale), vs = state_of(PySequence_Fast_GET_ITEM(a[3], k), *p, t.v, t.v_scale);
+        if (ms < 0 || ms != vs || (state >= 0 && ms != state)) return none();
+        state = ms;
+        if (a[4] != Py_None) {
+            const at::Tensor *w = gpu_tensor(PySequence_Fast_GET_ITEM(a[4], k));
+            if (!w || w->scalar_type() != at::kFloat || w->device() != first->device() || !same_layout(*p, *w)) return none();
+            t.master = (float *)w->data_ptr();
+            changed.push_back(w);
+        }
+    }
+    if ((pt != at::kFloat && pt != at::kBFloat16) || (gt != at::kFloat && gt != at::kBFloat16)) return none();
+    const float *scale_dev = nullptr;
+    if (a[13] != Py_None) {
+        const at::Tensor *s = gpu_tensor(a[13]);
+        if (!s || s->scalar_type() != at::kFloat || s->numel() != 1 || s->device() != first->device()) return none();
+        scale_dev = (const float *)s->data_ptr();
+    }
+    const int64_t step = PyLong_AsLongLong(a[6]);
+    const double lr = PyFloat_AsDouble(a[7]), b1 = PyFloat_AsDouble(a[8]), b2 = PyFloat_AsDouble(a[9]), eps = PyFloat_AsDouble(a[10]), wd = PyFloat_AsDouble(a[11]),
+                 scale = PyFloat_AsDouble(a[12]);
+    const uint64_t seed = PyLong_AsUnsignedLongLongMask(a[14]);
+    void *st;
+    if (PyErr_Occurred() || c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() != first->device()) return PyErr_Occurred() ? nullptr : none();
+    if (!stream(*first, st)) return nullptr;
+    int rc;
+    {
+        NoGil free;
+        rc = p_adamw(all.data(), (int)count, pt == at::kFloat ? NM_F32 : NM_BF16, gt == at::kFloat ? NM_F32 : NM_BF16, state, lr, b1, b2, eps, wd, step, (float)scale,
+                     scale_dev, seed, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    for (const at::Tensor *t : changed)
+        if (!t->is_inference()) t->unsafeGetTensorImpl()->bump_version();            // (a graph that has saved it then says so)
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
 // bind({name: address}, stream_of)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -278,7 +367,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         {"mvue_prune_1of2", (void **)&p_prune_1of2}, {"mvue_prune_2of4", (void **)&p_prune_2of4}, {"nm_update_gemm", (void **)&p_update_gemm},
         {"nm_update_gemm_workspace", (void **)&p_update_gemm_workspace}, {"nm_linear_update", (void **)&p_linear_update},
         {"nm_linear_update_workspace", (void **)&p_linear_update_workspace}, {"nm_linear_forward", (void **)&p_linear_forward},
-        {"nm_linear_input_grad", (void **)&p_linear_input_grad}};
+        {"nm_linear_input_grad", (void **)&p_linear_input_grad}, {"nm_adamw", (void **)&p_adamw}};
     for (auto &f : all) {
         PyObject *address = PyDict_GetItemString(a[0], f.name);
         if (!address) { PyErr_Format(PyExc_KeyError, "%s", f.name); return nullptr; }
@@ -292,7 +381,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 #define NM_METHOD(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {NM_METHOD(bind), NM_METHOD(prune), NM_METHOD(update_gemm), NM_METHOD(linear_update), NM_METHOD(linear_forward), NM_METHOD(linear_input_grad),
+PyMethodDef methods[] = {NM_METHOD(bind), NM_METHOD(prune), NM_METHOD(update_gemm), NM_METHOD(linear_update), NM_METHOD(linear_forward), NM_METHOD(linear_input_grad), NM_METHOD(adamw),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_nm_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
