@@ -414,6 +414,22 @@ int nm_linear_forward(const void *x, int64_t ldx, const void *w, const void *bia
 int nm_linear_input_grad(const void *g, int64_t ldg, const void *w, int64_t T, int64_t O, int64_t I, void *dx, void *hip_stream);
 
 /*
+ * Embedding: out[n] = scale * table[ids[n]], rounded once to out_dtype, and the table's gradient
+ *     out[v] = (accumulate ? out[v] : 0) + scale * sum over the n with ids[n] = v of g[n]
+ * table [V x D], g and out [N x D] (gradient: out [V x D]), row strides ldt, ldg, ldo in elements; ids of id_bits (32 or 64) bits.  Any sizes, strides and
+ * bases on their elements' boundary (rows on 16-byte boundaries are read in vectors); a row stride does not count where there is one row.
+ * A token outside 0 .. V-1 is a row of NaN in the lookup and counts for nothing in the gradient, nor does the token `padding` (none: -1).
+ * A row's sum runs over its tokens in groups by place, each in the order of the tokens, in binary32: the result depends on ids, N and g
+ * only.  accumulate = 0 writes every row of the table, 1 the rows of tokens that are there.  N below 2^31 - 65536, V below 2^31 - 1.
+ * workspace: nm_embed_grad_workspace(...) bytes.
+ */
+int nm_embed(const void *table, int64_t V, int64_t D, int64_t ldt, int table_dtype, const void *ids, int id_bits, int64_t N, float scale, void *out, int64_t ldo,
+             int out_dtype, void *hip_stream);
+int nm_embed_grad(const void *g, int64_t ldg, int g_dtype, const void *ids, int id_bits, int64_t N, int64_t V, int64_t D, float scale, int64_t padding, int accumulate,
+                  void *out, int64_t ldo, int out_dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t nm_embed_grad_workspace(int64_t N, int64_t V, int64_t D);
+
+/*
  * One AdamW step over many tensors (decoupled weight decay), one launch for every 48 of them:
  *     g <- g * grad_scale * (grad_scale_dev ? *grad_scale_dev : 1)
  *     m <- beta1 m + (1 - beta1) g      v <- beta2 v + (1 - beta2) g^2

@@ -102,6 +102,12 @@ def load():
     lib.nm_linear_forward.restype = i32
     lib.nm_linear_input_grad.argtypes = [vp, i64, vp, i64, i64, i64, vp, vp]
     lib.nm_linear_input_grad.restype = i32
+    lib.nm_embed.argtypes = [vp, i64, i64, i64, i32, vp, i32, i64, f32, vp, i64, i32, vp]
+    lib.nm_embed.restype = i32
+    lib.nm_embed_grad.argtypes = [vp, i64, i32, vp, i32, i64, i64, i64, f32, i64, i32, vp, i64, i32, vp, sz, vp]
+    lib.nm_embed_grad.restype = i32
+    lib.nm_embed_grad_workspace.argtypes = [i64, i64, i64]
+    lib.nm_embed_grad_workspace.restype = sz
     lib.nm_adamw.argtypes = [vp, i32, i32, i32, i32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, i64, f32, vp, u64, vp]
     lib.nm_adamw.restype = i32
     for f in (lib.mvue_prune_1of2, lib.mvue_prune_2of4, lib.nm_compress, lib.nm_update_gemm, lib.mvue_prune_2of4_q8,
@@ -115,7 +121,7 @@ def load():
         from . import _nm_torch as native
         native.bind({f: C.cast(getattr(lib, f), vp).value for f in (
             "mvue_prune_1of2", "mvue_prune_2of4", "nm_update_gemm", "nm_update_gemm_workspace", "nm_linear_update", "nm_linear_update_workspace",
-            "nm_linear_forward", "nm_linear_input_grad", "nm_adamw")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
+            "nm_linear_forward", "nm_linear_input_grad", "nm_adamw", "nm_embed", "nm_embed_grad", "nm_embed_grad_workspace")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
     except ImportError as e:
         warnings.warn(f"_nm_torch.so is not built for this torch ({e}): every call takes the slower way through ctypes and linear layers take the "
                       "framework's products until `python -m paper_2203_10991_amd.build` has run")
@@ -127,7 +133,7 @@ def load():
 
 class _NoNative:
     """In the place of _nm_torch: no call is its own."""
-    prune = update_gemm = linear_update = linear_forward = linear_input_grad = adamw = staticmethod(lambda *a: None)
+    prune = update_gemm = linear_update = linear_forward = linear_input_grad = adamw = embed = embed_grad = staticmethod(lambda *a: None)
 
 
 def _native_result(r):
@@ -693,6 +699,75 @@ def own_linear_input_grad(g: torch.Tensor, weight: torch.Tensor) -> Optional[tor
         return None
     load()
     return _native_result(_native.linear_input_grad(g, weight))
+
+
+# ---- embedding
+
+def _ids(ids: torch.Tensor, device) -> Tuple[torch.Tensor, int]:
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"ids are int32 or int64, got {ids.dtype}")
+    if ids.device != device:
+        raise ValueError("ids live on the GPU of the table or gradient")
+    return ids.contiguous(), 64 if ids.dtype == torch.int64 else 32
+
+
+def _unit_columns(t: torch.Tensor) -> torch.Tensor:
+    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+def _bf16_or_not(dtype: Optional[torch.dtype]):
+    if dtype not in (None, torch.float32, torch.bfloat16):
+        raise TypeError(f"results are float32 or bfloat16, got {dtype}")
+    return None if dtype is None else dtype == torch.bfloat16
+
+
+def nm_embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """scale * table[ids], rounded once to out_dtype (the table's by default).  table [V x D] float32 or bfloat16, ids int32 or int64 of any shape;
+    a token outside the table gives a row of NaN."""
+    lib = load()
+    r = _native_result(_native.embed(table, ids, float(scale), _bf16_or_not(out_dtype)))
+    if r is not None:
+        return r
+    if not table.is_cuda or table.dim() != 2:
+        raise ValueError("the table is a 2-D tensor on the GPU")
+    dt = _dtype_code(table)
+    ids, bits = _ids(ids, table.device)
+    table = _unit_columns(table)
+    (V, D), N = table.shape, ids.numel()
+    out = torch.empty((*ids.shape, D), dtype=out_dtype or table.dtype, device=table.device)
+    with torch.cuda.device(table.device):
+        _check(lib.nm_embed(_ptr(table), V, D, _rowmajor(table, "table"), dt, _ptr(ids), bits, N, float(scale), _ptr(out), D, _dtype_code(out), _stream(table)))
+    return out
+
+
+def nm_embed_grad(g: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, padding_idx: Optional[int] = None, out_dtype: Optional[torch.dtype] = None,
+                  out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
+    """Gradient [vocab x D] of an embedding table: row v is scale times the sum of the rows of g (ids.shape + (D,), float32 or bfloat16) whose token is v,
+    in binary32 and in a fixed order.  Tokens outside the table and padding_idx count for nothing.  out, accumulate: write, or add, to a given tensor."""
+    lib = load()
+    padding = -1 if padding_idx is None else int(padding_idx)
+    if accumulate and out is None:
+        raise ValueError("accumulate adds to a given tensor: pass out")
+    if out is None:
+        r = _native_result(_native.embed_grad(g, ids, vocab, float(scale), padding, _bf16_or_not(out_dtype)))
+        if r is not None:
+            return r
+    if not g.is_cuda or tuple(g.shape[:-1]) != tuple(ids.shape) or g.dim() < 1:
+        raise ValueError(f"a gradient {tuple(g.shape)} on {g.device} of ids {tuple(ids.shape)}")
+    dt = _dtype_code(g)
+    ids, bits = _ids(ids, g.device)
+    D, N = g.shape[-1], ids.numel()
+    g = _unit_columns(g.reshape(N, D))
+    if out is None:
+        out = torch.empty((vocab, D), dtype=out_dtype or g.dtype, device=g.device)
+    elif tuple(out.shape) != (vocab, D) or out.device != g.device or (out_dtype is not None and out.dtype != out_dtype):
+        raise ValueError(f"out has to be a {vocab} x {D} tensor of the wanted type on the gradient's device")
+    need = int(lib.nm_embed_grad_workspace(N, vocab, D))
+    ws = torch.empty(need, dtype=torch.uint8, device=g.device)
+    with torch.cuda.device(g.device):
+        _check(lib.nm_embed_grad(_ptr(g), _rowmajor(g, "g"), dt, _ptr(ids), bits, N, vocab, D, float(scale), padding, int(accumulate), _ptr(out), _rowmajor(out, "out"),
+                                 _dtype_code(out), _ptr(ws), need, _stream(g)))
+    return out
 
 
 # ---- the optimizer's step

@@ -330,3 +330,31 @@ class NMConv2d(torch.nn.Conv2d):
 
     def forward(self, x):
         return _NMConv2dFn.apply(x, self.weight, self.bias, self.stride, self.padding, self.dilation, self.cfg)
+
+
+class _NMEmbeddingFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, weight, ids, scale, padding_idx):
+        ctx.save_for_backward(ids)
+        ctx.vocab, ctx.scale, ctx.padding_idx, ctx.dtype = weight.shape[0], scale, padding_idx, weight.dtype
+        return api.nm_embed(weight, ids, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        ids, = ctx.saved_tensors
+        return api.nm_embed_grad(gy, ids, ctx.vocab, ctx.scale, padding_idx=ctx.padding_idx, out_dtype=ctx.dtype), None, None, None
+
+
+class NMEmbedding(torch.nn.Embedding):
+    """torch.nn.Embedding on the library's lookup and its gradient by sorted tokens, with a factor on the rows (e.g. sqrt(width)).  The gradient is dense and
+    the same bits every time."""
+
+    def __init__(self, num_embeddings: int, embedding_dim: int, padding_idx: Optional[int] = None, scale: float = 1.0, **kw):
+        super().__init__(num_embeddings, embedding_dim, padding_idx=padding_idx, **kw)
+        if self.max_norm is not None or self.scale_grad_by_freq or self.sparse:
+            raise ValueError("NMEmbedding has no max_norm, scale_grad_by_freq or sparse")
+        self.scale = scale
+
+    def forward(self, ids):
+        return _NMEmbeddingFn.apply(self.weight, ids, self.scale, self.padding_idx)

@@ -1,4 +1,4 @@
-// C ABI of the operators around the update phase: AdamW.  Host-side argument validation and dispatch, as in nm_abi.hip.
+// C ABI of the operators around the update phase: embedding, AdamW.  Host-side argument validation and dispatch, as in nm_abi.hip.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdarg.h>
@@ -37,9 +37,72 @@ struct Range { uintptr_t lo, hi; };
 inline Range range_of(const void *p, int64_t bytes) { return Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)(p && bytes > 0 ? bytes : 0)}; }
 inline bool overlap(const Range &a, const Range &b) { return a.lo < b.hi && b.lo < a.hi && a.lo != a.hi && b.lo != b.hi; }
 
+// rows x stride elements must stay far below 2^63 bytes: every byte range below is formed without overflow
+inline bool too_big(int64_t rows, int64_t stride)
+{
+    const int64_t lim = (int64_t)1 << 56;
+    return rows > lim || stride > lim || (rows > 0 && stride > 0 && rows > lim / stride);
+}
+// a matrix [R x C] of dt: sizes, stride, base
+int check_matrix(const char *fn, const char *what, const void *p, int64_t R, int64_t C, int64_t ld, int dt)
+{
+    if (!is_float(dt)) return fail(NM_ERR_DTYPE, "%s: %s is NM_F32 (0) or NM_BF16 (1), got %d", fn, what, dt);
+    if (R < 0 || C < 0 || too_big(R, C) || too_big(R, ld)) return fail(NM_ERR_SHAPE, "%s: %s has sizes %lld x %lld, row stride %lld", fn, what, (long long)R, (long long)C, (long long)ld);
+    if (R == 0 || C == 0) return NM_OK;
+    if (!p) return fail(NM_ERR_NULL, "%s: %s is NULL", fn, what);
+    if (R > 1 && ld < C) return fail(NM_ERR_SHAPE, "%s: row stride %lld of %s is smaller than %lld", fn, (long long)ld, what, (long long)C);
+    if (!aligned(p, esize(dt))) return fail(NM_ERR_ALIGN, "%s: %s is not on its elements' boundary", fn, what);
+    return NM_OK;
+}
+inline Range matrix_range(const void *p, int64_t R, int64_t C, int64_t ld, int dt) { return range_of(p, R > 0 && C > 0 ? ((R - 1) * ld + C) * esize(dt) : 0); }
+int check_ids(const char *fn, const void *ids, int bits, int64_t N)
+{
+    if (bits != 32 && bits != 64) return fail(NM_ERR_DTYPE, "%s: ids are 32 or 64 bits wide, got %d", fn, bits);
+    if (N < 0 || N > 0x7fffffff - 65536) return fail(NM_ERR_SHAPE, "%s: %lld tokens", fn, (long long)N);
+    if (N && !ids) return fail(NM_ERR_NULL, "%s: ids is NULL", fn);
+    if (N && !aligned(ids, bits / 8)) return fail(NM_ERR_ALIGN, "%s: ids are not on their elements' boundary", fn);
+    return NM_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int nm_embed(const void *table, int64_t V, int64_t D, int64_t ldt, int table_dtype, const void *ids, int id_bits, int64_t N, float scale, void *out, int64_t ldo,
+             int out_dtype, void *hip_stream)
+{
+    const char *fn = "nm_embed";
+    if (int rc = check_ids(fn, ids, id_bits, N)) return rc;
+    if (int rc = check_matrix(fn, "table", table, V, D, ldt, table_dtype)) return rc;
+    if (int rc = check_matrix(fn, "out", out, N, D, ldo, out_dtype)) return rc;
+    const Range ro = matrix_range(out, N, D, ldo, out_dtype);
+    if (overlap(ro, matrix_range(table, V, D, ldt, table_dtype)) || overlap(ro, range_of(ids, N * id_bits / 8))) return fail(NM_ERR_ALIAS, "%s: out must not overlap the table or the ids", fn);
+    return launched(fn, nm::launch_embed(table_dtype, out_dtype, table, V, D, ldt, ids, id_bits == 64, N, scale, out, ldo, (hipStream_t)hip_stream));
+}
+
+size_t nm_embed_grad_workspace(int64_t N, int64_t V, int64_t D)
+{
+    if (N <= 0 || V < 0 || D <= 0 || N > 0x7fffffff - 65536 || V > 0x7ffffffe || D > ((int64_t)1 << 32)) return 0;
+    return nm::embed_grad_workspace(N, V, D);
+}
+
+int nm_embed_grad(const void *g, int64_t ldg, int g_dtype, const void *ids, int id_bits, int64_t N, int64_t V, int64_t D, float scale, int64_t padding, int accumulate,
+                  void *out, int64_t ldo, int out_dtype, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const char *fn = "nm_embed_grad";
+    if (int rc = check_ids(fn, ids, id_bits, N)) return rc;
+    if (V > 0x7ffffffe || D > ((int64_t)1 << 32)) return fail(NM_ERR_SHAPE, "%s: a table of %lld x %lld", fn, (long long)V, (long long)D);
+    if (int rc = check_matrix(fn, "g", g, N, D, ldg, g_dtype)) return rc;
+    if (int rc = check_matrix(fn, "out", out, V, D, ldo, out_dtype)) return rc;
+    if (V == 0 || D == 0) { nm::abi_clear(); return NM_OK; }
+    const size_t need = nm_embed_grad_workspace(N, V, D);
+    if (need && (!workspace || workspace_bytes < need)) return fail(NM_ERR_WORKSPACE, "%s: workspace of %zu bytes required, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
+    if (need && !aligned(workspace, 16)) return fail(NM_ERR_ALIGN, "%s: workspace needs a 16-byte aligned base", fn);
+    const Range rg = matrix_range(g, N, D, ldg, g_dtype), ro = matrix_range(out, V, D, ldo, out_dtype), ri = range_of(ids, N * id_bits / 8), rw = range_of(workspace, (int64_t)need);
+    if (overlap(ro, rg) || overlap(ro, ri) || overlap(rw, ro) || overlap(rw, rg) || overlap(rw, ri))
+        return fail(NM_ERR_ALIAS, "%s: out and the workspace must not overlap an input or each other", fn);
+    return launched(fn, nm::launch_embed_grad(g_dtype, out_dtype, g, ldg, ids, id_bits == 64, N, V, D, scale, padding, accumulate != 0, out, ldo, workspace, (hipStream_t)hip_stream));
+}
 
 int nm_adamw(const nm_adamw_tensor *tensors, int count, int param_dtype, int grad_dtype, int state, double lr, double beta1, double beta2,
              double eps, double weight_decay, int64_t step, float grad_scale, const float *grad_scale_dev, uint64_t seed, void *hip_stream)

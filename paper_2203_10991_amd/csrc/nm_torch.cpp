@@ -35,6 +35,9 @@ decltype(&nm_linear_update_workspace) p_linear_update_workspace;
 decltype(&nm_linear_forward) p_linear_forward;
 decltype(&nm_linear_input_grad) p_linear_input_grad;
 decltype(&nm_adamw) p_adamw;
+decltype(&nm_embed) p_embed;
+decltype(&nm_embed_grad) p_embed_grad;
+decltype(&nm_embed_grad_workspace) p_embed_grad_workspace;
 PyObject *stream_of = nullptr;
 
 struct NoGil {                                                       // as a ctypes call does: a launch may wait for the queue
@@ -272,6 +275,73 @@ PyObject *linear_input_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- embedding.  embed(table, ids, scale, bf16 or None) -> out, of the table's type or bf16 (True) or binary32 (False)
+bool on_current_device(const at::Tensor &t) { return c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() == t.device(); }
+bool is_float(const at::Tensor &t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
+int code_of(at::ScalarType t) { return t == at::kFloat ? NM_F32 : NM_BF16; }
+int id_bits(const at::Tensor &ids) { return !ids.is_contiguous() ? 0 : ids.scalar_type() == at::kLong ? 64 : ids.scalar_type() == at::kInt ? 32 : 0; }
+
+PyObject *embed(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 4) return none();
+    const at::Tensor *table = gpu_tensor(a[0]), *ids = gpu_tensor(a[1]);
+    if (!table || !ids || !is_float(*table) || !PyFloat_Check(a[2]) || ids->device() != table->device() || !on_current_device(*table)) return none();
+    const int64_t ld = row_stride(*table);
+    const int bits = id_bits(*ids);
+    if (ld < 0 || !bits) return none();
+    const at::ScalarType type = a[3] == Py_None ? table->scalar_type() : a[3] == Py_True ? at::kBFloat16 : at::kFloat;
+    void *st;
+    if (!stream(*table, st)) return nullptr;
+    const int64_t N = ids->numel(), V = table->size(0), D = table->size(1);
+    at::DimVector size(ids->sizes().begin(), ids->sizes().end());
+    size.push_back(D);
+    at::Tensor out = empty(size, type, *table);
+    const void *pt = table->data_ptr(), *pi = ids->data_ptr();
+    void *po = out.data_ptr();
+    const float scale = (float)PyFloat_AS_DOUBLE(a[2]);
+    const int dt = code_of(table->scalar_type());
+    int rc;
+    {
+        NoGil free;
+        rc = p_embed(pt, V, D, ld, dt, pi, bits, N, scale, po, D, code_of(type), st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// embed_grad(g, ids, vocabulary, scale, padding, bf16 or None) -> the table's gradient
+PyObject *embed_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) return none();
+    const at::Tensor *g = gpu_tensor(a[0]), *ids = gpu_tensor(a[1]);
+    if (!g || !ids || !is_float(*g) || !whole_number(a[2]) || !PyFloat_Check(a[3]) || !whole_number(a[4]) || ids->device() != g->device() || !on_current_device(*g)) return none();
+    const int bits = id_bits(*ids);
+    if (!bits || g->dim() < 1 || g->size(-1) < 1 || g->dim() != ids->dim() + 1 || g->sizes().slice(0, ids->dim()) != ids->sizes()) return none();
+    const int64_t N = ids->numel(), D = g->size(-1), V = PyLong_AsLongLong(a[2]), padding = PyLong_AsLongLong(a[4]);
+    const int64_t ld = g->is_contiguous() ? D : g->dim() == 2 ? row_stride(*g) : -1;
+    if (PyErr_Occurred() || V < 0 || ld < 0) return PyErr_Occurred() ? nullptr : none();
+    const at::ScalarType type = a[5] == Py_None ? g->scalar_type() : a[5] == Py_True ? at::kBFloat16 : at::kFloat;
+    void *st;
+    if (!stream(*g, st)) return nullptr;
+    const size_t need = p_embed_grad_workspace(N, V, D);
+    at::Tensor out = empty({V, D}, type, *g), ws = empty({(int64_t)need}, at::kByte, *g);
+    const void *pg = g->data_ptr(), *pi = ids->data_ptr();
+    void *po = out.data_ptr(), *pw = ws.data_ptr();
+    const float scale = (float)PyFloat_AS_DOUBLE(a[3]);
+    const int dt = code_of(g->scalar_type());
+    int rc;
+    {
+        NoGil free;
+        rc = p_embed_grad(pg, ld, dt, pi, bits, N, V, D, scale, padding, 0, po, D, code_of(type), pw, need, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
 // ---- adamw(params, grads, ms, vs, masters or None, numbers or None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, grad_scale tensor or None, seed) -> True:
 // the step has been taken.  Lists of one length; one type of parameters, gradients and states, all on one device, a tensor's arrays with one dense layout.
 // A state is a binary32 tensor, or a pair of e4m3 codes and binary32 scales.
@@ -367,7 +437,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         {"mvue_prune_1of2", (void **)&p_prune_1of2}, {"mvue_prune_2of4", (void **)&p_prune_2of4}, {"nm_update_gemm", (void **)&p_update_gemm},
         {"nm_update_gemm_workspace", (void **)&p_update_gemm_workspace}, {"nm_linear_update", (void **)&p_linear_update},
         {"nm_linear_update_workspace", (void **)&p_linear_update_workspace}, {"nm_linear_forward", (void **)&p_linear_forward},
-        {"nm_linear_input_grad", (void **)&p_linear_input_grad}, {"nm_adamw", (void **)&p_adamw}};
+        {"nm_linear_input_grad", (void **)&p_linear_input_grad}, {"nm_adamw", (void **)&p_adamw}, {"nm_embed", (void **)&p_embed},
+        {"nm_embed_grad", (void **)&p_embed_grad}, {"nm_embed_grad_workspace", (void **)&p_embed_grad_workspace}};
     for (auto &f : all) {
         PyObject *address = PyDict_GetItemString(a[0], f.name);
         if (!address) { PyErr_Format(PyExc_KeyError, "%s", f.name); return nullptr; }
@@ -381,7 +452,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 #define NM_METHOD(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {NM_METHOD(bind), NM_METHOD(prune), NM_METHOD(update_gemm), NM_METHOD(linear_update), NM_METHOD(linear_forward), NM_METHOD(linear_input_grad), NM_METHOD(adamw),
+PyMethodDef methods[] = {NM_METHOD(bind), NM_METHOD(prune), NM_METHOD(update_gemm), NM_METHOD(linear_update), NM_METHOD(linear_forward), NM_METHOD(linear_input_grad), NM_METHOD(adamw), NM_METHOD(embed), NM_METHOD(embed_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_nm_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
