@@ -414,6 +414,33 @@ int nm_linear_forward(const void *x, int64_t ldx, const void *w, const void *bia
 int nm_linear_input_grad(const void *g, int64_t ldg, const void *w, int64_t T, int64_t O, int64_t I, void *dx, void *hip_stream);
 
 /*
+ * Products in 8-bit integers with a scale for each token (row of x) and each output channel (row of w):
+ *     y [T x O] = act(float(sum_i xq[t][i] wq[o][i]) * (xs[t] * ws[o]) + bias[o])
+ * 32-bit integer sums (I from 1 to 131072, which they hold), binary32 behind them, one rounding to y_dtype; act: max(., 0) where relu != 0 (a NaN
+ * stays one).  bias [O] of bias_dtype, NULL = none.  The input gradient of a layer is the same product, of the gradient's rows with the
+ * weights' columns (nm_quant_i8_t).
+ *
+ * nm_quant_i8: the rows of x [R x C] as codes and scales: a = max|x|, q = the integer nearest to x * (127 * (1 / a)), ties to even,
+ * scale = a / 127 (binary32, one rounding an operation).
+ * Codes in columns C .. ldq - 1 become zeros.  A row of zeros, or with a below 2^-110: zero codes and scale 0; a row that is not finite: zero
+ * codes and scale NaN (its products are NaN).  nm_quant_i8_t: the same of the columns of x, q [C x ldq] holding them as rows.
+ * nm_linear_i8: x [T x I] of x_dtype by nm_quant_i8's rule into the workspace, and the product, in one call.
+ *
+ * Codes: base and row stride multiples of 16 bytes, stride at most 2^21, each row readable up to its next multiple of 16; what stands there
+ * does not count.  x, bias and y: any stride and base on their elements' boundary (rows of x on 16-byte boundaries are read in vectors); rows of y at
+ * most 2^21 elements apart.  T and O up to 2^30.
+ */
+int nm_quant_i8(const void *x, int64_t R, int64_t C, int64_t ldx, int dtype, int8_t *q, int64_t ldq, float *scale, void *hip_stream);
+int nm_quant_i8_t(const void *x, int64_t R, int64_t C, int64_t ldx, int dtype, int8_t *q, int64_t ldq, float *scale, void *workspace, size_t workspace_bytes,
+                  void *hip_stream);
+size_t nm_quant_i8_t_workspace(int64_t R, int64_t C);
+int nm_gemm_i8(const int8_t *xq, int64_t ldx, const float *xs, const int8_t *wq, int64_t ldw, const float *ws, const void *bias, int bias_dtype, int64_t T, int64_t O,
+               int64_t I, int relu, void *y, int64_t ldy, int y_dtype, void *hip_stream);
+int nm_linear_i8(const void *x, int64_t ldx, int x_dtype, const int8_t *wq, int64_t ldw, const float *ws, const void *bias, int bias_dtype, int64_t T, int64_t O, int64_t I,
+                 int relu, void *y, int64_t ldy, int y_dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t nm_linear_i8_workspace(int64_t T, int64_t I);
+
+/*
  * Embedding: out[n] = scale * table[ids[n]], rounded once to out_dtype, and the table's gradient
  *     out[v] = (accumulate ? out[v] : 0) + scale * sum over the n with ids[n] = v of g[n]
  * table [V x D], g and out [N x D] (gradient: out [V x D]), row strides ldt, ldg, ldo in elements; ids of id_bits (32 or 64) bits.  Any sizes, strides and

@@ -102,6 +102,18 @@ def load():
     lib.nm_linear_forward.restype = i32
     lib.nm_linear_input_grad.argtypes = [vp, i64, vp, i64, i64, i64, vp, vp]
     lib.nm_linear_input_grad.restype = i32
+    lib.nm_quant_i8.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
+    lib.nm_quant_i8.restype = i32
+    lib.nm_quant_i8_t.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp, sz, vp]
+    lib.nm_quant_i8_t.restype = i32
+    lib.nm_quant_i8_t_workspace.argtypes = [i64, i64]
+    lib.nm_quant_i8_t_workspace.restype = sz
+    lib.nm_gemm_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i32, i64, i64, i64, i32, vp, i64, i32, vp]
+    lib.nm_gemm_i8.restype = i32
+    lib.nm_linear_i8.argtypes = [vp, i64, i32, vp, i64, vp, vp, i32, i64, i64, i64, i32, vp, i64, i32, vp, sz, vp]
+    lib.nm_linear_i8.restype = i32
+    lib.nm_linear_i8_workspace.argtypes = [i64, i64]
+    lib.nm_linear_i8_workspace.restype = sz
     lib.nm_embed.argtypes = [vp, i64, i64, i64, i32, vp, i32, i64, f32, vp, i64, i32, vp]
     lib.nm_embed.restype = i32
     lib.nm_embed_grad.argtypes = [vp, i64, i32, vp, i32, i64, i64, i64, f32, i64, i32, vp, i64, i32, vp, sz, vp]
@@ -121,7 +133,8 @@ def load():
         from . import _nm_torch as native
         native.bind({f: C.cast(getattr(lib, f), vp).value for f in (
             "mvue_prune_1of2", "mvue_prune_2of4", "nm_update_gemm", "nm_update_gemm_workspace", "nm_linear_update", "nm_linear_update_workspace",
-            "nm_linear_forward", "nm_linear_input_grad", "nm_adamw", "nm_embed", "nm_embed_grad", "nm_embed_grad_workspace")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
+            "nm_linear_forward", "nm_linear_input_grad", "nm_adamw", "nm_embed", "nm_embed_grad", "nm_embed_grad_workspace",
+            "nm_quant_i8", "nm_quant_i8_t", "nm_quant_i8_t_workspace", "nm_linear_i8", "nm_linear_i8_workspace")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
     except ImportError as e:
         warnings.warn(f"_nm_torch.so is not built for this torch ({e}): every call takes the slower way through ctypes and linear layers take the "
                       "framework's products until `python -m paper_2203_10991_amd.build` has run")
@@ -133,7 +146,7 @@ def load():
 
 class _NoNative:
     """In the place of _nm_torch: no call is its own."""
-    prune = update_gemm = linear_update = linear_forward = linear_input_grad = adamw = embed = embed_grad = staticmethod(lambda *a: None)
+    prune = update_gemm = linear_update = linear_forward = linear_input_grad = adamw = embed = embed_grad = quant_i8 = linear_i8 = staticmethod(lambda *a: None)
 
 
 def _native_result(r):
@@ -699,6 +712,113 @@ def own_linear_input_grad(g: torch.Tensor, weight: torch.Tensor) -> Optional[tor
         return None
     load()
     return _native_result(_native.linear_input_grad(g, weight))
+
+
+# ---- products in 8-bit integers
+
+def _quant_i8(x: torch.Tensor, columns: bool):
+    lib = load()
+    r = _native_result(_native.quant_i8(x, columns))
+    if r is not None:
+        return r
+    if not x.is_cuda or x.dim() != 2:
+        raise ValueError("x is a 2-D tensor on the GPU")
+    dt = _dtype_code(x)
+    x = _unit_columns(x)
+    R, Cc = x.shape
+    rows, cols = (Cc, R) if columns else (R, Cc)
+    q = torch.empty((rows, max(-(-cols // 128) * 128, 128)), dtype=torch.int8, device=x.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    with torch.cuda.device(x.device):
+        if columns:
+            need = int(lib.nm_quant_i8_t_workspace(R, Cc))
+            ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+            _check(lib.nm_quant_i8_t(_ptr(x), R, Cc, _rowmajor(x, "x"), dt, _ptr(q), q.shape[1], _ptr(scale), _ptr(ws), need, _stream(x)))
+        else:
+            _check(lib.nm_quant_i8(_ptr(x), R, Cc, _rowmajor(x, "x"), dt, _ptr(q), q.shape[1], _ptr(scale), _stream(x)))
+    return q[:, :cols], scale
+
+
+def nm_quant_i8(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(codes int8 [R x C], scales [R]) of the rows of x: codes = round(x * (127 * (1 / max|x|))), scale = max|x| / 127.  The codes' rows are laid out a
+    multiple of 128 bytes apart with zeros behind them."""
+    return _quant_i8(x, False)
+
+
+def nm_quant_i8_t(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """nm_quant_i8(x.t()): (codes int8 [C x R], scales [C]) of the columns of x."""
+    return _quant_i8(x, True)
+
+
+def _codes(q: torch.Tensor, scale: torch.Tensor, what: str, width: int, device) -> Tuple[torch.Tensor, int]:
+    """(codes, row stride) as the products read them; a copy where the rows do not start on 16-byte boundaries or end with the memory."""
+    if q.dtype != torch.int8 or scale.dtype != torch.float32:
+        raise TypeError(f"{what} is int8 codes and float32 scales, got {q.dtype} and {scale.dtype}")
+    if q.dim() != 2 or q.shape[1] != width or tuple(scale.shape) != (q.shape[0],) or q.device != device or scale.device != device:
+        raise ValueError(f"{what}: codes {tuple(q.shape)} and scales {tuple(scale.shape)} do not fit a width of {width}, or live elsewhere")
+    wide = -(-width // 16) * 16
+    ld = q.stride(0) if q.shape[0] > 1 else wide
+    end = q.storage_offset() + (q.shape[0] - 1) * ld + wide
+    if q.stride(1) != 1 or ld < wide or ld % 16 or q.data_ptr() % 16 or end > q.untyped_storage().nbytes():
+        p = torch.zeros((q.shape[0], wide), dtype=torch.int8, device=device)
+        p[:, :width] = q
+        return p, wide
+    return q, ld
+
+
+def _i8_result(x_rows: int, wq: torch.Tensor, bias: Optional[torch.Tensor], dtype: torch.dtype, device):
+    O, I = wq.shape
+    if I < 1:
+        raise ValueError("the reduction axis is empty")
+    if bias is not None and (tuple(bias.shape) != (O,) or bias.device != device):
+        raise ValueError(f"bias {tuple(bias.shape)} on {bias.device} for {O} outputs on {device}")
+    _bf16_or_not(dtype)
+    return torch.empty((x_rows, O), dtype=dtype, device=device), None if bias is None else bias.contiguous()
+
+
+def nm_gemm_i8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
+               out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """y [T x O] = (xq [T x I] wq [O x I]^T) * xs[:, None] * ws + bias, with the ReLU behind it where asked: 8-bit integer codes with a scale for each
+    row, 32-bit integer sums."""
+    lib = load()
+    if not xq.is_cuda:
+        raise ValueError("nm_gemm_i8 takes tensors on the GPU")
+    if wq.dim() != 2:
+        raise ValueError(f"wq is a matrix, got {tuple(wq.shape)}")
+    (O, I), device = wq.shape, xq.device
+    y, bias = _i8_result(xq.shape[0], wq, bias, out_dtype, device)
+    xq, ldx = _codes(xq, xs, "x", I, device)
+    wq, ldw = _codes(wq, ws, "w", I, device)
+    xs, ws = xs.contiguous(), ws.contiguous()
+    with torch.cuda.device(device):
+        _check(lib.nm_gemm_i8(_ptr(xq), ldx, _ptr(xs), _ptr(wq), ldw, _ptr(ws), _ptr(bias), 0 if bias is None else _dtype_code(bias), xq.shape[0], O, I, int(relu), _ptr(y), max(O, 1),
+                              _dtype_code(y), _stream(y)))
+    return y
+
+
+def nm_linear_i8(x: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False,
+                 out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """A linear layer over the last dimension of x (float32 or bfloat16) whose weights are 8-bit integers wq [O x I] with a scale ws [O] for each output: x is
+    rounded to 8-bit integers with a scale for each token, nm_gemm_i8 follows.  out_dtype: x's by default."""
+    lib = load()
+    r = _native_result(_native.linear_i8(x, wq, ws, bias, relu, _bf16_or_not(out_dtype)))
+    if r is not None:
+        return r
+    if not x.is_cuda or x.dim() < 1:
+        raise ValueError("nm_linear_i8 takes tensors on the GPU")
+    if wq.dim() != 2 or x.shape[-1] != wq.shape[1]:
+        raise ValueError(f"x {tuple(x.shape)} and wq {tuple(wq.shape)} do not fit")
+    (O, I), device, dt = wq.shape, x.device, _dtype_code(x)
+    shape, x = x.shape, _unit_columns(x.reshape(-1, I)) if I else x
+    y, bias = _i8_result(x.shape[0], wq, bias, out_dtype or x.dtype, device)
+    wq, ldw = _codes(wq, ws, "w", I, device)
+    ws = ws.contiguous()
+    need = int(lib.nm_linear_i8_workspace(x.shape[0], I))
+    work = torch.empty(need, dtype=torch.uint8, device=device)
+    with torch.cuda.device(device):
+        _check(lib.nm_linear_i8(_ptr(x), _rowmajor(x, "x"), dt, _ptr(wq), ldw, _ptr(ws), _ptr(bias), 0 if bias is None else _dtype_code(bias), x.shape[0], O, I, int(relu), _ptr(y),
+                                max(O, 1), _dtype_code(y), _ptr(work), need, _stream(x)))
+    return y.reshape(*shape[:-1], O)
 
 
 # ---- embedding

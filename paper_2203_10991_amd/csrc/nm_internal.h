@@ -164,12 +164,13 @@ hipError_t launch_dense_gemm(bool nn, const void *x, int64_t ldx, const void *w,
                              bool relu, hipStream_t st);
 
 // ---- 8-bit integer products of a linear layer
-// Rows of x [R x C] as 8-bit integers and a scale: a = max |x|, q = the integer nearest to x * (127 / a), ties to even, scale = a / 127.  Columns C .. ldq - 1 of q
+// Rows of x [R x C] as 8-bit integers and a scale: a = max |x|, q = the integer nearest to x * (127 * (1 / a)), ties to even, scale = a / 127.  Columns C .. ldq - 1 of q
 // become zeros.  ..._t: the columns of x instead, transposed: q [C x R]; part: C * quant_i8_slabs(R, C) words of workspace.
 hipError_t launch_quant_i8(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, hipStream_t st);
 int quant_i8_slabs(int64_t R, int64_t C);
 hipError_t launch_quant_i8_t(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, uint32_t *part, hipStream_t st);
-// y [M x N] = act((x w^T) xs ws + bias): x [M x K], row stride ldx, zeros from K to the next multiple of I8_K; w [N x K], row stride ldw (a multiple of 16)
+// y [M x N] = act((x w^T) xs ws + bias): x [M x K], w [N x K], row strides ldx and ldw multiples of 16, rows readable up to the next multiple of 16;
+// x_zeros: x's rows hold zeros up to the next multiple of I8_K
 constexpr int I8_K = 128;
 struct I8Arg {
     const int8_t *x, *w;
@@ -177,7 +178,7 @@ struct I8Arg {
     const void *bias;
     void *y;
     int64_t ldx, ldw, ldy, M, N, K;
-    int bias_dt, y_dt, relu;
+    int bias_dt, y_dt, relu, x_zeros;
 };
 hipError_t launch_gemm_i8(const I8Arg &p, hipStream_t st);
 

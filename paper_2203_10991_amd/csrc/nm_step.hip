@@ -1,4 +1,4 @@
-// C ABI of the operators around the update phase: embedding, AdamW.  Host-side argument validation and dispatch, as in nm_abi.hip.
+// C ABI of the operators around the update phase: 8-bit integer products, embedding, AdamW.  Host-side argument validation and dispatch, as in nm_abi.hip.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdarg.h>
@@ -64,9 +64,103 @@ int check_ids(const char *fn, const void *ids, int bits, int64_t N)
     return NM_OK;
 }
 
+constexpr int64_t I8_SIZE = (int64_t)1 << 30, I8_LD = (int64_t)1 << 21, I8_K_MOST = 131072;
+
+// codes [R x C] of 8-bit integers with a scale for each row
+int check_codes(const char *fn, const char *what, const int8_t *q, int64_t ld, const float *scale, int64_t R, int64_t C)
+{
+    if (R < 0 || C < 0 || R > I8_SIZE || C > I8_SIZE) return fail(NM_ERR_SHAPE, "%s: %s has sizes %lld x %lld", fn, what, (long long)R, (long long)C);
+    if (ld < C || ld % 16 || ld > I8_LD) return fail(ld % 16 ? NM_ERR_ALIGN : NM_ERR_SHAPE, "%s: row stride %lld of %s has to be a multiple of 16 from %lld to 2^21", fn, (long long)ld, what, (long long)C);
+    if (R == 0) return NM_OK;
+    if (!q || !scale) return fail(NM_ERR_NULL, "%s: %s and its scales must not be NULL", fn, what);
+    if (!aligned(q, 16) || !aligned(scale, 4)) return fail(NM_ERR_ALIGN, "%s: %s needs a 16-byte aligned base, its scales a 4-byte aligned one", fn, what);
+    return NM_OK;
+}
+inline Range codes_range(const int8_t *q, int64_t ld, int64_t R) { return range_of(q, R * ld); }
+// ... as an input: its last row may end with its last whole 16 bytes
+inline Range codes_in(const int8_t *q, int64_t ld, int64_t R, int64_t C) { return range_of(q, R ? (R - 1) * ld + (C + 15) / 16 * 16 : 0); }
+inline int64_t i8_row(int64_t I) { return (I + nm::I8_K - 1) / nm::I8_K * nm::I8_K; }
+
+// what the two products have in common: w, bias and y
+int check_product(const char *fn, const int8_t *wq, int64_t ldw, const float *ws, const void *bias, int bias_dtype, int64_t T, int64_t O, int64_t I, const void *y, int64_t ldy, int y_dtype)
+{
+    if (T < 0 || O < 0 || I < 1 || T > I8_SIZE || O > I8_SIZE || I > I8_K_MOST)
+        return fail(NM_ERR_SHAPE, "%s: T=%lld O=%lld I=%lld (I from 1 to 131072: the sums are 32-bit integers)", fn, (long long)T, (long long)O, (long long)I);
+    if (int rc = check_codes(fn, "w", wq, ldw, ws, O, I)) return rc;
+    if (int rc = check_matrix(fn, "y", y, T, O, ldy, y_dtype)) return rc;
+    if (ldy > I8_LD || O > I8_LD) return fail(NM_ERR_SHAPE, "%s: rows of y are at most 2^21 elements apart", fn);
+    if (bias && !is_float(bias_dtype)) return fail(NM_ERR_DTYPE, "%s: bias is NM_F32 (0) or NM_BF16 (1), got %d", fn, bias_dtype);
+    if (bias && !aligned(bias, esize(bias_dtype))) return fail(NM_ERR_ALIGN, "%s: bias is not on its elements' boundary", fn);
+    const Range ry = matrix_range(y, T, O, ldy, y_dtype);
+    if (overlap(ry, codes_in(wq, ldw, O, I)) || overlap(ry, range_of(ws, O * 4)) || overlap(ry, range_of(bias, O * esize(bias_dtype)))) return fail(NM_ERR_ALIAS, "%s: y must not overlap an input", fn);
+    return NM_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int nm_quant_i8(const void *x, int64_t R, int64_t C, int64_t ldx, int dtype, int8_t *q, int64_t ldq, float *scale, void *hip_stream)
+{
+    const char *fn = "nm_quant_i8";
+    if (int rc = check_matrix(fn, "x", x, R, C, ldx, dtype)) return rc;
+    if (int rc = check_codes(fn, "q", q, ldq, scale, R, C)) return rc;
+    const Range rx = matrix_range(x, R, C, ldx, dtype), rq = codes_range(q, ldq, R), rs = range_of(scale, R * 4);
+    if (overlap(rq, rx) || overlap(rs, rx) || overlap(rq, rs)) return fail(NM_ERR_ALIAS, "%s: q and scale must not overlap x or each other", fn);
+    return launched(fn, nm::launch_quant_i8(dtype, x, R, C, ldx, q, ldq, scale, (hipStream_t)hip_stream));
+}
+
+size_t nm_quant_i8_t_workspace(int64_t R, int64_t C) { return R < 0 || C <= 0 || R > I8_SIZE || C > I8_LD ? 0 : (size_t)nm::quant_i8_slabs(R, C) * (size_t)C * 4; }
+
+int nm_quant_i8_t(const void *x, int64_t R, int64_t C, int64_t ldx, int dtype, int8_t *q, int64_t ldq, float *scale, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const char *fn = "nm_quant_i8_t";
+    if (int rc = check_matrix(fn, "x", x, R, C, ldx, dtype)) return rc;
+    if (C > I8_LD) return fail(NM_ERR_SHAPE, "%s: %lld columns, 2^21 at most", fn, (long long)C);
+    if (int rc = check_codes(fn, "q", q, ldq, scale, C, R)) return rc;
+    const size_t need = nm_quant_i8_t_workspace(R, C);
+    if (need && (!workspace || workspace_bytes < need)) return fail(NM_ERR_WORKSPACE, "%s: workspace of %zu bytes required, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
+    if (need && !aligned(workspace, 16)) return fail(NM_ERR_ALIGN, "%s: workspace needs a 16-byte aligned base", fn);
+    const Range rx = matrix_range(x, R, C, ldx, dtype), rq = codes_range(q, ldq, C), rs = range_of(scale, C * 4), rw = range_of(workspace, (int64_t)need);
+    if (overlap(rq, rx) || overlap(rs, rx) || overlap(rq, rs) || overlap(rw, rx) || overlap(rw, rq) || overlap(rw, rs))
+        return fail(NM_ERR_ALIAS, "%s: q, scale and the workspace must not overlap x or each other", fn);
+    return launched(fn, nm::launch_quant_i8_t(dtype, x, R, C, ldx, q, ldq, scale, (uint32_t *)workspace, (hipStream_t)hip_stream));
+}
+
+int nm_gemm_i8(const int8_t *xq, int64_t ldx, const float *xs, const int8_t *wq, int64_t ldw, const float *ws, const void *bias, int bias_dtype, int64_t T, int64_t O,
+               int64_t I, int relu, void *y, int64_t ldy, int y_dtype, void *hip_stream)
+{
+    const char *fn = "nm_gemm_i8";
+    if (int rc = check_product(fn, wq, ldw, ws, bias, bias_dtype, T, O, I, y, ldy, y_dtype)) return rc;
+    if (int rc = check_codes(fn, "x", xq, ldx, xs, T, I)) return rc;
+    const Range ry = matrix_range(y, T, O, ldy, y_dtype);
+    if (overlap(ry, codes_in(xq, ldx, T, I)) || overlap(ry, range_of(xs, T * 4))) return fail(NM_ERR_ALIAS, "%s: y must not overlap an input", fn);
+    return launched(fn, nm::launch_gemm_i8(nm::I8Arg{xq, wq, xs, ws, bias, y, ldx, ldw, ldy, T, O, I, bias_dtype, y_dtype, relu, 0}, (hipStream_t)hip_stream));
+}
+
+size_t nm_linear_i8_workspace(int64_t T, int64_t I) { return T <= 0 || I < 1 || T > I8_SIZE || I > I8_K_MOST ? 0 : (size_t)T * (size_t)i8_row(I) + ((size_t)T * 4 + 15) / 16 * 16; }
+
+int nm_linear_i8(const void *x, int64_t ldx, int x_dtype, const int8_t *wq, int64_t ldw, const float *ws, const void *bias, int bias_dtype, int64_t T, int64_t O, int64_t I,
+                 int relu, void *y, int64_t ldy, int y_dtype, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const char *fn = "nm_linear_i8";
+    if (int rc = check_product(fn, wq, ldw, ws, bias, bias_dtype, T, O, I, y, ldy, y_dtype)) return rc;
+    if (int rc = check_matrix(fn, "x", x, T, I, ldx, x_dtype)) return rc;
+    if (T == 0 || O == 0) { nm::abi_clear(); return NM_OK; }
+    const size_t need = nm_linear_i8_workspace(T, I);
+    if (!workspace || workspace_bytes < need) return fail(NM_ERR_WORKSPACE, "%s: workspace of %zu bytes required, %zu given", fn, need, workspace ? workspace_bytes : (size_t)0);
+    if (!aligned(workspace, 16)) return fail(NM_ERR_ALIGN, "%s: workspace needs a 16-byte aligned base", fn);
+    const Range rx = matrix_range(x, T, I, ldx, x_dtype), ry = matrix_range(y, T, O, ldy, y_dtype), rw = range_of(workspace, (int64_t)need);
+    if (overlap(ry, rx) || overlap(rw, rx) || overlap(rw, ry) || overlap(rw, codes_in(wq, ldw, O, I)) || overlap(rw, range_of(ws, O * 4)) || overlap(rw, range_of(bias, O * esize(bias_dtype))))
+        return fail(NM_ERR_ALIAS, "%s: y and the workspace must not overlap an input or each other", fn);
+    const int64_t row = i8_row(I);
+    int8_t *q = (int8_t *)workspace;
+    float *s = (float *)(q + T * row);
+    hipStream_t st = (hipStream_t)hip_stream;
+    hipError_t e = nm::launch_quant_i8(x_dtype, x, T, I, ldx, q, row, s, st);
+    if (e == hipSuccess) e = nm::launch_gemm_i8(nm::I8Arg{q, wq, s, ws, bias, y, row, ldw, ldy, T, O, I, bias_dtype, y_dtype, relu, 1}, st);
+    return launched(fn, e);
+}
 
 int nm_embed(const void *table, int64_t V, int64_t D, int64_t ldt, int table_dtype, const void *ids, int id_bits, int64_t N, float scale, void *out, int64_t ldo,
              int out_dtype, void *hip_stream)

@@ -36,6 +36,11 @@ decltype(&nm_linear_forward) p_linear_forward;
 decltype(&nm_linear_input_grad) p_linear_input_grad;
 decltype(&nm_adamw) p_adamw;
 decltype(&nm_embed) p_embed;
+decltype(&nm_quant_i8) p_quant_i8;
+decltype(&nm_quant_i8_t) p_quant_i8_t;
+decltype(&nm_quant_i8_t_workspace) p_quant_i8_t_workspace;
+decltype(&nm_linear_i8) p_linear_i8;
+decltype(&nm_linear_i8_workspace) p_linear_i8_workspace;
 decltype(&nm_embed_grad) p_embed_grad;
 decltype(&nm_embed_grad_workspace) p_embed_grad_workspace;
 PyObject *stream_of = nullptr;
@@ -342,6 +347,79 @@ PyObject *embed_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- 8-bit integer products.  quant_i8(x, columns) -> (codes, scales) of the rows of x, or of its columns
+PyObject *quant_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 2) return none();
+    const at::Tensor *x = gpu_tensor(a[0]);
+    if (!x || !is_float(*x) || !on_current_device(*x)) return none();
+    const int64_t ld = row_stride(*x);
+    const bool turned = a[1] == Py_True;
+    void *st;
+    if (ld < 0) return none();
+    if (!stream(*x, st)) return nullptr;
+    const int64_t R = x->size(0), C = x->size(1), rows = turned ? C : R, cols = turned ? R : C, ldq = std::max<int64_t>((cols + 127) / 128 * 128, 128);
+    const size_t need = turned ? p_quant_i8_t_workspace(R, C) : 0;
+    at::Tensor q = empty({rows, ldq}, at::kChar, *x), s = empty({rows}, at::kFloat, *x), ws;
+    if (need) ws = empty({(int64_t)need}, at::kByte, *x);
+    const void *px = x->data_ptr();
+    int8_t *pq = (int8_t *)q.data_ptr();
+    float *ps = (float *)s.data_ptr();
+    void *pw = need ? ws.data_ptr() : nullptr;
+    const int dt = code_of(x->scalar_type());
+    int rc;
+    {
+        NoGil free;
+        rc = turned ? p_quant_i8_t(px, R, C, ld, dt, pq, ldq, ps, pw, need, st) : p_quant_i8(px, R, C, ld, dt, pq, ldq, ps, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    if (cols != ldq) q = q.narrow(1, 0, cols);
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(q)), THPVariable_Wrap(std::move(s)));
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_i8(x, wq, ws, bias or None, relu, bf16 or None) -> y: over the last dimension of x
+PyObject *linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) return none();
+    const at::Tensor *x = gpu_tensor(a[0]), *w = gpu_tensor(a[1]), *s = gpu_tensor(a[2]), *b = a[3] == Py_None ? nullptr : gpu_tensor(a[3]);
+    const int relu = PyObject_IsTrue(a[4]);
+    if (relu < 0) return nullptr;
+    if (!x || !w || !s || (a[3] != Py_None && !b) || !is_float(*x) || w->scalar_type() != at::kChar || s->scalar_type() != at::kFloat || x->dim() < 1 || w->dim() != 2 ||
+        x->size(-1) != w->size(1) || w->size(1) < 1 || s->dim() != 1 || s->size(0) != w->size(0) || !s->is_contiguous() || w->device() != x->device() ||
+        s->device() != x->device() || !on_current_device(*x))
+        return none();
+    const int64_t O = w->size(0), I = w->size(1), T = x->numel() / I;
+    if (b && (b->dim() != 1 || b->size(0) != O || !is_float(*b) || !b->is_contiguous() || b->device() != x->device())) return none();
+    const int64_t ldx = x->dim() == 2 ? row_stride(*x) : x->is_contiguous() ? I : -1;
+    // rows of codes on 16-byte boundaries, whose last one can be read to the end of its last 16 bytes
+    const int64_t ldw = O > 1 ? w->stride(0) : (I + 15) / 16 * 16;
+    const uintptr_t end = (uintptr_t)w->storage().data() + w->storage().nbytes();
+    if (ldx < 0 || w->stride(1) != 1 || ldw < I || ldw % 16 || (uintptr_t)w->data_ptr() % 16 || (uintptr_t)w->data_ptr() + (O - 1) * ldw + (I + 15) / 16 * 16 > end || O < 1) return none();
+    const at::ScalarType type = a[5] == Py_None ? x->scalar_type() : a[5] == Py_True ? at::kBFloat16 : at::kFloat;
+    void *st;
+    if (!stream(*x, st)) return nullptr;
+    at::DimVector size(x->sizes().begin(), x->sizes().end());
+    size.back() = O;
+    const size_t need = p_linear_i8_workspace(T, I);
+    at::Tensor y = empty(size, type, *x), ws = empty({(int64_t)need}, at::kByte, *x);
+    const void *px = x->data_ptr(), *pb = b ? b->data_ptr() : nullptr;
+    const int8_t *pw = (const int8_t *)w->data_ptr();
+    const float *ps = (const float *)s->data_ptr();
+    void *py = y.data_ptr(), *pk = ws.data_ptr();
+    const int xt = code_of(x->scalar_type()), bt = b ? code_of(b->scalar_type()) : 0;
+    int rc;
+    {
+        NoGil free;
+        rc = p_linear_i8(px, ldx, xt, pw, ldw, ps, pb, bt, T, O, I, relu, py, O, code_of(type), pk, need, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
 // ---- adamw(params, grads, ms, vs, masters or None, numbers or None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, grad_scale tensor or None, seed) -> True:
 // the step has been taken.  Lists of one length; one type of parameters, gradients and states, all on one device, a tensor's arrays with one dense layout.
 // A state is a binary32 tensor, or a pair of e4m3 codes and binary32 scales.
@@ -438,7 +516,9 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         {"nm_update_gemm_workspace", (void **)&p_update_gemm_workspace}, {"nm_linear_update", (void **)&p_linear_update},
         {"nm_linear_update_workspace", (void **)&p_linear_update_workspace}, {"nm_linear_forward", (void **)&p_linear_forward},
         {"nm_linear_input_grad", (void **)&p_linear_input_grad}, {"nm_adamw", (void **)&p_adamw}, {"nm_embed", (void **)&p_embed},
-        {"nm_embed_grad", (void **)&p_embed_grad}, {"nm_embed_grad_workspace", (void **)&p_embed_grad_workspace}};
+        {"nm_embed_grad", (void **)&p_embed_grad}, {"nm_embed_grad_workspace", (void **)&p_embed_grad_workspace},
+        {"nm_quant_i8", (void **)&p_quant_i8}, {"nm_quant_i8_t", (void **)&p_quant_i8_t}, {"nm_quant_i8_t_workspace", (void **)&p_quant_i8_t_workspace},
+        {"nm_linear_i8", (void **)&p_linear_i8}, {"nm_linear_i8_workspace", (void **)&p_linear_i8_workspace}};
     for (auto &f : all) {
         PyObject *address = PyDict_GetItemString(a[0], f.name);
         if (!address) { PyErr_Format(PyExc_KeyError, "%s", f.name); return nullptr; }
@@ -452,7 +532,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 #define NM_METHOD(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {NM_METHOD(bind), NM_METHOD(prune), NM_METHOD(update_gemm), NM_METHOD(linear_update), NM_METHOD(linear_forward), NM_METHOD(linear_input_grad), NM_METHOD(adamw), NM_METHOD(embed), NM_METHOD(embed_grad),
+PyMethodDef methods[] = {NM_METHOD(bind), NM_METHOD(prune), NM_METHOD(update_gemm), NM_METHOD(linear_update), NM_METHOD(linear_forward), NM_METHOD(linear_input_grad), NM_METHOD(adamw), NM_METHOD(embed), NM_METHOD(embed_grad), NM_METHOD(quant_i8), NM_METHOD(linear_i8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_nm_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -183,7 +183,7 @@ def test_layer(dtype):
             a = (layer(ids).double() * gy).sum()
             layer.weight.add_(d)
             b = (layer(ids).double() * gy).sum()
-        got = (layer.weight.grad.double() * d).sum()
+            got = (layer.weight.grad.double() * d).sum()
             size = (layer(ids).detach().double() * gy).abs().sum()
         assert abs(float(b - a - got.detach())) <= 1e-4 * float(size)
     with pytest.raises(ValueError):
