@@ -31,6 +31,9 @@ class NMConfig:
     # sparse MFMA (Sec. 5, 8-bit rows); "bf16x3": float32 tensors, the update GEMM through three bf16 terms per value
     # on the sparse 16-bit path
     precision: str = "native"
+    # the layer's dense products, linear layers only: "native": the tensors' own dtype; "i8": 8-bit integers with a scale for each token and each
+    # channel, x W^T from the rows of x and W, g W from the rows of g and the columns of W (rounded to nearest; dW is not touched by it)
+    dense: str = "native"
     step: int = 0              # iteration counter; advance() once per optimizer step
     # True: the layer that owns this configuration advances `step` itself after every backward pass (the default
     # configuration a layer makes for itself: a drop-in layer then draws fresh samples every `reuse_every`
@@ -163,8 +166,12 @@ def _one_call(g2: torch.Tensor, h2: torch.Tensor, weight: torch.Tensor, cfg: NMC
             and api.nm_linear_update_workspace(g2.shape[0], g2.shape[1], h2.shape[1], cfg.precision == "q8", bias) > 0)
 
 
-def _linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], relu: bool = False) -> torch.Tensor:
+def _linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], relu: bool = False, cfg: Optional[NMConfig] = None) -> torch.Tensor:
     """x W^T + b of eq. (1), and the ReLU behind it: the library's product where it takes the call, otherwise the framework's."""
+    if cfg is not None and cfg.dense != "native":
+        if cfg.dense != "i8":
+            raise ValueError(f"unknown dense product {cfg.dense!r}")
+        return api.nm_linear_i8(x, *api.nm_quant_i8(weight), bias, relu=relu)
     y = api.own_linear_forward(x, weight, bias, relu)
     if y is None:
         y = F.linear(x, weight, bias)
@@ -173,8 +180,10 @@ def _linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor],
     return y
 
 
-def _input_grad(g: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
+def _input_grad(g: torch.Tensor, weight: torch.Tensor, cfg: Optional[NMConfig] = None) -> torch.Tensor:
     """g W of eq. (2); the framework's where gradients are recorded (create_graph=True)."""
+    if cfg is not None and cfg.dense == "i8" and not torch.is_grad_enabled():
+        return api.nm_linear_i8(g, *api.nm_quant_i8_t(weight))
     dx = api.own_linear_input_grad(g, weight)
     return g @ weight if dx is None else dx
 
@@ -184,14 +193,14 @@ class _NMLinearFn(torch.autograd.Function):
     def forward(ctx, x, weight, bias, cfg):
         ctx.save_for_backward(x, weight)
         ctx.cfg, ctx.has_bias = cfg, bias is not None
-        return _linear(x, weight, bias)
+        return _linear(x, weight, bias, cfg=cfg)
 
     @staticmethod
     def backward(ctx, gy):
         x, weight = ctx.saved_tensors
         dW = db = None
         g2, h2, cfg = gy.reshape(-1, gy.shape[-1]), x.reshape(-1, x.shape[-1]), ctx.cfg
-        dx = _input_grad(gy, weight) if ctx.needs_input_grad[0] else None         # backward phase: dense (eq. (2))
+        dx = _input_grad(gy, weight, cfg) if ctx.needs_input_grad[0] else None         # backward phase: dense (eq. (2))
         bias = ctx.has_bias and ctx.needs_input_grad[2]
         bias_in_call = _bias_in_call(bias)
         if ctx.needs_input_grad[1] and _one_call(g2, h2, weight, cfg, bias_in_call):
@@ -224,7 +233,7 @@ class _NMLinearReLUFn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, cfg):
-        y = _linear(x, weight, bias, relu=True)
+        y = _linear(x, weight, bias, relu=True, cfg=cfg)
         ctx.save_for_backward(x, weight, y)               # relu'(z) = [y > 0]
         ctx.cfg, ctx.has_bias = cfg, bias is not None
         return y
@@ -260,7 +269,7 @@ class _NMLinearReLUFn(torch.autograd.Function):
                                                  stream_id=cfg.stream_id, bias=bias_in_call)
             elif ctx.needs_input_grad[1]:
                 dW = _update_gemm(g2, h2, cfg).to(weight.dtype)
-        dx = _input_grad(g2, weight).reshape(x.shape) if ctx.needs_input_grad[0] else None
+        dx = _input_grad(g2, weight, cfg).reshape(x.shape) if ctx.needs_input_grad[0] else None
         if bias and db is None:
             db = g2.sum(0)
         if cfg.auto_advance:
