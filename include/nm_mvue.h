@@ -461,7 +461,7 @@ size_t nm_embed_grad_workspace(int64_t N, int64_t V, int64_t D);
  *     g <- g * grad_scale * (grad_scale_dev ? *grad_scale_dev : 1)
  *     m <- beta1 m + (1 - beta1) g      v <- beta2 v + (1 - beta2) g^2
  *     p <- p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * binary32 throughout.  tensors: a HOST array of `count` entries, read before the call returns; arrays contiguous, n elements each:
+ * binary32 throughout, root and quotient to a unit in the last place (a v below 2^-126 has the root 0).  tensors: a HOST array of `count` entries, read before the call returns; arrays contiguous, n elements each:
  *   param, grad    of param_dtype and grad_dtype (NM_F32 or NM_BF16, one for all tensors of a call)
  *   master         binary32 copy of a bf16 parameter that takes the step in its place, the parameter is then its rounding; NULL = none,
  *                  for all tensors of a call
@@ -470,9 +470,9 @@ size_t nm_embed_grad_workspace(int64_t N, int64_t V, int64_t D);
  *   number         of the tensor, in the counter of its random words
  * NM_STATE_Q8 writes a block's scale as the smallest power of two that brings its largest finite magnitude to 448 or below (1 for a block of zeros,
  * exponents kept in [-126, 126]), and rounds a magnitude y / scale to one of its two e4m3 neighbours: up where its fraction of the
- * step plus r / 2^16 reaches 1 (below 2^-6 the step is 2^-9 and y / scale + 2^-6 is rounded to binary32 first).  r is half a word of
- * Philox4x32-10: key = seed, counter = (e/4 low, e/4 high, number, 2^31 + step), word e % 4 for element e, its low half for m and
- * its high half for sqrt(v).  sqrt(v) > 0 gets code 1 at least; what is not finite gets the NaN code.
+ * step plus r / 2^16 reaches 1 (the step below 2^-6 is 2^-9).  r is half a word of Philox4x32-10: key = seed, counter = (e/4 low,
+ * e/4 high, number, 2^31 + step), word e % 4 for element e, its low half for m and its high half for sqrt(v).  v > 0 gets code 1 at
+ * least; what is not finite gets a NaN code.
  * Bases on their elements' boundary; on 16-byte boundaries they are read in vectors.  The arrays of a tensor, and those of different
  * tensors, must not overlap (checked within a tensor).
  */

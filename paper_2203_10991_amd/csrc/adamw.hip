@@ -20,7 +20,7 @@ namespace nm {
 
 namespace {
 
-constexpr int AB = 256;          // elements of a block with one scale: a quad for each lane of a wave
+constexpr int AB = 256;          // elements of a block with one scale: a quad for each lane of a wave, which takes one block
 
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
@@ -71,19 +71,18 @@ __device__ __forceinline__ int block_exponent(uint32_t top)
     const int e = (int)(top >> 23) - 135 + ((top & 0x7fffffu) > 0x600000u);
     return top ? min(max(e, -126), 126) : 0;
 }
-// e4m3 code of |u| = y (at most 448), rounded by 16 random bits.  The binary32 pattern of y holds the three bits that are kept at 20; below 2^-6, where
-// the grid is even, y + 2^-6 does.
-__device__ __forceinline__ uint32_t e4m3_code(float y, uint32_t random16)
+// r over its block's scale: at most 448 (a root that is a unit too large must not pass it), and where v > 0 at least the smallest code's value; infinities and
+// NaN as they are
+__device__ __forceinline__ float code_input(float y, float v)
 {
-    const bool small = y < 0x1p-6f;
-    const uint32_t t = __float_as_uint(small ? y + 0x1p-6f : y) + (random16 << 4);
-    return (t >> 20) - (small ? 968u : 960u);
+    const float least = v > 0.f ? 0x1p-9f : 0.f;
+    return v < __builtin_inff() ? __builtin_amdgcn_fmed3f(y, least, 448.f) : v;
 }
 
 struct AdamwArg {
     AdamwTensor t[ADAMW_MOST];
     int first[ADAMW_MOST];       // first workgroup of a tensor
-    int count, per_wave;         // blocks of 256 that a wave takes
+    int count;
     float b1, c1, b2, c2, rate, grow, eps, keep, scale;
     const float *scale_dev;
     uint32_t seed_lo, seed_hi, step;
@@ -110,10 +109,10 @@ __device__ __forceinline__ void load_block(const AdamwTensor &t, int64_t at, int
                 }
         }
         const float ms = t.m_scale[at / AB], vs = t.v_scale[at / AB];
-        x.m[0] = __builtin_amdgcn_cvt_f32_fp8(mc, 0) * ms; x.m[1] = __builtin_amdgcn_cvt_f32_fp8(mc, 1) * ms;
-        x.m[2] = __builtin_amdgcn_cvt_f32_fp8(mc, 2) * ms; x.m[3] = __builtin_amdgcn_cvt_f32_fp8(mc, 3) * ms;
-        x.v[0] = __builtin_amdgcn_cvt_f32_fp8(vc, 0) * vs; x.v[1] = __builtin_amdgcn_cvt_f32_fp8(vc, 1) * vs;
-        x.v[2] = __builtin_amdgcn_cvt_f32_fp8(vc, 2) * vs; x.v[3] = __builtin_amdgcn_cvt_f32_fp8(vc, 3) * vs;
+        const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc, true),
+                   v01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vc, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vc, true);
+        x.m[0] = m01[0] * ms; x.m[1] = m01[1] * ms; x.m[2] = m23[0] * ms; x.m[3] = m23[1] * ms;
+        x.v[0] = v01[0] * vs; x.v[1] = v01[1] * vs; x.v[2] = v23[0] * vs; x.v[3] = v23[1] * vs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x.v[i] = x.v[i] * x.v[i];
     } else {
@@ -131,40 +130,36 @@ __device__ __forceinline__ void step_block(const AdamwArg &a, const AdamwTensor 
         const float g = x.g[i] * gs;
         x.m[i] = x.m[i] * a.b1 + g * a.c1;
         x.v[i] = x.v[i] * a.b2 + (g * g) * a.c2;
-        r[i] = sqrtf(x.v[i]);
-        x.p[i] = x.p[i] * a.keep - (x.m[i] * a.rate) / (r[i] * a.grow + a.eps);
+        // (the root and the quotient to a unit in the last place: correctly rounded they took a quarter of the kernel's instructions)
+        r[i] = __builtin_amdgcn_sqrtf(x.v[i]);
+        x.p[i] = x.p[i] * a.keep - (x.m[i] * a.rate) * __builtin_amdgcn_rcpf(r[i] * a.grow + a.eps);
     }
     if constexpr (Q8) {
         uint32_t mt = 0, vt = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t mb = __float_as_uint(x.m[i]) & 0x7fffffffu, vb = __float_as_uint(r[i]) & 0x7fffffffu;
+            const uint32_t mb = __float_as_uint(x.m[i]) & 0x7fffffffu, vb = __float_as_uint(x.v[i]);
             if (i < left) {
                 mt = max(mt, mb < 0x7f800000u ? mb : 0u);
                 vt = max(vt, vb < 0x7f800000u ? vb : 0u);
             }
         }
-        const int me = block_exponent(wave_max(mt)), ve = block_exponent(wave_max(vt));
+        // (the block's root is rounded correctly, so that its scale is the one of the definition to the last bit)
+        const int me = block_exponent(wave_max(mt)), ve = block_exponent(__float_as_uint(sqrtf(__uint_as_float(wave_max(vt)))));
         const float down_m = __uint_as_float((uint32_t)(127 - me) << 23), down_v = __uint_as_float((uint32_t)(127 - ve) << 23);
         uint32_t w[4];
         const uint64_t quad = (uint64_t)at >> 2;
-        philox4x32_10_uniform_c123((uint32_t)quad, __builtin_amdgcn_readfirstlane((uint32_t)(quad >> 32)), t.number,
-                                   0x80000000u + a.step, a.seed_lo, a.seed_hi, w);
-        uint32_t mc = 0, vc = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t mb = __float_as_uint(x.m[i]), am = mb & 0x7fffffffu, av = __float_as_uint(r[i]) & 0x7fffffffu;
-            const float ym = __uint_as_float(am) * down_m, yv = __uint_as_float(av) * down_v;
-            uint32_t cm = e4m3_code(ym, w[i] & 0xffffu) | (mb >> 24 & 0x80u), cv = e4m3_code(yv, w[i] >> 16);
-            if (yv > 0.f) cv = max(cv, 1u);
-            if (am >= 0x7f800000u) cm = 0x7fu;
-            if (av >= 0x7f800000u) cv = 0x7fu;
-            mc |= cm << (8 * i);
-            vc |= cv << (8 * i);
-        }
+        philox4x32_10_uniform_c123((uint32_t)quad, __builtin_amdgcn_readfirstlane((uint32_t)(quad >> 32)), t.number, 0x80000000u + a.step, a.seed_lo, a.seed_hi, w);
+        // v_cvt_sr_fp8_f32 adds the upper 20 bits of its random word to what lies behind the bits that stay, and cuts: what is not finite becomes a NaN
+        int mc = 0, vc = 0;
+#define NM_CODE(I)                                                                                                                          \
+        mc = __builtin_amdgcn_cvt_sr_fp8_f32(x.m[I] * down_m, (int)(w[I] << 16), mc, I);                                                    \
+        vc = __builtin_amdgcn_cvt_sr_fp8_f32(code_input(r[I] * down_v, x.v[I]), (int)(w[I] & 0xffff0000u), vc, I)
+        NM_CODE(0); NM_CODE(1); NM_CODE(2); NM_CODE(3);
+#undef NM_CODE
         if constexpr (VEC) {
-            *(uint32_t *)((uint8_t *)t.m + at) = mc;
-            *(uint32_t *)((uint8_t *)t.v + at) = vc;
+            *(int *)((uint8_t *)t.m + at) = mc;
+            *(int *)((uint8_t *)t.v + at) = vc;
         } else {
             for (int i = 0; i < 4; ++i)
                 if (i < left) {
@@ -195,19 +190,16 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArg a)
     const AdamwTensor t = a.t[k];
     const float gs = a.scale_dev ? a.scale * *a.scale_dev : a.scale;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int64_t block = ((int64_t)(blockIdx.x - a.first[k]) * 4 + wave) * a.per_wave;
-    const int64_t end = min(block + a.per_wave, (t.n + AB - 1) / AB);
-    for (; block < end; ++block) {
-        const int64_t base = block * AB, at = base + 4 * lane;
-        Quad x;
-        if (t.aligned && base + AB <= t.n) {
-            load_block<PT, GT, Q8, MASTER, true>(t, at, 4, x);
-            step_block<PT, GT, Q8, MASTER, true>(a, t, gs, at, 4, x);
-        } else {
-            const int left = (int)max(min(t.n - at, (int64_t)4), (int64_t)0);
-            load_block<PT, GT, Q8, MASTER, false>(t, at, left, x);
-            step_block<PT, GT, Q8, MASTER, false>(a, t, gs, at, left, x);
-        }
+    const int64_t base = ((int64_t)(blockIdx.x - a.first[k]) * 4 + wave) * AB, at = base + 4 * lane;
+    if (base >= t.n) return;
+    Quad x;
+    if (t.aligned && base + AB <= t.n) {
+        load_block<PT, GT, Q8, MASTER, true>(t, at, 4, x);
+        step_block<PT, GT, Q8, MASTER, true>(a, t, gs, at, 4, x);
+    } else {
+        const int left = (int)max(min(t.n - at, (int64_t)4), (int64_t)0);
+        load_block<PT, GT, Q8, MASTER, false>(t, at, left, x);
+        step_block<PT, GT, Q8, MASTER, false>(a, t, gs, at, left, x);
     }
 }
 
@@ -224,12 +216,11 @@ hipError_t launch_adamw(const AdamwTensor *tensors, int count, int param_dt, int
     a.scale = r.grad_scale; a.scale_dev = r.grad_scale_dev;
     a.seed_lo = (uint32_t)seed; a.seed_hi = (uint32_t)(seed >> 32); a.step = (uint32_t)r.step;
     a.count = count;
-    a.per_wave = 4;
     int64_t wgs = 0;
     for (int k = 0; k < count; ++k) {
         a.t[k] = tensors[k];
         a.first[k] = (int)wgs;
-        wgs += (tensors[k].n + (int64_t)AB * 4 * a.per_wave - 1) / ((int64_t)AB * 4 * a.per_wave);
+        wgs += (tensors[k].n + AB * 4 - 1) / (AB * 4);
         if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
     }
     if (!wgs) return hipSuccess;
