@@ -2,11 +2,11 @@
 //     out[n] = scale E[id_n]                     dE[v] = scale * sum over the tokens n with id_n = v of g[n], in the order of n
 // The gradient's tokens are sorted by id, stably, and each row's sum runs over its tokens in their order in binary32: the result does not depend on the
 // launch, and a row that half of the tokens share costs no more than as many rows with a token each.
-//   sort    up to RANK_MOST tokens, one launch: the rank of a token is the number of tokens whose (id, position) is smaller, which 64 x 4 threads count
-//           for 64 tokens from LDS.  Beyond, radix passes of at most 9 bits, a counting launch and a moving one each.
-//           Workgroups behind those of the first launch fill the gradient with zeros meanwhile.
-//   sum     a workgroup takes CHUNK consecutive tokens of the sorted list and a slab of columns.  Rows whose tokens all lie inside are written; the sums of
-//           a row that began in an earlier chunk, or runs on into the next one, go to the workspace.
+//   sort    up to RANK_MOST tokens, one launch: the rank of a token is the number of tokens whose (id, position) is smaller, which 16 waves count
+//           for 64 tokens from LDS.  Up to MERGE_MOST, two: chunks of 256 tokens sorted that way, and merged.  Beyond, radix passes of at most 9 bits, a counting
+//           launch and a moving one each.  Workgroups behind those of the first launch fill the gradient with zeros meanwhile.
+//   sum     a workgroup takes CHUNK consecutive tokens of the sorted list and a slab of columns.  A row with at most LIGHT tokens is summed, and written, where
+//           it begins; of a longer one each chunk leaves its part in the workspace.
 //   join    those rows: the chunk where a row begins adds up its parts, chunk after chunk.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -14,154 +14,182 @@
 #include <algorithm>
 
 #include "nm_internal.h"
+#include "gemm_plan.h"           // NM_CUS
 #include "prune_common.h"        // Row, pack_bf16_rne
 
 namespace nm {
 
 namespace {
 
-__device__ __forceinline__ int64_t id_at(const void *ids, bool wide, int64_t n)
-{
-    return wide ? ((const int64_t *)ids)[n] : (int64_t)((const int32_t *)ids)[n];
-}
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-// W elements of a row as binary32, and back.  VEC: W elements fill 16 bytes of the wider of the two types, on a boundary of their size.
-template <int DT, int W, bool VEC> __device__ __forceinline__ void load_row(const void *p, int64_t at, int left, float (&v)[W])
+// Tokens: 32 or 64 bits wide, read as words of 32 without a branch (a branch for each load would have it waited for before the next one is sent)
+struct Ids { const uint32_t *at; int words; };
+// the token at n where it lies in 0 .. V - 1, otherwise V
+__device__ __forceinline__ uint32_t token_at(const Ids &ids, int64_t n, int64_t V)
 {
-    if constexpr (VEC && DT == NM_DT_F32) {
-#pragma unroll
-        for (int i = 0; i < W; i += 4) {
-            const float4 x = *(const float4 *)((const float *)p + at + i);
-            v[i] = x.x; v[i + 1] = x.y; v[i + 2] = x.z; v[i + 3] = x.w;
-        }
-    } else if constexpr (VEC && W == 8) {
-        const uint4 x = *(const uint4 *)((const uint16_t *)p + at);
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = Row<NM_DT_BF16>::get(x, i);
-    } else if constexpr (VEC) {
-        const uint2 x = *(const uint2 *)((const uint16_t *)p + at);
-        v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u); v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            v[i] = 0.f;
-            if (i < left) v[i] = DT == NM_DT_F32 ? ((const float *)p)[at + i] : __uint_as_float((uint32_t)((const uint16_t *)p)[at + i] << 16);
-        }
-    }
-}
-template <int DT, int W, bool VEC> __device__ __forceinline__ void store_row(void *p, int64_t at, int left, const float (&v)[W])
-{
-    if constexpr (VEC && DT == NM_DT_F32) {
-#pragma unroll
-        for (int i = 0; i < W; i += 4) *(float4 *)((float *)p + at + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    } else if constexpr (VEC && W == 8) {
-        *(uint4 *)((uint16_t *)p + at) = make_uint4(pack_bf16_rne(v[0], v[1]), pack_bf16_rne(v[2], v[3]), pack_bf16_rne(v[4], v[5]), pack_bf16_rne(v[6], v[7]));
-    } else if constexpr (VEC) {
-        *(uint2 *)((uint16_t *)p + at) = make_uint2(pack_bf16_rne(v[0], v[1]), pack_bf16_rne(v[2], v[3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            if (i < left) {
-                if constexpr (DT == NM_DT_F32) ((float *)p)[at + i] = v[i];
-                else                           ((uint16_t *)p)[at + i] = (uint16_t)pack_bf16_rne(v[i], v[i]);
-            }
-    }
+    const uint32_t lo = ids.at[n * ids.words], hi = ids.at[n * ids.words + ids.words - 1];
+    return (ids.words == 2 ? hi == 0 : (int32_t)lo >= 0) && lo < (uint64_t)V ? lo : (uint32_t)V;
 }
 
 constexpr int EW = 8;            // elements of a row that a thread takes at a time: 16 bytes of bf16, 32 of binary32
 
+// EW elements of a row as they are stored, as binary32, and back.  Rows start on any element's boundary, which vector loads and stores here do not mind.  The last
+// of a row's threads takes the row's last EW elements, those that its neighbour has too among them, and leaves them alone where it adds (`skip`: how many).
+// NARROW: a row has fewer, `left`.
+template <int DT> struct Raw;
+template <> struct Raw<NM_DT_F32> { u32x4 v[2]; };
+template <> struct Raw<NM_DT_BF16> { u32x4 v[1]; };
+template <int DT, bool NARROW = false> __device__ __forceinline__ Raw<DT> load_raw(const void *p, int64_t at, int left = EW)
+{
+    Raw<DT> r;
+    if constexpr (DT == NM_DT_F32) {
+        typedef u32x4 any __attribute__((aligned(4)));
+        const uint32_t *from = (const uint32_t *)p + at;
+        if constexpr (!NARROW) { r.v[0] = *(const any *)from; r.v[1] = *(const any *)(from + 4); }
+        else
+#pragma unroll
+            for (int i = 0; i < EW; ++i) r.v[i / 4][i % 4] = i < left ? from[i] : 0u;
+    } else {
+        typedef u32x4 any __attribute__((aligned(2)));
+        const uint16_t *from = (const uint16_t *)p + at;
+        if constexpr (!NARROW) r.v[0] = *(const any *)from;
+        else
+#pragma unroll
+            for (int i = 0; i < EW; i += 2) r.v[0][i / 2] = (i < left ? (uint32_t)from[i] : 0u) | (i + 1 < left ? (uint32_t)from[i + 1] << 16 : 0u);
+    }
+    return r;
+}
+template <int DT> __device__ __forceinline__ float element(const Raw<DT> &r, int i)
+{
+    if constexpr (DT == NM_DT_F32) return __uint_as_float(r.v[i / 4][i % 4]);
+    else return __uint_as_float(i & 1 ? r.v[0][i / 2] & 0xffff0000u : r.v[0][i / 2] << 16);
+}
+template <int DT> __device__ __forceinline__ void store_row(void *p, int64_t at, int skip, int left, const float (&v)[EW])
+{
+    if constexpr (DT == NM_DT_F32) {
+        typedef u32x4 any __attribute__((aligned(4)));
+        float *to = (float *)p + at;
+        if (skip == 0 && left >= EW)
+#pragma unroll
+            for (int i = 0; i < EW; i += 4) *(any *)(to + i) = u32x4{__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])};
+        else
+#pragma unroll
+            for (int i = 0; i < EW; ++i)
+                if (i >= skip && i < left) to[i] = v[i];
+    } else {
+        typedef u32x4 any __attribute__((aligned(2)));
+        uint16_t *to = (uint16_t *)p + at;
+        const u32x4 w = {pack_bf16_rne(v[0], v[1]), pack_bf16_rne(v[2], v[3]), pack_bf16_rne(v[4], v[5]), pack_bf16_rne(v[6], v[7])};
+        if (skip == 0 && left >= EW) *(any *)to = w;
+        else
+#pragma unroll
+            for (int i = 0; i < EW; ++i)
+                if (i >= skip && i < left) to[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    }
+}
+
 // ---- lookup: 2^shift threads to a row
-template <int TT, int OT, bool VEC>
-__global__ __launch_bounds__(256) void embed_kernel(const void *table, int64_t V, int64_t D, int64_t ldt, const void *ids, bool wide, int64_t N, float scale,
-                                                    void *out, int64_t ldo, int shift)
+template <int TT, int OT, bool NARROW>
+__global__ __launch_bounds__(256) void embed_kernel(const void *table, int64_t V, int64_t D, int64_t ldt, Ids ids, int64_t N, float scale, void *out, int64_t ldo, int shift)
 {
     const int64_t n = (int64_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
     if (n >= N) return;
-    const int64_t id = id_at(ids, wide, n);
-    const bool there = id >= 0 && id < V;                            // (a token outside the table: a row of NaN, nothing is read)
+    const int64_t id = token_at(ids, n, V);
+    const bool there = id < V;                                       // (a token outside the table: a row of NaN, nothing is read)
     const int64_t step = (int64_t)EW << shift;
-    for (int64_t c = (int64_t)(threadIdx.x & ((1 << shift) - 1)) * EW; c < D; c += step) {
-        const int left = (int)min(D - c, (int64_t)EW);
+    for (int64_t c0 = (int64_t)(threadIdx.x & ((1 << shift) - 1)) * EW; c0 < D; c0 += step) {
+        const int64_t c = NARROW ? c0 : min(c0, D - EW);             // (the row's last elements are written twice, with the same values)
+        const int left = NARROW ? (int)D : EW;
         float v[EW];
         if (there) {
-            if (VEC && left == EW) load_row<TT, EW, true>(table, id * ldt + c, left, v); else load_row<TT, EW, false>(table, id * ldt + c, left, v);
+            const Raw<TT> r = load_raw<TT, NARROW>(table, id * ldt + c, left);
 #pragma unroll
-            for (int i = 0; i < EW; ++i) v[i] *= scale;
+            for (int i = 0; i < EW; ++i) v[i] = element(r, i) * scale;
         } else
 #pragma unroll
             for (int i = 0; i < EW; ++i) v[i] = __uint_as_float(0x7fc00000u);
-        if (VEC && left == EW) store_row<OT, EW, true>(out, n * ldo + c, left, v); else store_row<OT, EW, false>(out, n * ldo + c, left, v);
+        store_row<OT>(out, n * ldo + c, 0, left, v);
     }
 }
 
 // ---- the gradient's sort
-constexpr int64_t RANK_MOST = 8192;
+constexpr int RANK_MOST = 4096, MERGE_MOST = 32768;
 constexpr int RADIX_BITS = 9, RADIX_BINS = 1 << RADIX_BITS, KEYS = 2048;     // keys of a workgroup in a radix pass: KEYS or a multiple
 
 struct Fill { char *at; int64_t rows, row_bytes, stride_bytes; };            // rows that become zeros; rows == 0: none
-// rows are taken as one run of bytes where they are contiguous
-__device__ void fill_zeros(const Fill &f, int64_t wg, int64_t wgs)
+// Rows are taken as one run of bytes where they are contiguous, FILL of them to a workgroup: 983 MB take 144 us (6.8 TB/s) in workgroups of their own, 190 us dealt in
+// turn to the threads of 2048.
+constexpr int FILL = 16384;
+template <int THREADS> __device__ __forceinline__ void fill_zeros(const Fill &f, int64_t wg, int64_t wgs)
 {
-    const int64_t tid = wg * blockDim.x + threadIdx.x, all = wgs * blockDim.x;
     if (f.row_bytes == f.stride_bytes && ((uintptr_t)f.at & 15) == 0) {
         const int64_t bytes = f.rows * f.row_bytes, n = bytes / 16;
         const uint4 z = make_uint4(0, 0, 0, 0);
-        for (int64_t i = tid; i < n; i += all) ((uint4 *)f.at)[i] = z;
-        for (int64_t i = n * 16 + 2 * tid; i < bytes; i += 2 * all) *(uint16_t *)(f.at + i) = 0;
+        for (int64_t i = wg * (FILL / 16) + threadIdx.x; i < n; i += wgs * (FILL / 16))
+#pragma unroll
+            for (int j = 0; j < FILL / 16; j += THREADS)
+                if (i + j < n) ((uint4 *)f.at)[i + j] = z;
+        if (wg == 0)
+            for (int64_t i = n * 16 + 2 * threadIdx.x; i < bytes; i += 2 * THREADS) *(uint16_t *)(f.at + i) = 0;
     } else {
         for (int64_t r = wg; r < f.rows; r += wgs)
-            for (int64_t i = 2 * threadIdx.x; i < f.row_bytes; i += 2 * blockDim.x) *(uint16_t *)(f.at + r * f.stride_bytes + i) = 0;
+            for (int64_t i = 2 * threadIdx.x; i < f.row_bytes; i += 2 * THREADS) *(uint16_t *)(f.at + r * f.stride_bytes + i) = 0;
     }
 }
 
 // the key of a token: its id, or V where it counts for nothing
-__device__ __forceinline__ uint32_t key_of(const void *ids, bool wide, int64_t n, int64_t V, int64_t padding)
+__device__ __forceinline__ uint32_t key_of(const Ids &ids, int64_t n, int64_t V, int64_t padding)
 {
-    const int64_t id = id_at(ids, wide, n);
-    return id < 0 || id >= V || id == padding ? (uint32_t)V : (uint32_t)id;
+    const uint32_t id = token_at(ids, n, V);
+    return (int64_t)id == padding ? (uint32_t)V : id;
 }
 
-// rank by counting: N <= RANK_MOST tokens, 13 bits of position behind the id's
-__global__ __launch_bounds__(256) void embed_rank_kernel(const void *ids, bool wide, int N, int64_t V, int64_t padding, int sort_wgs, uint32_t *keys, uint32_t *perm, Fill f)
+// Rank by counting: a wave counts for 64 tokens through a sixteenth of the list.  Keys in order of their tokens compare by key alone: of the tokens before a token those
+// with its key count too.
+__global__ __launch_bounds__(1024) void embed_rank_kernel(Ids ids, int N, int64_t V, int64_t padding, int sort_wgs, uint32_t *keys, uint32_t *perm, uint32_t *heavy, Fill f)
 {
-    if ((int)blockIdx.x >= sort_wgs) { fill_zeros(f, (int)blockIdx.x - sort_wgs, (int)gridDim.x - sort_wgs); return; }
-    extern __shared__ __attribute__((aligned(16))) uint2 all[];              // (position, key) of each token
+    if (heavy && blockIdx.x == 0 && threadIdx.x == 0) *heavy = 0;
+    if ((int)blockIdx.x >= sort_wgs) { fill_zeros<1024>(f, (int)blockIdx.x - sort_wgs, (int)gridDim.x - sort_wgs); return; }
+    __shared__ __attribute__((aligned(16))) uint32_t all[RANK_MOST];
     __shared__ int rank[64];
-    const int tid = threadIdx.x, lane = tid & 63, part = tid >> 6;
-    const int padded = (N + 7) & ~7;
-    for (int n = tid; n < padded; n += 256) all[n] = n < N ? make_uint2((uint32_t)n, key_of(ids, wide, n, V, padding)) : make_uint2(0xffffffffu, 0xffffffffu);
+    const int tid = threadIdx.x, lane = tid & 63, part = __builtin_amdgcn_readfirstlane(tid >> 6), first = (int)blockIdx.x * 64, mine = first + lane;
+    const int each = ((N + 15) / 16 + 15) & ~15, from = part * each, to = min(from + each, (N + 15) & ~15);
+    for (int n = tid; n < RANK_MOST && n < N + 16; n += 1024) all[n] = n < N ? key_of(ids, n, V, padding) : 0xffffffffu;
     if (tid < 64) rank[tid] = 0;
     __syncthreads();
-    const int mine = (int)blockIdx.x * 64 + lane;
-    if (mine < N) {
-        const uint2 me = all[mine];
-        const uint64_t key = (uint64_t)me.y << 32 | me.x;
-        int below = 0;
-        for (int i = part * 2; i < padded; i += 8) {                         // two entries a read
-            const uint4 v = *(const uint4 *)&all[i];
-            below += ((uint64_t)v.y << 32 | v.x) < key;
-            below += ((uint64_t)v.w << 32 | v.z) < key;
-        }
-        atomicAdd(&rank[lane], below);
-    }
+    const uint32_t me = all[min(mine, N - 1)];
+    int below = 0;
+    auto count = [&](int lo, int hi, uint32_t limit) {                       // keys below `limit` at places lo .. hi - 1, multiples of 16
+#pragma unroll 2
+        for (int i = lo; i < hi; i += 16)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const uint4 v = *(const uint4 *)&all[i + j];
+                below += (v.x < limit) + (v.y < limit) + (v.z < limit) + (v.w < limit);
+            }
+    };
+    // (first is a multiple of 64, and each part of 16: a part lies before the 64 tokens, behind them, or among them in groups of 16)
+    const int a = min(max(first, from), to), b = min(max(first + 64, from), to);
+    count(from, a, me + 1);
+    for (int i = a; i < b; ++i) below += all[i] < me || (all[i] == me && i < mine);
+    count(b, to, me);
+    atomicAdd(&rank[lane], below);
     __syncthreads();
-    if (tid < 64 && mine < N) {
-        const uint2 me = all[mine];
-        keys[rank[lane]] = me.y;
-        perm[rank[lane]] = me.x;
-    }
+    if (tid < 64 && mine < N) { keys[rank[lane]] = me; perm[rank[lane]] = (uint32_t)mine; }
 }
 
 // A radix pass: a workgroup takes `per_wg` consecutive keys (a multiple of 256: a quarter to each wave).  counts: [bins][workgroups]
-struct Radix { const void *ids; bool wide; int64_t N, V, padding; const uint32_t *keys_in, *perm_in; uint32_t *keys_out, *perm_out, *counts; int shift, bins, wgs, per_wg; };
+struct Radix { Ids ids; int64_t N, V, padding; const uint32_t *keys_in, *perm_in; uint32_t *keys_out, *perm_out, *counts; int shift, bins, wgs, per_wg; };
 __device__ __forceinline__ uint32_t radix_key(const Radix &r, int64_t n)
 {
-    return r.keys_in ? r.keys_in[n] : key_of(r.ids, r.wide, n, r.V, r.padding);
+    return r.keys_in ? r.keys_in[n] : key_of(r.ids, n, r.V, r.padding);
 }
 
-__global__ __launch_bounds__(256) void embed_count_kernel(Radix r, Fill f)
+__global__ __launch_bounds__(256) void embed_count_kernel(Radix r, uint32_t *heavy, Fill f)
 {
-    if ((int)blockIdx.x >= r.wgs) { fill_zeros(f, (int)blockIdx.x - r.wgs, (int)gridDim.x - r.wgs); return; }
+    if (heavy && blockIdx.x == 0 && threadIdx.x == 0) *heavy = 0;
+    if ((int)blockIdx.x >= r.wgs) { fill_zeros<256>(f, (int)blockIdx.x - r.wgs, (int)gridDim.x - r.wgs); return; }
     __shared__ uint32_t count[RADIX_BINS];
     for (int b = threadIdx.x; b < r.bins; b += 256) count[b] = 0;
     __syncthreads();
@@ -236,121 +264,252 @@ __global__ __launch_bounds__(256) void embed_move_kernel(Radix r)
     }
 }
 
+// Chunks of 256 tokens sorted each by a workgroup, a token's rank in its chunk by counting; then a token's place is its rank plus, from each other chunk, the
+// number of keys below its own, which a search in eight steps finds (of earlier chunks the equal ones count too).  The search runs in LDS, which holds all
+// keys: 64 tokens to a workgroup, each of its 16 waves searches every sixteenth chunk.
+constexpr int SORTED = 256;
+__global__ __launch_bounds__(SORTED) void embed_chunk_kernel(Ids ids, int N, int64_t V, int64_t padding, int sort_wgs, uint32_t *keys, uint32_t *perm, uint32_t *heavy, Fill f)
+{
+    if (heavy && blockIdx.x == 0 && threadIdx.x == 0) *heavy = 0;
+    if ((int)blockIdx.x >= sort_wgs) { fill_zeros<256>(f, (int)blockIdx.x - sort_wgs, (int)gridDim.x - sort_wgs); return; }
+    __shared__ __attribute__((aligned(16))) uint32_t all[SORTED];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = (int)blockIdx.x * SORTED + tid;
+    const uint32_t me = n < N ? key_of(ids, n, V, padding) : 0xffffffffu;
+    all[tid] = me;
+    __syncthreads();
+    int rank = 0;
+    auto count = [&](int lo, int hi, uint32_t limit) {
+#pragma unroll 4
+        for (int i = lo; i < hi; i += 4) {
+            const uint4 v = *(const uint4 *)&all[i];
+            rank += (v.x < limit) + (v.y < limit) + (v.z < limit) + (v.w < limit);
+        }
+    };
+    count(0, wave * 64, me + 1);                                             // (of what lies behind the list's end none is asked: 0xffffffff + 1 is 0)
+#pragma unroll 4
+    for (int i = 0; i < 64; ++i) {
+        const uint32_t other = all[wave * 64 + i];
+        rank += other < me || (other == me && wave * 64 + i < tid);
+    }
+    count(wave * 64 + 64, SORTED, me);
+    if (n < N) {
+        const int at = (int)blockIdx.x * SORTED + rank;
+        keys[at] = me;
+        perm[at] = (uint32_t)n;
+    }
+}
+__global__ __launch_bounds__(1024) void embed_merge_kernel(const uint32_t *keys_in, const uint32_t *perm_in, int N, int chunks, int rounds, uint32_t *keys, uint32_t *perm)
+{
+    extern __shared__ __attribute__((aligned(16))) uint32_t sorted[];       // [chunk][SORTED]
+    __shared__ int place[64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int i = 4 * tid; i < chunks * SORTED; i += 4096) {
+        uint4 v = make_uint4(0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu);
+        if (i + 4 <= N) v = *(const uint4 *)(keys_in + i);
+        else {
+            if (i < N) v.x = keys_in[i];
+            if (i + 1 < N) v.y = keys_in[i + 1];
+            if (i + 2 < N) v.z = keys_in[i + 2];
+        }
+        *(uint4 *)&sorted[i] = v;
+    }
+    for (int first = (int)blockIdx.x * 64 * rounds, end = min(first + 64 * rounds, N); first < end; first += 64) {
+        const int mine = min(first + lane, N - 1), own = first / SORTED;
+        __syncthreads();                                                     // (the round before is done with place)
+        if (tid < 64) place[tid] = first + tid - own * SORTED;
+        __syncthreads();
+        const uint32_t me = sorted[mine];
+        int below = 0;
+#pragma unroll 4
+        for (int c = wave; c < chunks; c += 16) {
+            const uint32_t *list = sorted + c * SORTED, limit = me + (c < own ? 1 : 0);
+            int at = 0;
+#pragma unroll
+            for (int step = SORTED / 2; step; step >>= 1) at += list[at + step - 1] < limit ? step : 0;
+            at += list[at] < limit;                                          // (at is SORTED - 1 at most)
+            below += c == own ? 0 : at;
+        }
+        atomicAdd(&place[lane], below);
+        __syncthreads();
+        if (tid < 64 && first + tid < N) { keys[place[tid]] = me; perm[place[tid]] = perm_in[mine]; }
+    }
+}
+
 // ---- sums
+constexpr int CHUNK = 16;        // tokens of a workgroup
+constexpr int LIGHT = 48;        // tokens of a row that one workgroup sums, wherever they lie: it sees 64 places from its chunk on
 struct Sums {
     const void *g;
     int64_t ldg, D, ldo;
-    int N, chunk, chunks;
+    int N, chunks;
     uint32_t V;
     const uint32_t *keys, *perm;
     void *out;
     float *part;                 // [chunks][2][part_ld]: the sums of the row that began before the chunk, and of the one that runs on behind it
     int64_t part_ld;
+    uint32_t *heavy;             // how many rows have more than LIGHT tokens, and the chunks where they begin
     float scale;
     int accumulate;
 };
 
-template <int OT, bool VEC> __device__ __forceinline__ void write_sum(const Sums &s, uint32_t row, int64_t c, int left, float (&v)[EW])
+template <int OT, bool NARROW> __device__ __forceinline__ void write_sum(const Sums &s, uint32_t row, int64_t c, int skip, float (&v)[EW])
 {
     const int64_t at = (int64_t)row * s.ldo + c;
+    const int left = NARROW ? (int)s.D : EW;
 #pragma unroll
     for (int i = 0; i < EW; ++i) v[i] *= s.scale;
-    const bool vec = VEC && left == EW;
     if (s.accumulate) {
-        float old[EW];
-        if (vec) load_row<OT, EW, true>(s.out, at, left, old); else load_row<OT, EW, false>(s.out, at, left, old);
+        const Raw<OT> old = load_raw<OT, NARROW>(s.out, at, left);
 #pragma unroll
-        for (int i = 0; i < EW; ++i) v[i] += old[i];
+        for (int i = 0; i < EW; ++i) v[i] += element(old, i);
     }
-    if (vec) store_row<OT, EW, true>(s.out, at, left, v); else store_row<OT, EW, false>(s.out, at, left, v);
+    store_row<OT>(s.out, at, skip, left, v);
 }
 
-template <int GT, int OT, bool VEC>
+// What a chunk has to do, from the 64 keys before it (lane i: place from - 64 + i) and the 64 from its first on.  A row with at most LIGHT tokens belongs to the
+// chunk where it begins; a longer one leaves the sum of its tokens in each chunk in the workspace.
+struct Share {
+    int begin, end;              // places to sum, from the chunk's first on
+    bool head, tail;             // the first of their rows began earlier, the last one runs on behind the chunk: both longer than LIGHT
+};
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int k) { return (uint32_t)__builtin_amdgcn_readlane((int)v, k); }
+__device__ __forceinline__ Share share_of(uint32_t before, uint32_t here, int n)
+{
+    Share s{0, n, false, false};
+    const uint32_t first = lane_of(here, 0);
+    const uint64_t differ = ~__ballot(here == first), differ_before = ~__ballot(before == first);
+    const int after = differ ? __builtin_ctzll(differ) : 64, earlier = differ_before ? __builtin_clzll(differ_before) : 64;
+    if (earlier > 0) {
+        if (earlier + after <= LIGHT) s.begin = min(after, n);
+        else s.head = true;
+    }
+    const uint32_t last = lane_of(here, n - 1);
+    const uint64_t runs = __ballot(here == last) >> (n - 1);                 // from the chunk's last place on
+    const int behind = (~runs ? __builtin_ctzll(~runs) : 64) - 1;            // places of the last row behind the chunk
+    if (n == CHUNK && behind > 0 && !(last == first && after > n - 1 && earlier > 0)) {      // (a row that began earlier is not this chunk's)
+        const uint64_t back = ~(__ballot(here == last) << (63 - (n - 1)));   // from the chunk's last place backwards
+        const int begun = n - min(n, back ? __builtin_clzll(back) : 64);     // where the last row begins
+        const int length = n - begun + behind;
+        if (length <= LIGHT) s.end = n + behind;
+        else s.tail = true;
+    }
+    return s;
+}
+
+template <int GT, int OT, bool NARROW>
 __global__ __launch_bounds__(256) void embed_sum_kernel(Sums s)
 {
-    const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * EW;
-    if (c >= s.D) return;
-    const int left = (int)min(s.D - c, (int64_t)EW);
-    const int from = (int)blockIdx.x * s.chunk, to = min(from + s.chunk, s.N);
-    const uint32_t before = from > 0 ? s.keys[from - 1] : 0xffffffffu, behind = to < s.N ? s.keys[to] : 0xffffffffu;
+    const int64_t c0 = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * EW, c = NARROW ? c0 : min(c0, s.D - EW);
+    const int skip = (int)(c0 - c);
+    const int from = (int)blockIdx.x * CHUNK, n = min(CHUNK, s.N - from), lane = threadIdx.x & 63;
+    uint32_t before = 0xffffffffu, here = 0xfffffffeu, place = 0;
+    if (from - 64 + lane >= 0) before = s.keys[from - 64 + lane];
+    if (from + lane < s.N) { here = s.keys[from + lane]; place = s.perm[from + lane]; }
+    if (lane_of(here, 0) >= s.V) return;                                     // (tokens that count for nothing, the last of the list)
+    const Share share = share_of(before, here, n);
+    if (share.tail && blockIdx.y == 0 && threadIdx.x == 0) s.heavy[1 + atomicAdd(s.heavy, 1u)] = blockIdx.x;       // (in any order: each row is joined by itself)
+    if (c0 >= s.D || share.begin >= share.end) return;
     float acc[EW];
 #pragma unroll
-    for (int j = 0; j < EW; ++j) acc[j] = 0.f;
-    uint32_t row = s.keys[from];
-    bool began = row != before;                                              // whether this row's tokens begin in this chunk
-    auto leave = [&](bool runs_on) {
-        if (row >= s.V) return;                                              // (tokens that count for nothing)
-        if (began && !runs_on) write_sum<OT, VEC>(s, row, c, left, acc);
-        else {
-            float *to_part = s.part + ((int64_t)blockIdx.x * 2 + (began ? 1 : 0)) * s.part_ld + c;
-            *(float4 *)to_part = make_float4(acc[0], acc[1], acc[2], acc[3]);
-            *(float4 *)(to_part + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    for (int e = 0; e < EW; ++e) acc[e] = 0.f;
+    uint32_t row = lane_of(here, share.begin);
+    bool head = share.head;
+    auto leave = [&](bool tail) {
+        if (row < s.V) {
+            if (!head && !tail) write_sum<OT, NARROW>(s, row, c, skip, acc);
+            else {
+                float *to_part = s.part + ((int64_t)blockIdx.x * 2 + (head ? 0 : 1)) * s.part_ld + c0;
+                *(float4 *)to_part = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                *(float4 *)(to_part + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+            }
         }
-    };
-    constexpr int AHEAD = GT == NM_DT_F32 ? 4 : 8;
-    for (int i = from; i < to; i += AHEAD) {
-        float v[AHEAD][EW];
+        head = false;
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int k = min(i + j, to - 1);
-            const int64_t at = (int64_t)s.perm[k] * s.ldg + c;
-            if (VEC && left == EW) load_row<GT, EW, true>(s.g, at, left, v[j]); else load_row<GT, EW, false>(s.g, at, left, v[j]);
-        }
+        for (int e = 0; e < EW; ++e) acc[e] = 0.f;
+    };
+    constexpr int AHEAD = GT == NM_DT_F32 ? 4 : 8;                           // rows on their way
+    for (int k = share.begin; k < share.end; k += AHEAD) {
+        Raw<GT> v[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)                                      // (past the end the last token's again)
+            v[j] = load_raw<GT, NARROW>(s.g, (int64_t)lane_of(place, min(k + j, share.end - 1)) * s.ldg + c, NARROW ? (int)s.D : EW);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j)
-            if (i + j < to) {
-                const uint32_t key = s.keys[i + j];
-                if (key != row) {
-                    leave(false);
-                    row = key;
-                    began = true;
+            if (k + j < share.end) {
+                const uint32_t key = lane_of(here, k + j);
+                if (key != row) { leave(false); row = key; }
 #pragma unroll
-                    for (int e = 0; e < EW; ++e) acc[e] = 0.f;
-                }
-#pragma unroll
-                for (int e = 0; e < EW; ++e) acc[e] += v[j][e];
+                for (int e = 0; e < EW; ++e) acc[e] += element(v[j], e);
             }
     }
-    leave(row == behind);
+    leave(share.tail);
 }
 
-// a row that runs over several chunks, where it begins: its parts, chunk after chunk
-template <int OT, bool VEC>
-__global__ __launch_bounds__(256) void embed_join_kernel(Sums s)
+// The rows with more than LIGHT tokens: their parts in 16 groups, each chunk after chunk, and the groups in order
+constexpr int GROUPS = 16;
+template <int OT, bool NARROW>
+__global__ __launch_bounds__(64 * GROUPS) void embed_join_kernel(Sums s)
 {
-    const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * EW;
-    const int chunk = (int)blockIdx.x, from = chunk * s.chunk, to = from + s.chunk;
-    if (to >= s.N) return;                                                   // the last chunk: nothing runs on
-    const uint32_t row = s.keys[to];
-    if (row >= s.V || s.keys[to - 1] != row || (from > 0 && s.keys[from] == row && s.keys[from - 1] == row)) return;
-    if (c >= s.D) return;
-    const int left = (int)min(s.D - c, (int64_t)EW);
-    // the last chunk that has some of the row
-    int lo = chunk + 1, hi = s.chunks - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (s.keys[mid * s.chunk] == row) lo = mid; else hi = mid - 1;
-    }
-    float acc[EW];
-    load_row<NM_DT_F32, EW, true>(s.part, ((int64_t)chunk * 2 + 1) * s.part_ld + c, EW, acc);
-    for (int k = chunk + 1; k <= lo; ++k) {
-        float v[EW];
-        load_row<NM_DT_F32, EW, true>(s.part, (int64_t)k * 2 * s.part_ld + c, EW, v);
+    __shared__ float sums[GROUPS - 1][EW][64];
+    const int lane = threadIdx.x & 63, group = threadIdx.x >> 6, count = (int)s.heavy[0];
+    const int64_t c0 = ((int64_t)blockIdx.y * 64 + lane) * EW, c = NARROW ? c0 : min(c0, s.D - EW);
+    const bool there = c0 < s.D;
+    for (int k = (int)blockIdx.x; k < count; k += (int)gridDim.x) {
+        const int chunk = (int)s.heavy[1 + k];
+        const uint32_t row = s.keys[(chunk + 1) * CHUNK];
+        // the last chunk that has some of the row, by 64 probes at a time
+        int lo = chunk + 1, hi = s.chunks - 1;
+        while (lo < hi) {
+            const int step = (hi - lo + 63) / 64;
+            const uint64_t others = ~__ballot(s.keys[min(lo + step * (lane + 1), hi) * CHUNK] == row);
+            const int same = others ? __builtin_ctzll(others) : 64;
+            const int to = min(lo + step * same, hi);
+            hi = same < 64 ? min(lo + step * (same + 1), hi) - 1 : hi;
+            lo = to;
+            if (same == 64) break;
+            hi = max(hi, lo);
+        }
+        const int parts = lo - chunk + 1, each = (parts + GROUPS - 1) / GROUPS, first = min(group * each, parts), last = min(first + each, parts);
+        float acc[EW];
 #pragma unroll
-        for (int e = 0; e < EW; ++e) acc[e] += v[e];
+        for (int e = 0; e < EW; ++e) acc[e] = 0.f;
+        if (there)
+            for (int i = first; i < last; i += 4) {
+                Raw<NM_DT_F32> v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int p = min(i + j, last - 1);                      // part 0: what the row has in the chunk where it begins
+                    v[j] = load_raw<NM_DT_F32>(s.part, ((int64_t)(chunk + p) * 2 + (p == 0 ? 1 : 0)) * s.part_ld + c0);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (i + j < last)
+#pragma unroll
+                        for (int e = 0; e < EW; ++e) acc[e] += element(v[j], e);
+            }
+        if (group > 0)
+#pragma unroll
+            for (int e = 0; e < EW; ++e) sums[group - 1][e][lane] = acc[e];
+        __syncthreads();
+        if (group == 0 && there) {
+#pragma unroll
+            for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+                for (int e = 0; e < EW; ++e) acc[e] += sums[g][e][lane];
+            write_sum<OT, NARROW>(s, row, c, (int)(c0 - c), acc);
+        }
+        __syncthreads();
     }
-    write_sum<OT, VEC>(s, row, c, left, acc);
 }
 
 int bits_of(int64_t v) { int b = 0; while (v >> b) ++b; return b; }
 
-struct GradPlan { int64_t keys, perm, counts, part, part_ld, bytes; int chunk, chunks, per_wg, wgs, passes, digit; };
+struct GradPlan { int64_t keys, perm, counts, heavy, part, part_ld, bytes; int chunks, per_wg, wgs, passes, digit; };
 GradPlan plan_grad(int64_t N, int64_t V, int64_t D)
 {
     GradPlan p{};
     auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
-    p.chunk = 16;
-    p.chunks = (int)((N + p.chunk - 1) / p.chunk);
+    p.chunks = (int)((N + CHUNK - 1) / CHUNK);
     p.part_ld = (D + EW - 1) / EW * EW;
     const int bits = bits_of(V);                                             // keys are 0 .. V
     p.passes = N <= RANK_MOST ? 0 : (bits + RADIX_BITS - 1) / RADIX_BITS;
@@ -360,7 +519,8 @@ GradPlan plan_grad(int64_t N, int64_t V, int64_t D)
     p.keys = 0;
     p.perm = p.keys + 2 * up(N * 4);
     p.counts = p.perm + 2 * up(N * 4);
-    p.part = p.counts + up((int64_t)RADIX_BINS * p.wgs * 4);
+    p.heavy = p.counts + up((int64_t)RADIX_BINS * p.wgs * 4);
+    p.part = p.heavy + up((N / LIGHT + 2) * 4);
     p.bytes = p.part + up((int64_t)p.chunks * 2 * p.part_ld * 4);
     return p;
 }
@@ -371,16 +531,15 @@ hipError_t launch_embed(int table_dt, int out_dt, const void *table, int64_t V, 
                         int64_t ldo, hipStream_t st)
 {
     if (N == 0 || D == 0) return hipSuccess;
+    const Ids tokens{(const uint32_t *)ids, wide ? 2 : 1};
     int shift = 0;
     while (shift < 8 && ((int64_t)EW << shift) < D) ++shift;
-    const int64_t te = table_dt == NM_DT_F32 ? 4 : 2, oe = out_dt == NM_DT_F32 ? 4 : 2;
-    const bool vec = (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0 && ldt * te % 16 == 0 && ldo * oe % 16 == 0;
     const int64_t wgs = (N + (256 >> shift) - 1) / (256 >> shift);
     if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
-#define NM_EMBED(TT, OT)                                                                                                                                   \
-    do {                                                                                                                                                   \
-        if (vec) hipLaunchKernelGGL((embed_kernel<TT, OT, true>), dim3((unsigned)wgs), dim3(256), 0, st, table, V, D, ldt, ids, wide, N, scale, out, ldo, shift); \
-        else hipLaunchKernelGGL((embed_kernel<TT, OT, false>), dim3((unsigned)wgs), dim3(256), 0, st, table, V, D, ldt, ids, wide, N, scale, out, ldo, shift);    \
+#define NM_EMBED(TT, OT)                                                                                                                                          \
+    do {                                                                                                                                                          \
+        if (D < EW) hipLaunchKernelGGL((embed_kernel<TT, OT, true>), dim3((unsigned)wgs), dim3(256), 0, st, table, V, D, ldt, tokens, N, scale, out, ldo, shift);  \
+        else hipLaunchKernelGGL((embed_kernel<TT, OT, false>), dim3((unsigned)wgs), dim3(256), 0, st, table, V, D, ldt, tokens, N, scale, out, ldo, shift);        \
     } while (0)
     if (table_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_EMBED(NM_DT_F32, NM_DT_F32); else NM_EMBED(NM_DT_F32, NM_DT_BF16); }
     else                       { if (out_dt == NM_DT_F32) NM_EMBED(NM_DT_BF16, NM_DT_F32); else NM_EMBED(NM_DT_BF16, NM_DT_BF16); }
@@ -393,45 +552,53 @@ size_t embed_grad_workspace(int64_t N, int64_t V, int64_t D) { return N > 0 ? (s
 hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, const void *ids, bool wide, int64_t N, int64_t V, int64_t D, float scale,
                              int64_t padding, bool accumulate, void *out, int64_t ldo, void *workspace, hipStream_t st)
 {
-    const int64_t oe = out_dt == NM_DT_F32 ? 4 : 2, ge = g_dt == NM_DT_F32 ? 4 : 2;
+    const int64_t oe = out_dt == NM_DT_F32 ? 4 : 2;
     const Fill fill{(char *)out, accumulate ? 0 : V, D * oe, ldo * oe};
-    const int fill_wgs = accumulate ? 0 : (int)std::min<int64_t>((V * D * oe + 16383) / 16384, 2048);
+    const int fill_wgs = accumulate ? 0 : (int)std::min<int64_t>((V * D * oe + FILL - 1) / FILL, 1 << 24);
     const GradPlan p = plan_grad(std::max<int64_t>(N, 1), V, D);
+    const Ids tokens{(const uint32_t *)ids, wide ? 2 : 1};
     char *w = (char *)workspace;
     uint32_t *keys[2], *perm[2];
     const int64_t half = (N * 4 + 255) / 256 * 256;
     for (int i = 0; i < 2; ++i) { keys[i] = (uint32_t *)(w + p.keys + i * half); perm[i] = (uint32_t *)(w + p.perm + i * half); }
+    uint32_t *heavy = N ? (uint32_t *)(w + p.heavy) : nullptr;               // (without tokens there is no workspace)
     int now = 0;
     if (p.passes == 0) {
         const int sort_wgs = (int)((N + 63) / 64);
         if (sort_wgs + fill_wgs == 0) return hipSuccess;
-        hipLaunchKernelGGL(embed_rank_kernel, dim3((unsigned)(sort_wgs + fill_wgs)), dim3(256), (size_t)(N + 7) / 8 * 64, st, ids, wide, (int)N, V, padding, sort_wgs, keys[0], perm[0], fill);
+        hipLaunchKernelGGL(embed_rank_kernel, dim3((unsigned)(sort_wgs + fill_wgs)), dim3(1024), 0, st, tokens, (int)N, V, padding, sort_wgs, keys[0], perm[0], heavy, fill);
+    } else if (N <= MERGE_MOST) {
+        const int chunks = (int)((N + SORTED - 1) / SORTED);
+        now = 1;
+        hipLaunchKernelGGL(embed_chunk_kernel, dim3((unsigned)(chunks + fill_wgs)), dim3(SORTED), 0, st, tokens, (int)N, V, padding, chunks, keys[0], perm[0], heavy, fill);
+        const int groups = (int)((N + 63) / 64), rounds = (groups + NM_CUS - 1) / NM_CUS;       // (a CU holds one workgroup's keys)
+        hipLaunchKernelGGL(embed_merge_kernel, dim3((unsigned)((groups + rounds - 1) / rounds)), dim3(1024), (size_t)chunks * SORTED * 4, st, keys[0], perm[0], (int)N, chunks, rounds, keys[1],
+                           perm[1]);
     } else {
         for (int k = 0; k < p.passes; ++k) {
-            const Radix r{ids, wide, N, V, padding, k ? keys[now] : nullptr, k ? perm[now] : nullptr, keys[k ? 1 - now : 0], perm[k ? 1 - now : 0], (uint32_t *)(w + p.counts),
+            const Radix r{tokens, N, V, padding, k ? keys[now] : nullptr, k ? perm[now] : nullptr, keys[k ? 1 - now : 0], perm[k ? 1 - now : 0], (uint32_t *)(w + p.counts),
                           k * p.digit, 1 << p.digit, p.wgs, p.per_wg};
             if (k) now = 1 - now;
-            hipLaunchKernelGGL(embed_count_kernel, dim3((unsigned)(p.wgs + (k ? 0 : fill_wgs))), dim3(256), 0, st, r, fill);
+            hipLaunchKernelGGL(embed_count_kernel, dim3((unsigned)(p.wgs + (k ? 0 : fill_wgs))), dim3(256), 0, st, r, heavy, fill);
             hipLaunchKernelGGL(embed_move_kernel, dim3((unsigned)p.wgs), dim3(256), 0, st, r);
         }
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (N == 0) return hipSuccess;
-    const Sums s{g, ldg, D, ldo, (int)N, p.chunk, p.chunks, (uint32_t)V, keys[now], perm[now], out, (float *)(w + p.part), p.part_ld, scale, accumulate};
-    const bool vec = (uintptr_t)g % 16 == 0 && (uintptr_t)out % 16 == 0 && ldg * ge % 16 == 0 && ldo * oe % 16 == 0;
+    const Sums s{g, ldg, D, ldo, (int)N, p.chunks, (uint32_t)V, keys[now], perm[now], out, (float *)(w + p.part), p.part_ld, heavy, scale, accumulate};
     const int64_t columns = (D + EW - 1) / EW;
     const int threads = (int)std::min<int64_t>((columns + 63) / 64 * 64, 256);
-    const dim3 grid((unsigned)p.chunks, (unsigned)((columns + threads - 1) / threads));
-#define NM_SUM(GT, OT, VEC)                                                                                  \
-    do {                                                                                                     \
-        hipLaunchKernelGGL((embed_sum_kernel<GT, OT, VEC>), grid, dim3(threads), 0, st, s);                   \
-        hipLaunchKernelGGL((embed_join_kernel<OT, VEC>), grid, dim3(threads), 0, st, s);                      \
+    const dim3 grid((unsigned)p.chunks, (unsigned)((columns + threads - 1) / threads)), join((unsigned)std::min<int64_t>(N / LIGHT + 1, 64), (unsigned)((columns + 63) / 64));
+#define NM_SUM_N(GT, OT, NARROW)                                                                 \
+    do {                                                                                         \
+        hipLaunchKernelGGL((embed_sum_kernel<GT, OT, NARROW>), grid, dim3(threads), 0, st, s);   \
+        hipLaunchKernelGGL((embed_join_kernel<OT, NARROW>), join, dim3(64 * GROUPS), 0, st, s);  \
     } while (0)
-#define NM_SUM_V(GT, OT) do { if (vec) NM_SUM(GT, OT, true); else NM_SUM(GT, OT, false); } while (0)
-    if (g_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_SUM_V(NM_DT_F32, NM_DT_F32); else NM_SUM_V(NM_DT_F32, NM_DT_BF16); }
-    else                   { if (out_dt == NM_DT_F32) NM_SUM_V(NM_DT_BF16, NM_DT_F32); else NM_SUM_V(NM_DT_BF16, NM_DT_BF16); }
-#undef NM_SUM_V
+#define NM_SUM(GT, OT) do { if (D < EW) NM_SUM_N(GT, OT, true); else NM_SUM_N(GT, OT, false); } while (0)
+    if (g_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_SUM(NM_DT_F32, NM_DT_F32); else NM_SUM(NM_DT_F32, NM_DT_BF16); }
+    else                   { if (out_dt == NM_DT_F32) NM_SUM(NM_DT_BF16, NM_DT_F32); else NM_SUM(NM_DT_BF16, NM_DT_BF16); }
 #undef NM_SUM
+#undef NM_SUM_N
     return hipGetLastError();
 }
 

@@ -21,6 +21,9 @@ def _ids(kind, N, V, gen):
         return torch.arange(N).flip(0) % V
     if kind == "two":                                                    # runs that end on, before and behind the borders of a chunk
         return (torch.arange(N) // 31) % min(V, 2)
+    if kind == "runs":                                                   # rows of 1 to 70 tokens in turn: either side of what one workgroup sums
+        length = torch.arange(N) % 70 + 1
+        return torch.repeat_interleave(torch.arange(N), length)[:N].remainder(V)[torch.randperm(N, generator=gen)]
     raise ValueError(kind)
 
 
@@ -66,11 +69,11 @@ def test_lookup_of_tokens_outside_and_other_layouts():
     assert bool(torch.isnan(nm.nm_embed(t[:0], ids)).all())
 
 
-GRADS = [(1, 1, 1), (2, 7, 5), (15, 3, 8), (16, 40, 33), (17, 1000, 64), (64, 2, 1024), (65, 300, 100), (1000, 50, 520), (4095, 30011, 72), (8192, 500, 136)]
-LARGE = [(8193, 500, 72), (8200, 3, 64), (20000, 70000, 40), (33000, 511, 24), (33000, 512, 33), (65536, 300000, 16)]
+GRADS = [(1, 1, 1), (2, 7, 5), (15, 3, 8), (16, 40, 33), (17, 1000, 64), (64, 2, 1024), (65, 300, 100), (1000, 50, 520), (4095, 30011, 72), (4096, 77, 40), (4097, 30011, 72), (8192, 500, 136)]
+LARGE = [(8193, 500, 72), (8200, 3, 64), (16384, 40000, 40), (16385, 200, 24), (20000, 70000, 40), (32768, 511, 16), (32769, 511, 16), (33000, 511, 24), (33000, 512, 33), (65536, 300000, 16), (65537, 513, 8), (70001, 300000, 16)]
 
 
-@pytest.mark.parametrize("kind", ["uniform", "frequent", "one", "falling", "two"])
+@pytest.mark.parametrize("kind", ["uniform", "frequent", "one", "falling", "two", "runs"])
 @pytest.mark.parametrize("N,V,D", GRADS + LARGE)
 def test_gradient(kind, N, V, D):
     import paper_2203_10991_amd as nm
@@ -85,7 +88,7 @@ def test_gradient(kind, N, V, D):
     _check(got, want, size, most)
     assert torch.equal(got, nm.nm_embed_grad(gd, idd.long(), V, 0.5))
     names = kernels_of(lambda: nm.nm_embed_grad(gd, idd, V, 0.5))
-    assert any("embed_move_kernel" in k for k in names) == (N > 8192) and any("embed_rank_kernel" in k for k in names) == (N <= 8192)
+    assert any(("embed_rank_kernel" if N <= 4096 else "embed_merge_kernel" if N <= 32768 else "embed_move_kernel") in k for k in names), names
 
 
 @pytest.mark.parametrize("gt", [F32, BF16])
