@@ -3,8 +3,8 @@
 // 32-bit integer sums (K at most 131072: 127^2 K stays below 2^31), then one conversion, the product with xs ws, bias and ReLU in binary32, one rounding.
 //
 // Instruction: v_mfma_i32_32x32x32_i8, both operands with 32 rows (lane % 32) and 16 consecutive bytes of the reduction axis to a lane.  Which of the 32 steps
-// of the axis those are does not matter, since both operands hold the same ones.  The weights are the first operand, so a lane holds four consecutive
-// features of a token and stores them together.
+// of the axis those are does not matter, since both operands hold the same ones.  bf16 results: the weights are the first operand, so a lane holds four
+// consecutive features of a token and stores them together.  binary32 results: x is the first one, and the lanes of half a wave store 32 features of a token.
 //
 // Workgroup = WM x WN waves, each AM x AN blocks of 32 tokens x 32 features.  The reduction axis advances in stages of 128 bytes, NS of which rotate through
 // LDS, filled by direct loads.  A row of a stage is eight chunks of 16 bytes, chunk c at position c ^ (row / 2 % 8), which makes the 16-byte reads
@@ -40,6 +40,14 @@ __device__ __forceinline__ void acc_clear(f32x16 &acc)
     asm volatile("s_nop 4\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %1, 0" : "+a"(acc) : "v"(z));
 }
 
+// one sum of a block.  (Read by itself: left to the compiler whole blocks are copied first, to registers that it has not got.)
+__device__ __forceinline__ float sum_of(float acc)
+{
+    int sum;
+    asm("v_accvgpr_read_b32 %0, %1" : "=v"(sum) : "a"(acc));
+    return (float)sum;
+}
+
 struct I8Tiles { I8Arg a; int tiles_m, tiles_n; };
 
 // eight bf16 features of a token, of which `left` are there (WHOLE: all or none).  Rows start anywhere: the stores of whole groups need
@@ -57,26 +65,23 @@ template <bool WHOLE> __device__ __forceinline__ void store_features(char *at, i
         if (left & 1) *(uint16_t *)at = (uint16_t)w0;
     }
 }
-__device__ __forceinline__ float bias_at(const I8Arg &p, int64_t f)
-{
-    return p.bias_dt == NM_DT_F32 ? ((const float *)p.bias)[f] : __uint_as_float((uint32_t)((const uint16_t *)p.bias)[f] << 16);
-}
-
+// WHOLE: N is a multiple of 8 (bf16 results only)
 template <int WM, int WN, int AM, int AN, int NS, int OT, bool WHOLE>
 __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
 {
     constexpr int NW = WM * WN, TM = WM * AM * 32, TN = WN * AN * 32;
     constexpr int X_BYTES = TM * I8_K, STAGE = X_BYTES + TN * I8_K;
-    constexpr int XL = TM / 8 / NW, WL = TN / 8 / NW, LPS = XL + WL;             // direct loads of a wave and stage
+    constexpr int RPL = 8;                                                       // rows of a direct load
+    constexpr int XL = TM / RPL / NW, WL = TN / RPL / NW, LPS = XL + WL;         // direct loads of a wave and stage
     constexpr int LDS = NS * STAGE;
     using OutT = std::conditional_t<OT == NM_DT_F32, float, uint16_t>;
-    static_assert(XL >= 1 && WL >= 1 && TM % (8 * NW) == 0 && TN % (8 * NW) == 0 && TM <= NW * 64 && TN <= NW * 64 && LDS + 3 * NW * 256 <= 160 * 1024, "tile");
+    static_assert(XL >= 1 && WL >= 1 && TM % (RPL * NW) == 0 && TN % (RPL * NW) == 0 && TM <= NW * 64 && TN <= NW * 64 && LDS + 3 * NW * 256 <= 160 * 1024, "tile");
     __shared__ __attribute__((aligned(1024))) char S[LDS];
     __shared__ __attribute__((aligned(16))) float tile_xs[NW * 64], tile_ws[NW * 64], tile_add[NW * 64];       // scales and bias of the tile that leaves
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN, hi = lane >> 5, l32 = lane & 31;
-    const int n = (int)((p.a.K + I8_K - 1) / I8_K);                              // stages of a tile
+    const int n = (int)((p.a.K + I8_K - 1) / I8_K);                               // stages of a tile
     const int tiles = p.tiles_m * p.tiles_n;
     auto place = [&](int tile, int64_t &m0, int64_t &n0) {
         int tm, tn;
@@ -93,9 +98,10 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
 
     // ---- direct loads: load d of a wave covers 1 KB of the stage's image at (wave * XL + d) KB, resp. (wave * WL + d) KB behind the x tile.  Rows past
     // the end are clamped to the last one, their results are not stored; the buffer of w ends with the last row's last chunk of 16 bytes.
-    const int r8 = lane >> 3, pos = lane & 7;
+    const int r_load = lane >> 3, pos = lane & 7;
     uint32_t x_src[XL], w_src[WL];
-    auto chunk_of = [&](int row) { return pos ^ ((row >> 1) & 7); };
+    auto key_of = [](int row) { return (row >> 1) & 7; };
+    auto chunk_of = [&](int row) { return pos ^ key_of(row); };
     // the tile and stage whose loads are being issued
     int f_tile = blockIdx.x, f_stage = 0;
     const char *xp, *wp;
@@ -106,12 +112,12 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
         const int rows_x = (int)min(p.a.M - 1 - m0, (int64_t)TM), rows_w = (int)min(p.a.N - 1 - n0, (int64_t)TN);
 #pragma unroll
         for (int d = 0; d < XL; ++d) {
-            const int row = (wave * XL + d) * 8 + r8;
+            const int row = (wave * XL + d) * RPL + r_load;
             x_src[d] = (uint32_t)min(row, rows_x) * (uint32_t)p.a.ldx + (uint32_t)chunk_of(row) * 16u;
         }
 #pragma unroll
         for (int d = 0; d < WL; ++d) {
-            const int row = (wave * WL + d) * 8 + r8;
+            const int row = (wave * WL + d) * RPL + r_load;
             w_src[d] = (uint32_t)min(row, rows_w) * (uint32_t)p.a.ldw + (uint32_t)chunk_of(row) * 16u;
         }
         xp = (const char *)(p.a.x + m0 * p.a.ldx);
@@ -142,7 +148,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
     const int k_last = p.a.x_zeros ? I8_K : (int)(p.a.K - (int64_t)(n - 1) * I8_K);
     auto clear_tail = [&](int buf) {
         for (int d = 0; d < XL; ++d) {
-            const int left = k_last - chunk_of((wave * XL + d) * 8 + r8) * 16;       // bytes of the lane's chunk that count
+            const int left = k_last - chunk_of((wave * XL + d) * RPL + r_load) * 16;       // bytes of the lane's chunk that count
             if (left < 16) {
                 u32x4 *at = (u32x4 *)(S + buf * STAGE + (wave * XL + d) * 1024 + lane * 16), v = *at;
 #pragma unroll
@@ -155,8 +161,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
 
     // ---- LDS reads
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)S;
-    const int key = (l32 >> 1) & 7;
-    const uint32_t rd = lds0 + (uint32_t)(l32 * I8_K + (hi ^ key) * 16);         // a row's chunk of MFMA step 0; that of step kk is chunk 2 kk + hi: bits 5 and 6 turned
+    const uint32_t rd = lds0 + (uint32_t)(l32 * I8_K + (hi ^ key_of(l32)) * 16);   // a row's chunk of MFMA step 0; that of step kk is chunk 2 kk + hi: bits 5 and 6 turned
     const uint32_t x_base = (uint32_t)(wm * AM * 32 * I8_K), w_base = (uint32_t)(X_BYTES + wn * AN * 32 * I8_K);
     u32x4 xf[2][AM], wf[2][AN];
 #pragma unroll
@@ -202,7 +207,8 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
         constexpr int set = decltype(kk_c)::value % 2, lo = decltype(lo_c)::value, n_l = decltype(hi_c)::value - lo, NM = AM * AN;
         static_for<NM>([&](auto i_c) {
             constexpr int i = decltype(i_c)::value, a = i / AN, b = i % AN;
-            mfma_i8_32x32x32(acc[a][b], wf[set][b], xf[set][a]);
+            if constexpr (OT == NM_DT_F32) mfma_i8_32x32x32(acc[a][b], xf[set][a], wf[set][b]);
+            else                           mfma_i8_32x32x32(acc[a][b], wf[set][b], xf[set][a]);
             static_for<LPS>([&](auto k_c) {
                 constexpr int k = decltype(k_c)::value;
                 if constexpr (k >= lo && k < lo + n_l && (k - lo) * NM / n_l == i) fetch_one(k_c, buf);
@@ -223,9 +229,23 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
     read(I0{}, 0);
     read(I1{}, 0);
     int buf = 0, s = 0, tile = blockIdx.x;                                       // the stage that is multiplied: its buffer, its number in its tile
+    // Scales and bias of the tile: every thread takes one of each, wanted or not, in the tile's last stage, ahead of the wait for the loads there
+    float my_xs = 0.f, my_ws = 0.f;
+    uint32_t my_add = 0;                                                         // as it is stored: what is made of a load waits for it
+    auto take_scales = [&]() {
+        int64_t m0, n0;
+        place(tile, m0, n0);
+        int t = tid;
+        asm volatile("" : "+v"(t));                                              // (computed here, tile by tile)
+        const int64_t f = min(n0 + min(t, TN - 1), p.a.N - 1);
+        my_xs = p.a.xs[min(m0 + min(t, TM - 1), p.a.M - 1)];
+        my_ws = p.a.ws[f];
+        if (p.a.bias) my_add = p.a.bias_dt == NM_DT_F32 ? ((const uint32_t *)p.a.bias)[f] : ((const uint16_t *)p.a.bias)[f];
+    };
     // a stage's first half; behind it every read has landed, so that the loop below closes with none on its way
     auto open = [&]() {
         const int next = buf == NS - 1 ? 0 : buf + 1;
+        if (s == n - 1) take_scales();
         asm volatile("s_waitcnt lgkmcnt(%0)" : : "n"(READS) : "memory");
         step(I0{}, I0{}, I0{}, 0);
         read(I2{}, buf);
@@ -261,67 +281,86 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
             // (what follows from these is computed here, tile by tile: left to itself the compiler keeps it in registers through the stages, which have none left)
             int l32 = lane & 31, hi = lane >> 5, tid = wave * 64 + lane;
             asm volatile("" : "+v"(l32), "+v"(hi), "+v"(tid));
-            // (every thread takes one of each, wanted or not: a branch here costs the accumulators their registers)
-            const int64_t f = min(n0 + min(tid, TN - 1), p.a.N - 1);
-            tile_xs[tid] = p.a.xs[min(m0 + min(tid, TM - 1), p.a.M - 1)];
-            tile_ws[tid] = p.a.ws[f];
-            tile_add[tid] = p.a.bias ? bias_at(p.a, f) : 0.f;
+            tile_xs[tid] = my_xs; tile_ws[tid] = my_ws; tile_add[tid] = __uint_as_float(p.a.bias_dt == NM_DT_BF16 ? my_add << 16 : my_add);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             const int rows = (int)min(p.a.M - m0, (int64_t)TM), cols = (int)min(p.a.N - n0, (int64_t)TN);
             char *y0 = (char *)((OutT *)p.a.y + m0 * p.a.ldy + n0);
-            const auto y_buffer = __builtin_amdgcn_make_buffer_rsrc((void *)y0, 0, 0x7fffffff, 0x00020000);
             const float least = p.a.relu ? 0.f : -__builtin_inff();
-            float xs[AM];
-            uint32_t at_row[AM];
+            if constexpr (OT == NM_DT_F32) {
+                // a lane holds the tokens 8 g + 4 hi .. + 3 of feature l32 of each block.  What is not there is sent out of the buffer's range, which drops it: branches
+                // here cost the accumulators their registers.
+                const auto y_buffer = __builtin_amdgcn_make_buffer_rsrc((void *)y0, 0, 0x7fffffff, 0x00020000);
+                const uint32_t row_bytes = (uint32_t)p.a.ldy * 4u;
 #pragma unroll
-            for (int a = 0; a < AM; ++a) {
-                const int row = (wm * AM + a) * 32 + l32;
-                xs[a] = tile_xs[row];
-                at_row[a] = (uint32_t)row * (uint32_t)p.a.ldy * (uint32_t)sizeof(OutT);
-            }
+                for (int b = 0; b < AN; ++b) {
+                    const int f = (wn * AN + b) * 32 + l32;
+                    const float ws = tile_ws[f], add = tile_add[f];
 #pragma unroll
-            for (int b = 0; b < AN; ++b) {
+                    for (int a = 0; a < AM; ++a) {
 #pragma unroll
-                for (int a = 0; a < AM; ++a) {
-                    const bool there = (wm * AM + a) * 32 + l32 < rows;
+                        for (int g = 0; g < 4; ++g) {
+                            const int row = (wm * AM + a) * 32 + 8 * g + 4 * hi;
+                            const float4 xs = *(const float4 *)&tile_xs[row];
+                            const float x4[4] = {xs.x, xs.y, xs.z, xs.w};
+                            const uint32_t at = (uint32_t)row * row_bytes + (uint32_t)f * 4u;
 #pragma unroll
-                    for (int g = 0; g < 4; g += 2) {
-                        const int f0 = (wn * AN + b) * 32 + 8 * g + 4 * hi;          // a lane holds the features f0 .. + 3 and f0 + 8 .. + 3 of a token
-                        float v[2][4];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float4 ws = *(const float4 *)&tile_ws[f0 + 8 * i], add = *(const float4 *)&tile_add[f0 + 8 * i];
-                            v[i][0] = (float)__float_as_int(acc[a][b][4 * (g + i)]) * (xs[a] * ws.x) + add.x;
-                            v[i][1] = (float)__float_as_int(acc[a][b][4 * (g + i) + 1]) * (xs[a] * ws.y) + add.y;
-                            v[i][2] = (float)__float_as_int(acc[a][b][4 * (g + i) + 2]) * (xs[a] * ws.z) + add.z;
-                            v[i][3] = (float)__float_as_int(acc[a][b][4 * (g + i) + 3]) * (xs[a] * ws.w) + add.w;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) v[i][j] = v[i][j] <= least ? least : v[i][j];        // (a NaN stays one)
-                        }
-                        if constexpr (OT == NM_DT_F32) {
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const uint32_t at = at_row[a] + (uint32_t)(f0 + 8 * i) * 4u;
-                                if constexpr (WHOLE) {
-                                    if (there && f0 + 8 * i < cols) *(u32x4_any *)(y0 + at) = u32x4{__float_as_uint(v[i][0]), __float_as_uint(v[i][1]), __float_as_uint(v[i][2]), __float_as_uint(v[i][3])};
-                                } else
-                                    // (what is not there is sent out of the buffer's range, which drops it: branches here cost the accumulators their registers)
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j)
-                                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[i][j]), y_buffer, there && f0 + 8 * i + j < cols ? (int)(at + 4u * j) : -1, 0, 0);
+                            for (int j = 0; j < 4; ++j) {
+                                float v = sum_of(acc[a][b][4 * g + j]) * (x4[j] * ws) + add;
+                                v = v <= least ? least : v;                          // (a NaN stays one)
+                                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), y_buffer, row + j < rows && f < cols ? (int)(at + (uint32_t)j * row_bytes) : -1, 0, 0);
                             }
-                        } else {
-                            // the two halves of the wave exchange, so that a lane holds eight features in a row: the lower half the first eight, the upper the eight behind
-                            const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16_rne(v[0][0], v[0][1]), pack_bf16_rne(v[1][0], v[1][1]), false, false),
-                                       up = __builtin_amdgcn_permlane32_swap(pack_bf16_rne(v[0][2], v[0][3]), pack_bf16_rne(v[1][2], v[1][3]), false, false);
-                            const int f = f0 + 4 * hi;
-                            if (there) store_features<WHOLE>(y0 + at_row[a] + (uint32_t)f * 2u, cols - f, u32x4{lo[0], up[0], lo[1], up[1]});
+                            __builtin_amdgcn_sched_barrier(0);
                         }
+                        acc_clear(acc[a][b]);
                         __builtin_amdgcn_sched_barrier(0);
                     }
-                    acc_clear(acc[a][b]);
-                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                // A lane holds four features of every eight of a token.  The halves of the wave exchange, so that it holds eight in a row, and their quarters then, so that four
+                // lanes hold the 64 bytes that a block has of a token; the neighbouring blocks' follow at once.  (Stores of 32 bytes of a token: 16384 x 1024 -> 4096
+                // 99 us, blocks apart 132.)
+                const int q = tid & 63, chunk = (q >> 4 & 1) * 2 + (q >> 5), l16 = q & 15;
+#pragma unroll
+                for (int a = 0; a < AM; ++a) {
+                    const int row = (wm * AM + a) * 32 + l16;
+                    const float xs = tile_xs[(wm * AM + a) * 32 + l32];
+                    const uint32_t at_row = (uint32_t)row * (uint32_t)p.a.ldy * 2u, half = (uint32_t)p.a.ldy * 32u;
+#pragma unroll
+                    for (int b = 0; b < AN; ++b) {
+                        u32x4 r[2];
+#pragma unroll
+                        for (int g = 0; g < 4; g += 2) {
+                            uint32_t w[2][2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int f0 = (wn * AN + b) * 32 + 8 * (g + i) + 4 * hi;
+                                const float4 ws = *(const float4 *)&tile_ws[f0], add = *(const float4 *)&tile_add[f0];
+                                const float w4[4] = {ws.x, ws.y, ws.z, ws.w}, b4[4] = {add.x, add.y, add.z, add.w};
+                                float v[4];
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const float t = sum_of(acc[a][b][4 * (g + i) + j]) * (xs * w4[j]) + b4[j];
+                                    v[j] = t <= least ? least : t;                   // (a NaN stays one)
+                                }
+                                w[i][0] = pack_bf16_rne(v[0], v[1]);
+                                w[i][1] = pack_bf16_rne(v[2], v[3]);
+                            }
+                            const auto lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false), up = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                            r[g / 2] = u32x4{lo[0], up[0], lo[1], up[1]};
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const auto both = __builtin_amdgcn_permlane16_swap(r[0][i], r[1][i], false, false);
+                            r[0][i] = both[0];
+                            r[1][i] = both[1];
+                        }
+                        const int f = (wn * AN + b) * 32 + 8 * chunk;
+                        if (row < rows) store_features<WHOLE>(y0 + at_row + (uint32_t)f * 2u, cols - f, r[0]);
+                        if (row + 16 < rows) store_features<WHOLE>(y0 + at_row + half + (uint32_t)f * 2u, cols - f, r[1]);
+                        acc_clear(acc[a][b]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
             }
             sums_settled();                                                          // (of the zeros)
@@ -349,18 +388,21 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
 hipError_t launch_gemm_i8(const I8Arg &a, hipStream_t st)
 {
     if (a.M == 0 || a.N == 0) return hipSuccess;
+    if (gemm_i8_few_takes(a.M, a.N)) return launch_gemm_i8_few(a, nullptr, 0, 0, st);
     I8Tiles p{a, 0, 0};
-    struct Tile { int tm, tn, per_cu; double alone, shared, round; };
-    constexpr Tile tiles[5] = {{64, 64, 2, 0.25, 0.42, 0.7}, {128, 64, 2, 0.33, 0.70, 1.0}, {128, 128, 2, 0.85, 1.0, 1.5}, {128, 128, 1, 0.25, 0.55, 1.5}, {256, 256, 1, 0.6, 1.75, 5.0}};
+    struct Tile { int tm, tn, per_cu; double alone, shared, round, round_f32; };
+    constexpr Tile tiles[5] = {{64, 64, 2, 0.20, 0.69, 0.58, 0.62}, {128, 64, 2, 0.23, 0.59, 0.99, 0.65}, {128, 128, 2, 0.58, 0.78, 1.51, 2.05}, {128, 128, 1, 0.41, 0.51, 1.13, 0.69},
+                               {256, 256, 1, 1.00, 1.13, 3.4, 12.5}};
     const double stages = (double)((a.K + I8_K - 1) / I8_K);
     int best = 0;
     double least = 1e300;
     for (int i = 0; i < 5; ++i) {
         const Tile &t = tiles[i];
-        const int64_t n = ((a.M + t.tm - 1) / t.tm) * ((a.N + t.tn - 1) / t.tn), round = (int64_t)t.per_cu * NM_CUS, left = n % round;
-        if (i == 3 && n > NM_CUS) continue;
+        if (i > 0 && a.M <= 64) continue;                                        // (half of the rows would be nobody's: 16 x 8192 -> 28672 50 us against 54 to 103)
+        const int64_t n = ((a.M + t.tm - 1) / t.tm) * ((a.N + t.tn - 1) / t.tn), whole = (int64_t)t.per_cu * NM_CUS, left = n % whole;
+        const double round = a.y_dt == NM_DT_F32 ? t.round_f32 : t.round;
         const double part = t.per_cu == 1 ? t.alone + (t.shared - t.alone) * (double)left / NM_CUS : left <= NM_CUS ? t.alone : t.shared;
-        const double cost = (double)(n / round) * (stages * t.shared + t.round) + (left ? stages * part + t.round : 0.0);
+        const double cost = (double)(n / whole) * (stages * t.shared + round) + (left ? stages * part + round : 0.0);
         if (cost < least) { least = cost; best = i; }
     }
     const int64_t tm = (a.M + tiles[best].tm - 1) / tiles[best].tm, tn = (a.N + tiles[best].tn - 1) / tiles[best].tn, n_tiles = tm * tn;
@@ -368,15 +410,12 @@ hipError_t launch_gemm_i8(const I8Arg &a, hipStream_t st)
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
     const int64_t wgs = std::min<int64_t>(n_tiles, (int64_t)tiles[best].per_cu * NM_CUS);
-#define NM_I8_W(WM, WN, AM, AN, NS, OT)                                                                                                                   \
-    do {                                                                                                                                                  \
-        if (a.N % 8 == 0) hipLaunchKernelGGL((gemm_i8_kernel<WM, WN, AM, AN, NS, OT, true>), dim3((unsigned)wgs), dim3(WM * WN * 64), 0, st, p);           \
-        else hipLaunchKernelGGL((gemm_i8_kernel<WM, WN, AM, AN, NS, OT, false>), dim3((unsigned)wgs), dim3(WM * WN * 64), 0, st, p);                       \
-    } while (0)
-#define NM_I8(WM, WN, AM, AN, NS)                                                                                                                         \
-    do {                                                                                                                                                  \
-        if (a.y_dt == NM_DT_F32) NM_I8_W(WM, WN, AM, AN, NS, NM_DT_F32);                                                                                  \
-        else NM_I8_W(WM, WN, AM, AN, NS, NM_DT_BF16);                                                                                                     \
+#define NM_I8_W(WM, WN, AM, AN, NS, OT, WHOLE) hipLaunchKernelGGL((gemm_i8_kernel<WM, WN, AM, AN, NS, OT, WHOLE>), dim3((unsigned)wgs), dim3(WM * WN * 64), 0, st, p)
+#define NM_I8(WM, WN, AM, AN, NS)                                                             \
+    do {                                                                                          \
+        if (a.y_dt == NM_DT_F32) NM_I8_W(WM, WN, AM, AN, NS, NM_DT_F32, false);               \
+        else if (a.N % 8 == 0) NM_I8_W(WM, WN, AM, AN, NS, NM_DT_BF16, true);                 \
+        else NM_I8_W(WM, WN, AM, AN, NS, NM_DT_BF16, false);                                  \
     } while (0)
     switch (best) {
     case 0: NM_I8(2, 2, 1, 1, 4); break;

@@ -181,6 +181,11 @@ struct I8Arg {
     int bias_dt, y_dt, relu, x_zeros;
 };
 hipError_t launch_gemm_i8(const I8Arg &p, hipStream_t st);
+// the same for few tokens or features (gemm_i8_few.hip: ..._takes); raw: the tokens themselves, of raw_dt, in x's place (where ..._fused says so)
+constexpr int64_t I8_FEW = 32;
+bool gemm_i8_few_takes(int64_t M, int64_t N);
+bool gemm_i8_few_fused(int64_t M, int64_t K);
+hipError_t launch_gemm_i8_few(const I8Arg &a, const void *raw, int64_t ldraw, int raw_dt, hipStream_t st);
 
 // ---- embedding (embed.hip).  ids: 32 or 64 bits wide
 hipError_t launch_embed(int table_dt, int out_dt, const void *table, int64_t V, int64_t D, int64_t ldt, const void *ids, bool wide, int64_t N, float scale, void *out,

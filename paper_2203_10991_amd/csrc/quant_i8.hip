@@ -8,59 +8,20 @@
 #include <algorithm>
 
 #include "nm_internal.h"
-#include "prune_common.h"        // Row
+#include "quant_i8.h"
 
 namespace nm {
 
 namespace {
 
-// factor and scale from the bits of the largest magnitude (which order like the magnitudes, with what is not finite on top)
-__device__ __forceinline__ void factors(uint32_t top, float &up, float &scale)
-{
-    const float a = __uint_as_float(top);
-    if (top >= 0x7f800000u) { up = 0.f; scale = __uint_as_float(0x7fc00000u); }
-    else if (a < 0x1p-110f) { up = 0.f; scale = 0.f; }
-    else                    { up = 127.f * (1.f / a); scale = a / 127.f; }
-}
-__device__ __forceinline__ uint32_t code(float x, float up)
-{
-    // (a product may pass 127 by a rounding: it still rounds to 127.  Where up is 0 a value that is not finite gives a NaN: code 0)
-    return (uint32_t)(int)rintf(up == 0.f ? 0.f : x * up) & 0xffu;
-}
-__device__ __forceinline__ uint32_t wave_max_u(uint32_t v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-    return v;
-}
-
-// eight consecutive elements as binary32; VEC: on a 16-byte boundary.  Elements from `left` on are zeros
-template <int DT, bool VEC> __device__ __forceinline__ void load8(const void *p, int64_t at, int64_t left, float (&v)[8])
-{
-    if (VEC && left >= 8) {
-        if constexpr (DT == NM_DT_F32) {
-            const float4 a = *(const float4 *)((const float *)p + at), b = *(const float4 *)((const float *)p + at + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 a = *(const uint4 *)((const uint16_t *)p + at);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = Row<NM_DT_BF16>::get(a, i);
-        }
-    } else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = 0.f;
-            if (i < left) v[i] = DT == NM_DT_F32 ? ((const float *)p)[at + i] : __uint_as_float((uint32_t)((const uint16_t *)p)[at + i] << 16);
-        }
-}
-
 // ---- rows: T threads to a row, T * 8 elements at a time; up to KEEP of them stay in registers between the two passes
-template <int DT, bool VEC, int T, int KEEP>
-__global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale)
+template <int T> constexpr int rows_wg = T > 256 ? T : 256;
+template <int DT, int T, int KEEP>
+__global__ __launch_bounds__(rows_wg<T>) void quant_rows_kernel(const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale)
 {
-    __shared__ uint32_t tops[256 / T][T / 64];
+    __shared__ uint32_t tops[rows_wg<T> / T][T / 64];
     const int lane = threadIdx.x % T, mine = threadIdx.x / T;
-    const int64_t r = (int64_t)blockIdx.x * (256 / T) + mine;
+    const int64_t r = (int64_t)blockIdx.x * (rows_wg<T> / T) + mine;
     const bool there = r < R;
     float v[KEEP][8];
     uint32_t top = 0;
@@ -68,20 +29,20 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t 
 #pragma unroll
         for (int k = 0; k < KEEP; ++k) {
             const int64_t c = ((int64_t)k * T + lane) * 8;
-            load8<DT, VEC>(x, r * ld + c, C - c, v[k]);
+            load8<DT>(x, r * ld + c, C - c, v[k]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[k][i]) & 0x7fffffffu);
         }
     if (there)
         for (int64_t c = ((int64_t)KEEP * T + lane) * 8; c < C; c += T * 8) {
             float w[8];
-            load8<DT, VEC>(x, r * ld + c, C - c, w);
+            load8<DT>(x, r * ld + c, C - c, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(w[i]) & 0x7fffffffu);
         }
     top = wave_max_u(top);
     if constexpr (T > 64) {
-        if (threadIdx.x % 64 == 0) tops[mine][lane / 64] = top;
+        if (lane % 64 == 0) tops[mine][lane / 64] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < T / 64; ++w) top = max(top, tops[mine][w]);
@@ -100,14 +61,14 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const void *x, int64_t 
     for (int k = 0; k < KEEP; ++k) put(((int64_t)k * T + lane) * 8, v[k]);
     for (int64_t c = ((int64_t)KEEP * T + lane) * 8; c < ldq; c += T * 8) {
         float w[8];
-        load8<DT, VEC>(x, r * ld + c, C - c, w);
+        load8<DT>(x, r * ld + c, C - c, w);
         put(c, w);
     }
 }
 
 // ---- columns, transposed.  First the largest magnitudes of a slab of rows for eight columns a thread
 constexpr int TILE = 64;         // rows and columns of a tile that is turned
-template <int DT, bool VEC>
+template <int DT>
 __global__ __launch_bounds__(256) void column_top_kernel(const void *x, int64_t R, int64_t C, int64_t ld, uint32_t *part, int64_t rows_per_slab)
 {
     const int64_t c = ((int64_t)blockIdx.x * 32 + threadIdx.x % 32) * 8;
@@ -117,7 +78,7 @@ __global__ __launch_bounds__(256) void column_top_kernel(const void *x, int64_t 
 #pragma unroll 4
         for (int64_t r = from + threadIdx.x / 32; r < to; r += 8) {
             float v[8];
-            load8<DT, VEC>(x, r * ld + c, C - c, v);
+            load8<DT>(x, r * ld + c, C - c, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top[i] = max(top[i], __float_as_uint(v[i]) & 0x7fffffffu);
         }
@@ -132,33 +93,44 @@ __global__ __launch_bounds__(256) void column_top_kernel(const void *x, int64_t 
     const int64_t at = (int64_t)blockIdx.x * 256 + col;
     if (at < C) part[(int64_t)blockIdx.y * C + at] = m;
 }
-template <int DT, bool VEC>
+// Then tiles of 64 x 64, turned through LDS in blocks of four columns by four rows: a thread packs four rows of a column into a word
+template <int DT>
 __global__ __launch_bounds__(256) void quant_turn_kernel(const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, const uint32_t *part, int slabs)
 {
+    __shared__ uint32_t tops[4][TILE];
     __shared__ float ups[TILE];
-    __shared__ __attribute__((aligned(16))) uint8_t turned[TILE][TILE + 16];         // [column][row]
+    __shared__ uint32_t turned[TILE][TILE / 4 + 1];                                  // [column][four rows]
     const int tid = threadIdx.x;
     const int64_t r0 = (int64_t)blockIdx.x * TILE, c0 = (int64_t)blockIdx.y * TILE;
-    if (tid < TILE && c0 + tid < C) {
-        uint32_t top = 0;
-        for (int s = 0; s < slabs; ++s) top = max(top, part[(int64_t)s * C + c0 + tid]);
+    // eight columns of rows 4 k .. 4 k + 3, on their way while the slabs' tops are compared
+    const int k = tid / 8 % 16, col = tid % 8 * 8, half = tid / 128;                 // (a thread loads two of the four rows, and gets the others from its partner)
+    float v[2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int row = 4 * k + 2 * half + i;
+        load8<DT>(x, (r0 + row) * ld + c0 + col, r0 + row < R ? C - c0 - col : 0, v[i]);
+    }
+    uint32_t top = 0;
+    if (c0 + tid % TILE < C)
+        for (int s = tid / TILE; s < slabs; s += 4) top = max(top, part[(int64_t)s * C + c0 + tid % TILE]);
+    tops[tid / TILE][tid % TILE] = top;
+    __syncthreads();
+    if (tid < TILE) {
         float up, sc;
-        factors(top, up, sc);
+        factors(max(max(tops[0][tid], tops[1][tid]), max(tops[2][tid], tops[3][tid])), up, sc);
         ups[tid] = up;
-        if (blockIdx.x == 0) scale[c0 + tid] = sc;
+        if (blockIdx.x == 0 && c0 + tid < C) scale[c0 + tid] = sc;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int row = k * 32 + tid / 8, col = tid % 8 * 8;
-        float v[8];
-        load8<DT, VEC>(x, (r0 + row) * ld + c0 + col, r0 + row < R ? C - c0 - col : 0, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) turned[col + i][row] = c0 + col + i < C ? (uint8_t)code(v[i], ups[col + i]) : 0;
+    for (int i = 0; i < 8; ++i) {
+        const float up = ups[col + i];
+        ((uint16_t *)&turned[col + i][k])[half] = (uint16_t)(code(v[0][i], up) | code(v[1][i], up) << 8);
     }
     __syncthreads();
-    const int col = tid / 4, row = tid % 4 * 16;
-    if (c0 + col < C && r0 + row < ldq) *(uint4 *)(q + (c0 + col) * ldq + r0 + row) = *(const uint4 *)&turned[col][row];
+    const int out = tid / 4, word = tid % 4 * 4;
+    if (c0 + out < C && r0 + 4 * word < ldq)
+        *(uint4 *)(q + (c0 + out) * ldq + r0 + 4 * word) = make_uint4(turned[out][word], turned[out][word + 1], turned[out][word + 2], turned[out][word + 3]);
 }
 
 }  // namespace
@@ -166,21 +138,16 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const void *x, int64_t 
 hipError_t launch_quant_i8(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, hipStream_t st)
 {
     if (R == 0) return hipSuccess;
-    const int64_t e = dt == NM_DT_F32 ? 4 : 2;
-    const bool vec = (uintptr_t)x % 16 == 0 && ld * e % 16 == 0;
-#define NM_QUANT_D(DT, T, KEEP)                                                                                                                  \
-    do {                                                                                                                                         \
-        if (vec) hipLaunchKernelGGL((quant_rows_kernel<DT, true, T, KEEP>), dim3((unsigned)wgs), dim3(256), 0, st, x, R, C, ld, q, ldq, scale);  \
-        else hipLaunchKernelGGL((quant_rows_kernel<DT, false, T, KEEP>), dim3((unsigned)wgs), dim3(256), 0, st, x, R, C, ld, q, ldq, scale);     \
-    } while (0)
+#define NM_QUANT_D(DT, T, KEEP) hipLaunchKernelGGL((quant_rows_kernel<DT, T, KEEP>), dim3((unsigned)wgs), dim3(rows_wg<T>), 0, st, x, R, C, ld, q, ldq, scale)
 #define NM_QUANT(T, KEEP)                                                                       \
     do {                                                                                        \
-        const int64_t wgs = (R + 256 / T - 1) / (256 / T);                                      \
+        const int64_t wgs = (R + rows_wg<T> / T - 1) / (rows_wg<T> / T);                        \
         if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;                              \
         if (dt == NM_DT_F32) NM_QUANT_D(NM_DT_F32, T, KEEP); else NM_QUANT_D(NM_DT_BF16, T, KEEP); \
     } while (0)
     if (C <= 512) NM_QUANT(64, 1);
     else if (C <= 1024) NM_QUANT(64, 2);
+    else if (R <= 512 && C > 2048) NM_QUANT(1024, 1);               // (rows that leave CUs idle)
     else if (C <= 4096) NM_QUANT(256, 2);
     else NM_QUANT(256, 4);
 #undef NM_QUANT
@@ -198,18 +165,15 @@ int quant_i8_slabs(int64_t R, int64_t C)
 hipError_t launch_quant_i8_t(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, uint32_t *part, hipStream_t st)
 {
     if (C == 0) return hipSuccess;
-    const int64_t e = dt == NM_DT_F32 ? 4 : 2;
-    const bool vec = (uintptr_t)x % 16 == 0 && ld * e % 16 == 0;
     const int slabs = quant_i8_slabs(R, C);
     const int64_t per = (R + slabs - 1) / slabs, panels = (C + 255) / 256, tr = std::max<int64_t>((ldq + TILE - 1) / TILE, 1), tc = (C + TILE - 1) / TILE;
     if (panels > 0x7fffffff || tr > 0x7fffffff || tc > 65535) return hipErrorInvalidConfiguration;
-#define NM_TURN(DT, VEC)                                                                                                                             \
-    do {                                                                                                                                             \
-        hipLaunchKernelGGL((column_top_kernel<DT, VEC>), dim3((unsigned)panels, (unsigned)slabs), dim3(256), 0, st, x, R, C, ld, part, per);         \
-        hipLaunchKernelGGL((quant_turn_kernel<DT, VEC>), dim3((unsigned)tr, (unsigned)tc), dim3(256), 0, st, x, R, C, ld, q, ldq, scale, part, slabs); \
+#define NM_TURN(DT)                                                                                                                              \
+    do {                                                                                                                                         \
+        hipLaunchKernelGGL((column_top_kernel<DT>), dim3((unsigned)panels, (unsigned)slabs), dim3(256), 0, st, x, R, C, ld, part, per);          \
+        hipLaunchKernelGGL((quant_turn_kernel<DT>), dim3((unsigned)tr, (unsigned)tc), dim3(256), 0, st, x, R, C, ld, q, ldq, scale, part, slabs); \
     } while (0)
-    if (dt == NM_DT_F32) { if (vec) NM_TURN(NM_DT_F32, true); else NM_TURN(NM_DT_F32, false); }
-    else                 { if (vec) NM_TURN(NM_DT_BF16, true); else NM_TURN(NM_DT_BF16, false); }
+    if (dt == NM_DT_F32) NM_TURN(NM_DT_F32); else NM_TURN(NM_DT_BF16);
 #undef NM_TURN
     return hipGetLastError();
 }

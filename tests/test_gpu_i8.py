@@ -92,7 +92,7 @@ def _check(y, q, xs, w, ws, bias, relu):
 
 
 SIZES = [(1, 1, 1), (1, 4096, 1024), (2, 33, 16), (16, 40, 127), (17, 8, 128), (31, 129, 129), (33, 1000, 250), (64, 64, 384), (65, 72, 4096), (100, 1333, 1001),
-         (197, 264, 256), (300, 135, 2050), (1, 300, 8192), (7, 5000, 515), (512, 512, 640)]
+         (197, 264, 256), (300, 135, 2050), (1, 300, 8192), (7, 5000, 515), (32, 70, 3000), (32, 16, 20000), (33, 70, 3000), (5, 1, 40), (512, 512, 640)]
 # each tile: one, several of them to a workgroup, ragged on every side
 TILES = [(2435, 1608, 520, "2, 2, 1, 1, 4"), (5116, 1567, 416, "2, 2, 2, 1, 3"), (9000, 3080, 72, "2, 2, 2, 2, 2"), (9000, 4103, 200, "2, 2, 2, 2, 2"),
          (2047, 1032, 72, "2, 4, 2, 1, 4"), (2774, 941, 1500, "2, 4, 2, 1, 4"), (5000, 2056, 264, "2, 4, 4, 2, 2"), (13357, 2013, 736, "2, 4, 4, 2, 2")]
@@ -139,7 +139,7 @@ def test_sums_that_fill_32_bits():
 
 
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
-@pytest.mark.parametrize("T,O,I", [(1, 1, 1), (1, 4096, 1024), (4, 100, 77), (16, 1000, 2048), (33, 65, 130), (197, 264, 1001), (1576, 1333, 1001), (40, 24, 9000)])
+@pytest.mark.parametrize("T,O,I", [(1, 1, 1), (1, 4096, 1024), (4, 100, 77), (16, 1000, 2048), (33, 65, 130), (1, 70, 16000), (1, 70, 17000), (4, 33, 4031), (4, 33, 4097), (3, 1000, 15), (2, 17, 64), (197, 264, 1001), (1576, 1333, 1001), (40, 24, 9000)])
 def test_layer(dtype, out, T, O, I):
     """nm_linear_i8 is the rounding of x and the product, bit for bit; x a view with NaN around it, in three dimensions"""
     import paper_2203_10991_amd as nm
