@@ -93,9 +93,14 @@ def _check(y, q, xs, w, ws, bias, relu):
 
 SIZES = [(1, 1, 1), (1, 4096, 1024), (2, 33, 16), (16, 40, 127), (17, 8, 128), (31, 129, 129), (33, 1000, 250), (64, 64, 384), (65, 72, 4096), (100, 1333, 1001),
          (197, 264, 256), (300, 135, 2050), (1, 300, 8192), (7, 5000, 515), (32, 70, 3000), (32, 16, 20000), (33, 70, 3000), (5, 1, 40), (512, 512, 640)]
-# each tile: one, several of them to a workgroup, ragged on every side
-TILES = [(2435, 1608, 520, "2, 2, 1, 1, 4"), (5116, 1567, 416, "2, 2, 2, 1, 3"), (9000, 3080, 72, "2, 2, 2, 2, 2"), (9000, 4103, 200, "2, 2, 2, 2, 2"),
-         (2047, 1032, 72, "2, 4, 2, 1, 4"), (2774, 941, 1500, "2, 4, 2, 1, 4"), (5000, 2056, 264, "2, 4, 4, 2, 2"), (13357, 2013, 736, "2, 4, 4, 2, 2")]
+# each tile, for bf16 and binary32 results: one of them to a workgroup and several, ragged on every side
+TILES = [(2771, 65, 77, BF16, "2, 2, 1, 1, 4"), (2231, 113, 61, F32, "2, 2, 1, 1, 4"), (914, 1381, 503, BF16, "2, 2, 2, 1, 3"), (13379, 1184, 189, BF16, "2, 2, 2, 1, 3"),
+         (914, 1381, 503, F32, "2, 2, 2, 1, 3"), (12187, 337, 1947, F32, "2, 2, 2, 1, 3"), (12187, 337, 1947, BF16, "2, 2, 2, 2, 2"), (10270, 2192, 1508, BF16, "2, 2, 2, 2, 2"),
+         (6303, 935, 2390, F32, "2, 2, 2, 2, 2"), (10270, 2189, 1508, F32, "2, 2, 2, 2, 2"), (7484, 482, 2938, BF16, "2, 4, 2, 1, 4"), (7484, 482, 2938, F32, "2, 4, 2, 1, 4"),
+         (6343, 2547, 128, F32, "2, 4, 2, 1, 4"), (6343, 2547, 127, BF16, "2, 4, 4, 2, 2"), (9727, 3107, 1251, BF16, "2, 4, 4, 2, 2"), (12052, 1187, 2622, F32, "2, 4, 4, 2, 2")]
+# few tokens, or few features: blocks of 16 or 32 tokens and of 16 or 32 features
+FEW = [(1, 4096, 1024, "1, 2, false"), (16, 70, 3000, "1, 1, false"), (9, 9000, 500, "1, 2, false"), (17, 70, 3000, "2, 1, false"), (32, 9001, 1300, "2, 2, false"),
+       (600, 200, 2001, "2, 1, false"), (1000, 200, 2001, "2, 2, false"), (700, 90, 77, "2, 2, false"), (64, 4096, 1023, "2, 2, false")]
 
 
 @pytest.mark.parametrize("layout", ["padded", "loose"])
@@ -114,9 +119,7 @@ def test_product(T, O, I, out, layout):
         _check(y, q, xs, w, ws, bias, relu)
 
 
-@pytest.mark.parametrize("out", [F32, BF16])
-@pytest.mark.parametrize("T,O,I,kernel", TILES)
-def test_every_tile(T, O, I, kernel, out):
+def _route(T, O, I, out):
     import paper_2203_10991_amd as nm
     gen = torch.Generator().manual_seed(T)
     q, xq = _random_codes(T, I, gen, "loose")
@@ -124,6 +127,28 @@ def test_every_tile(T, O, I, kernel, out):
     xs, ws, bias = torch.rand(T, generator=gen) + 0.1, torch.rand(O, generator=gen) + 0.1, torch.randn(O, generator=gen) * 1e3
     args = (xq, xs.to(DEV), wq, ws.to(DEV), bias.to(DEV))
     _check(nm.nm_gemm_i8(*args, out_dtype=out), q, xs, w, ws, bias, False)
+    return kernels_of(lambda: nm.nm_gemm_i8(*args, out_dtype=out))
+
+
+@pytest.mark.parametrize("T,O,I,out,kernel", TILES)
+def test_every_tile(T, O, I, out, kernel):
+    names = _route(T, O, I, out)
+    assert any(f"gemm_i8_kernel<{kernel}, " in k for k in names), names
+
+
+@pytest.mark.parametrize("T,O,I,kernel", FEW)
+def test_few_tokens_or_features(T, O, I, kernel):
+    names = _route(T, O, I, BF16)
+    assert any(f"gemm_i8_few_kernel<{kernel}>" in k for k in names), names
+
+
+@pytest.mark.parametrize("T,I,fused", [(1, 1024, True), (4, 4000, True), (4, 4100, False), (1, 16000, True), (1, 17000, False), (5, 64, False)])
+def test_tokens_rounded_inside_the_product(T, I, fused):
+    import paper_2203_10991_amd as nm
+    wq, ws = nm.nm_quant_i8(torch.randn(100, I, device=DEV))
+    x = torch.randn(T, I, device=DEV)
+    names = kernels_of(lambda: nm.nm_linear_i8(x, wq, ws))
+    assert any("quant_rows_kernel" in k for k in names) != fused and any("gemm_i8_few_kernel<1, 1, true>" in k for k in names) == fused, names
 
 
 def test_sums_that_fill_32_bits():
