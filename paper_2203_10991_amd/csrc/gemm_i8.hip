@@ -384,14 +384,19 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_i8_kernel(I8Tiles p)
 
 }  // namespace
 
-// Tiles as those of the bf16 products (gemm_dense.hip), whose stages move the same bytes
+// The tile whose time a model puts lowest: rounds of one or two tiles to a CU (`per_cu`), a round's stages in us at one tile to a CU (`alone`) and with every place
+// taken (`shared`), and what a round costs besides (`round`, and `round_f32` where the results are binary32).  Fitted to sweeps of all five over products of 65 to
+// 16384 tokens whose operands were in the caches; what the model takes is 0.3 % from the best.  (us, 64 x 64 / 128 x 64 / 128 x 128 two to a CU / one / 256 x 256:
+// 512 x 1024 -> 1024 7.5 / 8.4 / 10.0 / 10.0 / 18.5, 2048 x 2048 -> 2048 22.9 / 17.2 / 16.7 / 16.3 / 29.2, 2048 x 1024 -> 4096 26.2 / 19.4 / 16.4 / 18.5 /
+// 21.5, 4096 x 4096 -> 4096 136 / 99 / 77 / 87 / 65, 16384 x 1024 -> 4096 166 / 127 / 99 / 115 / 82.)
+// Few tokens or features go to gemm_i8_few.hip where its own model's time is the lower one; 4.1 + 1.6 times is what this one's become with weights that
+// come from memory.
 hipError_t launch_gemm_i8(const I8Arg &a, hipStream_t st)
 {
     if (a.M == 0 || a.N == 0) return hipSuccess;
-    if (gemm_i8_few_takes(a.M, a.N)) return launch_gemm_i8_few(a, nullptr, 0, 0, st);
     I8Tiles p{a, 0, 0};
     struct Tile { int tm, tn, per_cu; double alone, shared, round, round_f32; };
-    constexpr Tile tiles[5] = {{64, 64, 2, 0.20, 0.69, 0.58, 0.62}, {128, 64, 2, 0.23, 0.59, 0.99, 0.65}, {128, 128, 2, 0.58, 0.78, 1.51, 2.05}, {128, 128, 1, 0.41, 0.51, 1.13, 0.69},
+    constexpr Tile tiles[5] = {{64, 64, 2, 0.20, 0.45, 0.58, 0.62}, {128, 64, 2, 0.23, 0.59, 0.99, 0.65}, {128, 128, 2, 0.58, 0.78, 1.51, 2.05}, {128, 128, 1, 0.41, 0.51, 1.13, 0.69},
                                {256, 256, 1, 1.00, 1.13, 3.4, 12.5}};
     const double stages = (double)((a.K + I8_K - 1) / I8_K);
     int best = 0;
@@ -405,6 +410,7 @@ hipError_t launch_gemm_i8(const I8Arg &a, hipStream_t st)
         const double cost = (double)(n / whole) * (stages * t.shared + round) + (left ? stages * part + round : 0.0);
         if (cost < least) { least = cost; best = i; }
     }
+    if (gemm_i8_few_plan(a.M, a.N, a.K).us < 4.1 + 1.6 * least) return launch_gemm_i8_few(a, nullptr, 0, 0, st);
     const int64_t tm = (a.M + tiles[best].tm - 1) / tiles[best].tm, tn = (a.N + tiles[best].tn - 1) / tiles[best].tn, n_tiles = tm * tn;
     if (n_tiles > 0x7fffffffll - 1024) return hipErrorInvalidConfiguration;
     p.tiles_m = (int)tm;

@@ -181,9 +181,10 @@ struct I8Arg {
     int bias_dt, y_dt, relu, x_zeros;
 };
 hipError_t launch_gemm_i8(const I8Arg &p, hipStream_t st);
-// the same for few tokens or features (gemm_i8_few.hip: ..._takes); raw: the tokens themselves, of raw_dt, in x's place (where ..._fused says so)
-constexpr int64_t I8_FEW = 32;
-bool gemm_i8_few_takes(int64_t M, int64_t N);
+// the same for few tokens or features (gemm_i8_few.hip): blocks of 16 tokens and of 16 features to a workgroup, and the time to expect.
+// raw: the tokens themselves, of raw_dt, in x's place (where ..._fused says so)
+struct I8FewPlan { int tt, ft; double us; };
+I8FewPlan gemm_i8_few_plan(int64_t M, int64_t N, int64_t K);
 bool gemm_i8_few_fused(int64_t M, int64_t K);
 hipError_t launch_gemm_i8_few(const I8Arg &a, const void *raw, int64_t ldraw, int raw_dt, hipStream_t st);
 

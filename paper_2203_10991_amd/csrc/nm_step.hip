@@ -158,7 +158,7 @@ int nm_linear_i8(const void *x, int64_t ldx, int x_dtype, const int8_t *wq, int6
     float *s = (float *)(q + T * row);
     hipStream_t st = (hipStream_t)hip_stream;
     const nm::I8Arg product{q, wq, s, ws, bias, y, row, ldw, ldy, T, O, I, bias_dtype, y_dtype, relu, 1};
-    if (nm::gemm_i8_few_fused(T, I) && nm::gemm_i8_few_takes(T, O)) return launched(fn, nm::launch_gemm_i8_few(product, x, ldx, x_dtype, st));
+    if (nm::gemm_i8_few_fused(T, I)) return launched(fn, nm::launch_gemm_i8_few(product, x, ldx, x_dtype, st));
     hipError_t e = nm::launch_quant_i8(x_dtype, x, T, I, ldx, q, row, s, st);
     if (e == hipSuccess) e = nm::launch_gemm_i8(product, st);
     return launched(fn, e);

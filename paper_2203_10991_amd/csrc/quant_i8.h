@@ -38,9 +38,14 @@ template <int DT> __device__ __forceinline__ void load8(const void *p, int64_t a
             const quad_t a = *(const any *)from, b = *(const any *)(from + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[4 + i] = __uint_as_float(b[i]); }
+        } else if (left > 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = from[min((int64_t)i, left - 1)];  // (no branches: all on their way at once)
+#pragma unroll
+            for (int i = 1; i < 8; ++i) v[i] = i < left ? v[i] : 0.f;
         } else
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < left ? from[i] : 0.f;
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
     } else {
         typedef quad_t any __attribute__((aligned(2)));
         const uint16_t *from = (const uint16_t *)p + at;
@@ -48,9 +53,15 @@ template <int DT> __device__ __forceinline__ void load8(const void *p, int64_t a
             const quad_t a = *(const any *)from;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(i & 1 ? a[i / 2] & 0xffff0000u : a[i / 2] << 16);
+        } else if (left > 0) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = from[min((int64_t)i, left - 1)];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < left ? __uint_as_float(w[i] << 16) : 0.f;
         } else
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < left ? __uint_as_float((uint32_t)from[i] << 16) : 0.f;
+            for (int i = 0; i < 8; ++i) v[i] = 0.f;
     }
 }
 

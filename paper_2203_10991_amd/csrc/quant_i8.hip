@@ -15,13 +15,13 @@ namespace nm {
 namespace {
 
 // ---- rows: T threads to a row, T * 8 elements at a time; up to KEEP of them stay in registers between the two passes
-template <int T> constexpr int rows_wg = T > 256 ? T : 256;
+constexpr int ROWS_WG = 256;
 template <int DT, int T, int KEEP>
-__global__ __launch_bounds__(rows_wg<T>) void quant_rows_kernel(const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale)
+__global__ __launch_bounds__(ROWS_WG) void quant_rows_kernel(const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale)
 {
-    __shared__ uint32_t tops[rows_wg<T> / T][T / 64];
+    __shared__ uint32_t tops[ROWS_WG / T][T / 64];
     const int lane = threadIdx.x % T, mine = threadIdx.x / T;
-    const int64_t r = (int64_t)blockIdx.x * (rows_wg<T> / T) + mine;
+    const int64_t r = (int64_t)blockIdx.x * (ROWS_WG / T) + mine;
     const bool there = r < R;
     float v[KEEP][8];
     uint32_t top = 0;
@@ -66,32 +66,34 @@ __global__ __launch_bounds__(rows_wg<T>) void quant_rows_kernel(const void *x, i
     }
 }
 
-// ---- columns, transposed.  First the largest magnitudes of a slab of rows for eight columns a thread
+// ---- columns, transposed.  First the largest magnitudes of a slab of rows for 64 columns, eight threads side by side to a row
 constexpr int TILE = 64;         // rows and columns of a tile that is turned
 template <int DT>
 __global__ __launch_bounds__(256) void column_top_kernel(const void *x, int64_t R, int64_t C, int64_t ld, uint32_t *part, int64_t rows_per_slab)
 {
-    const int64_t c = ((int64_t)blockIdx.x * 32 + threadIdx.x % 32) * 8;
+    constexpr int H = 256 / 8;
+    const int across = threadIdx.x % 8, down = threadIdx.x / 8;
+    const int64_t c0 = (int64_t)blockIdx.x * TILE, c = c0 + across * 8;
     const int64_t from = (int64_t)blockIdx.y * rows_per_slab, to = min(from + rows_per_slab, R);
     uint32_t top[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (c < C)
 #pragma unroll 4
-        for (int64_t r = from + threadIdx.x / 32; r < to; r += 8) {
+        for (int64_t r = from + down; r < to; r += H) {
             float v[8];
             load8<DT>(x, r * ld + c, C - c, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top[i] = max(top[i], __float_as_uint(v[i]) & 0x7fffffffu);
         }
-    __shared__ uint32_t all[8][32][8];
+    __shared__ uint32_t all[H][TILE];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) all[threadIdx.x / 32][threadIdx.x % 32][i] = top[i];
+    for (int i = 0; i < 8; ++i) all[down][across * 8 + i] = top[i];
     __syncthreads();
     const int col = threadIdx.x;
+    if (col >= TILE || c0 + col >= C) return;
     uint32_t m = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) m = max(m, all[w][col / 8][col % 8]);
-    const int64_t at = (int64_t)blockIdx.x * 256 + col;
-    if (at < C) part[(int64_t)blockIdx.y * C + at] = m;
+    for (int h = 0; h < H; ++h) m = max(m, all[h][col]);
+    part[(int64_t)blockIdx.y * C + c0 + col] = m;
 }
 // Then tiles of 64 x 64, turned through LDS in blocks of four columns by four rows: a thread packs four rows of a column into a word
 template <int DT>
@@ -138,16 +140,15 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const void *x, int64_t 
 hipError_t launch_quant_i8(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, hipStream_t st)
 {
     if (R == 0) return hipSuccess;
-#define NM_QUANT_D(DT, T, KEEP) hipLaunchKernelGGL((quant_rows_kernel<DT, T, KEEP>), dim3((unsigned)wgs), dim3(rows_wg<T>), 0, st, x, R, C, ld, q, ldq, scale)
+#define NM_QUANT_D(DT, T, KEEP) hipLaunchKernelGGL((quant_rows_kernel<DT, T, KEEP>), dim3((unsigned)wgs), dim3(ROWS_WG), 0, st, x, R, C, ld, q, ldq, scale)
 #define NM_QUANT(T, KEEP)                                                                       \
     do {                                                                                        \
-        const int64_t wgs = (R + rows_wg<T> / T - 1) / (rows_wg<T> / T);                        \
+        const int64_t wgs = (R + ROWS_WG / T - 1) / (ROWS_WG / T);                        \
         if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;                              \
         if (dt == NM_DT_F32) NM_QUANT_D(NM_DT_F32, T, KEEP); else NM_QUANT_D(NM_DT_BF16, T, KEEP); \
     } while (0)
     if (C <= 512) NM_QUANT(64, 1);
     else if (C <= 1024) NM_QUANT(64, 2);
-    else if (R <= 512 && C > 2048) NM_QUANT(1024, 1);               // (rows that leave CUs idle)
     else if (C <= 4096) NM_QUANT(256, 2);
     else NM_QUANT(256, 4);
 #undef NM_QUANT
@@ -158,7 +159,7 @@ hipError_t launch_quant_i8(int dt, const void *x, int64_t R, int64_t C, int64_t 
 int quant_i8_slabs(int64_t R, int64_t C)
 {
     // slabs of at least 64 rows, about four workgroups to a CU
-    const int64_t panels = (C + 255) / 256;
+    const int64_t panels = (C + TILE - 1) / TILE;
     return (int)std::max<int64_t>(1, std::min<int64_t>({(R + 63) / 64, 1024 / std::max<int64_t>(panels, 1), 64}));
 }
 
@@ -166,11 +167,11 @@ hipError_t launch_quant_i8_t(int dt, const void *x, int64_t R, int64_t C, int64_
 {
     if (C == 0) return hipSuccess;
     const int slabs = quant_i8_slabs(R, C);
-    const int64_t per = (R + slabs - 1) / slabs, panels = (C + 255) / 256, tr = std::max<int64_t>((ldq + TILE - 1) / TILE, 1), tc = (C + TILE - 1) / TILE;
-    if (panels > 0x7fffffff || tr > 0x7fffffff || tc > 65535) return hipErrorInvalidConfiguration;
+    const int64_t per = (R + slabs - 1) / slabs, tr = std::max<int64_t>((ldq + TILE - 1) / TILE, 1), tc = (C + TILE - 1) / TILE;
+    if (tr > 0x7fffffff || tc > 65535) return hipErrorInvalidConfiguration;
 #define NM_TURN(DT)                                                                                                                              \
     do {                                                                                                                                         \
-        hipLaunchKernelGGL((column_top_kernel<DT>), dim3((unsigned)panels, (unsigned)slabs), dim3(256), 0, st, x, R, C, ld, part, per);          \
+        hipLaunchKernelGGL((column_top_kernel<DT>), dim3((unsigned)tc, (unsigned)slabs), dim3(256), 0, st, x, R, C, ld, part, per);              \
         hipLaunchKernelGGL((quant_turn_kernel<DT>), dim3((unsigned)tr, (unsigned)tc), dim3(256), 0, st, x, R, C, ld, q, ldq, scale, part, slabs); \
     } while (0)
     if (dt == NM_DT_F32) NM_TURN(NM_DT_F32); else NM_TURN(NM_DT_BF16);
