@@ -2,12 +2,17 @@
 //     out[n] = scale E[id_n]                     dE[v] = scale * sum over the tokens n with id_n = v of g[n], in the order of n
 // The gradient's tokens are sorted by id, stably, and each row's sum runs over its tokens in their order in binary32: the result does not depend on the
 // launch, and a row that half of the tokens share costs no more than as many rows with a token each.
+// Up to FEW_MOST tokens take one launch (embed_few_kernel), more of them:
 //   sort    up to RANK_MOST tokens, one launch: the rank of a token is the number of tokens whose (id, position) is smaller, which 16 waves count
 //           for 64 tokens from LDS.  Up to MERGE_MOST, two: chunks of 256 tokens sorted that way, and merged.  Beyond, radix passes of at most 9 bits, a counting
 //           launch and a moving one each.  Workgroups behind those of the first launch fill the gradient with zeros meanwhile.
 //   sum     a workgroup takes CHUNK consecutive tokens of the sorted list and a slab of columns.  A row with at most LIGHT tokens is summed, and written, where
 //           it begins; of a longer one each chunk leaves its part in the workspace.
 //   join    those rows: the chunk where a row begins adds up its parts, chunk after chunk.
+// Bound: HBM.  32768 tokens of 120001 x 4096 in bf16: lookup 69 us (441 MB moved, 6.4 TB/s), sort and zeros 145 + 13 (983 MB, 6.8 TB/s), sums 112 (359 MB; the
+// zeros that still wait to be written back are in their way: 69 with zeros that bypass the caches, which take 224 instead of 145), join 14.  16384 tokens of 50001 x
+// 1024 with a binary32 gradient: 14.3, 26 + 5, 18, 5.2: half of that is launches and latency.  Sorts in us: rank 256 / 1024 / 4096 tokens 2.6 / 5.1 / 9.5; chunks and
+// merge 4097 / 16384 / 32768 6.3 + 4 / 6.4 + 5 / 6.4 + 12.8 (4096 by rank and two launches saved beats it); radix 32769 / 65536 2 x 19 / 2 x 23.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -502,6 +507,74 @@ __global__ __launch_bounds__(64 * GROUPS) void embed_join_kernel(Sums s)
     }
 }
 
+// ---- up to FEW_MOST tokens: one launch, without a sorted list.  A workgroup to a token reads all ids; the first token with an id sums the rows of all that have it.  The
+// workgroups behind them fill with zeros the rows that no token has: each marks which of its rows those are.
+// (us, this way / sorted, rank, sum and join kernels: 14 tokens of 3070 x 97 9.3 / 15.3, 199 of 11855 x 135 9.1 / 14.7, 21 of 50605 x 789, 80 MB of gradient, 14.3 / 21.6, 200 of
+// 120001 x 4096 165 / 168; 256 tokens that share one row of 4096 12.5 / 14.5 in bf16, 17.5 / 14.5 in binary32.)
+constexpr int FEW_MOST = 256;
+template <int GT, int OT>
+__global__ __launch_bounds__(FEW_MOST) void embed_few_kernel(Ids ids, int64_t V, int64_t padding, Sums s, int rows_per_wg, int shift)
+{
+    __shared__ uint32_t keys[FEW_MOST], list[FEW_MOST], taken[FILL / (2 * EW)];
+    __shared__ int counts[FEW_MOST / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)blockIdx.x;
+    const uint32_t key = tid < s.N ? key_of(ids, tid, V, padding) : (uint32_t)V;
+    if (n >= s.N) {
+        if (blockIdx.y) return;
+        const int64_t r0 = (int64_t)(n - s.N) * rows_per_wg;
+        const int rows = (int)min(V - r0, (int64_t)rows_per_wg);
+        for (int r = tid; r < rows; r += FEW_MOST) taken[r] = 0;
+        __syncthreads();
+        if ((int64_t)key >= r0 && (int64_t)key < r0 + rows) taken[(int64_t)key - r0] = 1;
+        __syncthreads();
+        const float zeros[EW] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int r = tid >> shift; r < rows; r += FEW_MOST >> shift)
+            if (!taken[r])
+                for (int64_t c = (int64_t)(tid & ((1 << shift) - 1)) * EW; c < s.D; c += (int64_t)EW << shift) store_row<OT>(s.out, (r0 + r) * s.ldo + min(c, s.D - EW), 0, EW, zeros);
+        return;
+    }
+    keys[tid] = key;
+    __syncthreads();
+    const uint32_t row = keys[n];
+    const bool same = row != (uint32_t)V && key == row;
+    const uint64_t in_wave = __ballot(same);
+    if (lane == 0) counts[wave] = __popcll(in_wave);
+    if (__syncthreads_or(same && tid < n) || row == (uint32_t)V) return;         // (an earlier token's, or nobody's)
+    int total = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < FEW_MOST / 64; ++w) { before += w < wave ? counts[w] : 0; total += counts[w]; }
+    if (same) list[before + __popcll(in_wave & ((1ull << lane) - 1))] = (uint32_t)tid;
+    __syncthreads();
+    // a wave takes 512 columns; of more than AHEAD rows a quarter, and the quarters are added in their order
+    constexpr int AHEAD = GT == NM_DT_F32 ? 8 : 16, WAVES = FEW_MOST / 64;       // AHEAD: rows on their way
+    const int64_t c0 = ((int64_t)blockIdx.y * 64 + lane) * EW, c = min(c0, s.D - EW);
+    const int each = total > AHEAD ? (total + WAVES - 1) / WAVES : total, from = min(wave * each, total), to = min(from + each, total);
+    float acc[EW] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k = from; k < to; k += AHEAD) {
+        Raw<GT> v[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (k + j < to) v[j] = load_raw<GT>(s.g, (int64_t)list[k + j] * s.ldg + c);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (k + j < to)
+#pragma unroll
+                for (int e = 0; e < EW; ++e) acc[e] += element(v[j], e);
+    }
+    if (total > AHEAD) {
+        __shared__ float parts[WAVES - 1][EW][64];
+        if (wave > 0)
+#pragma unroll
+            for (int e = 0; e < EW; ++e) parts[wave - 1][e][lane] = acc[e];
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES - 1; ++w)
+#pragma unroll
+            for (int e = 0; e < EW; ++e) acc[e] += parts[w][e][lane];
+    }
+    if (wave == 0 && c0 < s.D) write_sum<OT, false>(s, row, c, (int)(c0 - c), acc);
+}
+
 int bits_of(int64_t v) { int b = 0; while (v >> b) ++b; return b; }
 
 struct GradPlan { int64_t keys, perm, counts, heavy, part, part_ld, bytes; int chunks, per_wg, wgs, passes, digit; };
@@ -562,6 +635,20 @@ hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, c
     const int64_t half = (N * 4 + 255) / 256 * 256;
     for (int i = 0; i < 2; ++i) { keys[i] = (uint32_t *)(w + p.keys + i * half); perm[i] = (uint32_t *)(w + p.perm + i * half); }
     uint32_t *heavy = N ? (uint32_t *)(w + p.heavy) : nullptr;               // (without tokens there is no workspace)
+    if (N > 0 && N <= FEW_MOST && D >= EW && D <= 65535 * 64) {
+        const int rows = (int)std::max<int64_t>(FILL / (D * oe), 1);
+        int shift = 0;
+        while (shift < 8 && ((int64_t)EW << shift) < D) ++shift;
+        const int64_t wgs = N + (accumulate ? 0 : (V + rows - 1) / rows);
+        const Sums s{g, ldg, D, ldo, (int)N, 0, (uint32_t)V, nullptr, nullptr, out, nullptr, 0, nullptr, scale, accumulate};
+#define NM_FEW(GT, OT) hipLaunchKernelGGL((embed_few_kernel<GT, OT>), dim3((unsigned)wgs, (unsigned)((D + 64 * EW - 1) / (64 * EW))), dim3(FEW_MOST), 0, st, tokens, V, padding, s, rows, shift)
+        if (wgs <= 0x7fffffff) {
+            if (g_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_FEW(NM_DT_F32, NM_DT_F32); else NM_FEW(NM_DT_F32, NM_DT_BF16); }
+            else                   { if (out_dt == NM_DT_F32) NM_FEW(NM_DT_BF16, NM_DT_F32); else NM_FEW(NM_DT_BF16, NM_DT_BF16); }
+            return hipGetLastError();
+        }
+#undef NM_FEW
+    }
     int now = 0;
     if (p.passes == 0) {
         const int sort_wgs = (int)((N + 63) / 64);

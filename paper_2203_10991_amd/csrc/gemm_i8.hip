@@ -13,6 +13,9 @@
 // registers, so its buffer is free and the loads of the stage NS later go there; the next stage's first fragments are read under the last two steps.
 // x has zeros from K to the next whole stage, so whatever stands there in w's rows, or in LDS where w's chunks are not loaded, adds nothing: the rows of a layer's
 // call hold them, those of a caller's own codes get them in LDS when the stage has landed.
+//
+// Bound: 32768 x 8192 -> 28672 the matrix pipelines under the power limit, 6.37 to 6.44 ms, 2.4 POP/s (the vendor's product with raw 32-bit results 6.78 ms).
+// 16384 x 1024 -> 4096 in bf16 82 us (vendor's, raw, 97): the eight stages of a tile take 59, what a tile's results take is the rest (their stores alone 8 to 14).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -2,6 +2,8 @@
 //     a = max |x|        q = the integer nearest to x * (127 * (1 / a)), ties to even        scale = a / 127
 // (binary32, one rounding an operation).  A row of zeros, and one whose largest magnitude is below 2^-110 (1 / a would overflow), has zero codes and scale
 // 0; a row with a value that is not finite has zero codes and a NaN for its scale, so that every product with it is NaN.
+// Bound: HBM; rows are read once (they stay in registers up to 8192 columns), columns twice.  Rows of bf16, us: 32768 x 8192 145 (805 MB, 5.6 TB/s), 16384 x 4096 37,
+// 16384 x 1024 13.5, 4096 x 1024 6.0; columns, tops and turn: 28672 x 8192 282 (1.17 GB from and to memory), 4096 x 1024 4.8 + 9.7.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -14,7 +16,8 @@ namespace nm {
 
 namespace {
 
-// ---- rows: T threads to a row, T * 8 elements at a time; up to KEEP of them stay in registers between the two passes
+// ---- rows: T threads to a row, T * 8 elements at a time; up to KEEP of them stay in registers between the two passes.  A wave to a row up to 1024
+// columns, which needs no barrier; the workgroup to a row beyond, where a wave would hold 32 elements a lane and more.
 constexpr int ROWS_WG = 256;
 template <int DT, int T, int KEEP>
 __global__ __launch_bounds__(ROWS_WG) void quant_rows_kernel(const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale)
