@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const void *table, int64_t V
 }
 
 // ---- the gradient's sort
-constexpr int RANK_MOST = 4096, MERGE_MOST = 32768;
+constexpr int FEW_MOST = 512, RANK_MOST = 4096, MERGE_MOST = 32768;
 constexpr int RADIX_BITS = 9, RADIX_BINS = 1 << RADIX_BITS, KEYS = 2048;     // keys of a workgroup in a radix pass: KEYS or a multiple
 
 struct Fill { char *at; int64_t rows, row_bytes, stride_bytes; };            // rows that become zeros; rows == 0: none
@@ -511,42 +511,69 @@ __global__ __launch_bounds__(64 * GROUPS) void embed_join_kernel(Sums s)
 // workgroups behind them fill with zeros the rows that no token has: each marks which of its rows those are.
 // (us, this way / sorted, rank, sum and join kernels: 14 tokens of 3070 x 97 9.3 / 15.3, 199 of 11855 x 135 9.1 / 14.7, 21 of 50605 x 789, 80 MB of gradient, 14.3 / 21.6, 200 of
 // 120001 x 4096 165 / 168; 256 tokens that share one row of 4096 12.5 / 14.5 in bf16, 17.5 / 14.5 in binary32.)
-constexpr int FEW_MOST = 256;
-template <int GT, int OT>
-__global__ __launch_bounds__(FEW_MOST) void embed_few_kernel(Ids ids, int64_t V, int64_t padding, Sums s, int rows_per_wg, int shift)
+constexpr int FEW_WG = 256;
+constexpr int FEW_WGS = 2048;    // all at once on the chip: with more than 256 tokens the way to take while its workgroups are no more than these (300 of 5000 x 512
+                                 // 8.3 / 12.9 us; 450 of 56382 x 2161, 17000 workgroups that read all ids each, 172 / 40)
+// PER: ids that a thread looks at, next to each other
+template <int GT, int OT, int PER>
+__global__ __launch_bounds__(FEW_WG) void embed_few_kernel(Ids ids, int64_t V, int64_t padding, Sums s, int rows_per_wg, int shift)
 {
-    __shared__ uint32_t keys[FEW_MOST], list[FEW_MOST], taken[FILL / (2 * EW)];
-    __shared__ int counts[FEW_MOST / 64];
+    constexpr int WAVES = FEW_WG / 64;
+    __shared__ uint32_t list[FEW_WG * PER], taken[FILL / (2 * EW)];
+    __shared__ int counts[WAVES];
+    __shared__ uint32_t wanted;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)blockIdx.x;
-    const uint32_t key = tid < s.N ? key_of(ids, tid, V, padding) : (uint32_t)V;
+    uint32_t key[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int at = tid * PER + j;
+        key[j] = key_of(ids, min(at, s.N - 1), V, padding);
+        if (at >= s.N) key[j] = (uint32_t)V;
+    }
     if (n >= s.N) {
         if (blockIdx.y) return;
         const int64_t r0 = (int64_t)(n - s.N) * rows_per_wg;
         const int rows = (int)min(V - r0, (int64_t)rows_per_wg);
-        for (int r = tid; r < rows; r += FEW_MOST) taken[r] = 0;
+        for (int r = tid; r < rows; r += FEW_WG) taken[r] = 0;
         __syncthreads();
-        if ((int64_t)key >= r0 && (int64_t)key < r0 + rows) taken[(int64_t)key - r0] = 1;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if ((int64_t)key[j] >= r0 && (int64_t)key[j] < r0 + rows) taken[(int64_t)key[j] - r0] = 1;
         __syncthreads();
         const float zeros[EW] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int r = tid >> shift; r < rows; r += FEW_MOST >> shift)
+        for (int r = tid >> shift; r < rows; r += FEW_WG >> shift)
             if (!taken[r])
                 for (int64_t c = (int64_t)(tid & ((1 << shift) - 1)) * EW; c < s.D; c += (int64_t)EW << shift) store_row<OT>(s.out, (r0 + r) * s.ldo + min(c, s.D - EW), 0, EW, zeros);
         return;
     }
-    keys[tid] = key;
-    __syncthreads();
-    const uint32_t row = keys[n];
-    const bool same = row != (uint32_t)V && key == row;
-    const uint64_t in_wave = __ballot(same);
-    if (lane == 0) counts[wave] = __popcll(in_wave);
-    if (__syncthreads_or(same && tid < n) || row == (uint32_t)V) return;         // (an earlier token's, or nobody's)
-    int total = 0, before = 0;
+    if (n / PER == tid)
 #pragma unroll
-    for (int w = 0; w < FEW_MOST / 64; ++w) { before += w < wave ? counts[w] : 0; total += counts[w]; }
-    if (same) list[before + __popcll(in_wave & ((1ull << lane) - 1))] = (uint32_t)tid;
+        for (int j = 0; j < PER; ++j)
+            if (n % PER == j) wanted = key[j];
+    __syncthreads();
+    const uint32_t row = wanted;
+    uint64_t in_wave[PER];
+    int mine = 0, before = 0;
+    bool earlier = false;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const bool same = key[j] == row;
+        in_wave[j] = __ballot(same);
+        mine += __popcll(in_wave[j]);
+        before += __popcll(in_wave[j] & ((1ull << lane) - 1));
+        earlier |= same && tid * PER + j < n;
+    }
+    if (lane == 0) counts[wave] = mine;
+    if (__syncthreads_or(earlier) || row == (uint32_t)V) return;                 // (an earlier token's, or nobody's)
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) { before += w < wave ? counts[w] : 0; total += counts[w]; }
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (key[j] == row) list[before++] = (uint32_t)(tid * PER + j);
     __syncthreads();
     // a wave takes 512 columns; of more than AHEAD rows a quarter, and the quarters are added in their order
-    constexpr int AHEAD = GT == NM_DT_F32 ? 8 : 16, WAVES = FEW_MOST / 64;       // AHEAD: rows on their way
+    constexpr int AHEAD = GT == NM_DT_F32 ? 8 : 16;                          // rows on their way
     const int64_t c0 = ((int64_t)blockIdx.y * 64 + lane) * EW, c = min(c0, s.D - EW);
     const int each = total > AHEAD ? (total + WAVES - 1) / WAVES : total, from = min(wave * each, total), to = min(from + each, total);
     float acc[EW] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -641,12 +668,14 @@ hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, c
         while (shift < 8 && ((int64_t)EW << shift) < D) ++shift;
         const int64_t wgs = N + (accumulate ? 0 : (V + rows - 1) / rows);
         const Sums s{g, ldg, D, ldo, (int)N, 0, (uint32_t)V, nullptr, nullptr, out, nullptr, 0, nullptr, scale, accumulate};
-#define NM_FEW(GT, OT) hipLaunchKernelGGL((embed_few_kernel<GT, OT>), dim3((unsigned)wgs, (unsigned)((D + 64 * EW - 1) / (64 * EW))), dim3(FEW_MOST), 0, st, tokens, V, padding, s, rows, shift)
-        if (wgs <= 0x7fffffff) {
+#define NM_FEW_P(GT, OT, PER) hipLaunchKernelGGL((embed_few_kernel<GT, OT, PER>), dim3((unsigned)wgs, (unsigned)((D + 64 * EW - 1) / (64 * EW))), dim3(FEW_WG), 0, st, tokens, V, padding, s, rows, shift)
+#define NM_FEW(GT, OT) do { if (N <= FEW_WG) NM_FEW_P(GT, OT, 1); else NM_FEW_P(GT, OT, 2); } while (0)
+        if (N <= FEW_WG ? wgs <= 0x7fffffff : wgs + N * ((D - 1) / (64 * EW)) <= FEW_WGS) {
             if (g_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_FEW(NM_DT_F32, NM_DT_F32); else NM_FEW(NM_DT_F32, NM_DT_BF16); }
             else                   { if (out_dt == NM_DT_F32) NM_FEW(NM_DT_BF16, NM_DT_F32); else NM_FEW(NM_DT_BF16, NM_DT_BF16); }
             return hipGetLastError();
         }
+#undef NM_FEW_P
 #undef NM_FEW
     }
     int now = 0;

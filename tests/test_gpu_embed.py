@@ -69,7 +69,7 @@ def test_lookup_of_tokens_outside_and_other_layouts():
     assert bool(torch.isnan(nm.nm_embed(t[:0], ids)).all())
 
 
-GRADS = [(1, 1, 1), (2, 7, 5), (15, 3, 8), (16, 40, 33), (17, 1000, 64), (64, 2, 1024), (65, 300, 100), (200, 1, 64), (255, 300, 8), (256, 40, 600), (256, 9000, 1030), (257, 40, 600), (1000, 50, 520), (4095, 30011, 72), (4096, 77, 40), (4097, 30011, 72), (8192, 500, 136)]
+GRADS = [(1, 1, 1), (2, 7, 5), (15, 3, 8), (16, 40, 33), (17, 1000, 64), (64, 2, 1024), (65, 300, 100), (200, 1, 64), (255, 300, 8), (256, 40, 600), (256, 9000, 1030), (257, 40, 600), (512, 300, 100), (300, 30000, 600), (513, 40, 64), (1000, 50, 520), (4095, 30011, 72), (4096, 77, 40), (4097, 30011, 72), (8192, 500, 136)]
 LARGE = [(8193, 500, 72), (8200, 3, 64), (16384, 40000, 40), (16385, 200, 24), (20000, 70000, 40), (32768, 511, 16), (32769, 511, 16), (33000, 511, 24), (33000, 512, 33), (65536, 300000, 16), (65537, 513, 8), (70001, 300000, 16)]
 
 
@@ -88,7 +88,7 @@ def test_gradient(kind, N, V, D):
     _check(got, want, size, most)
     assert torch.equal(got, nm.nm_embed_grad(gd, idd.long(), V, 0.5))
     names = kernels_of(lambda: nm.nm_embed_grad(gd, idd, V, 0.5))
-    assert any(("embed_few_kernel" if N <= 256 and D >= 8 else "embed_rank_kernel" if N <= 4096 else "embed_merge_kernel" if N <= 32768 else "embed_move_kernel") in k for k in names), names
+    assert any(("embed_few_kernel" if D >= 8 and (N <= 256 or N <= 512 and V * D < 500000) else "embed_rank_kernel" if N <= 4096 else "embed_merge_kernel" if N <= 32768 else "embed_move_kernel") in k for k in names), names
 
 
 @pytest.mark.parametrize("gt", [F32, BF16])
