@@ -33,7 +33,7 @@ def _view(t, left, right, fill):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("R,C", [(1, 1), (3, 7), (5, 8), (70, 33), (4, 512), (9, 513), (300, 1000), (2, 1025), (7, 4096), (3, 4104), (2, 8193), (5, 20001)])
+@pytest.mark.parametrize("R,C", [(1, 1), (3, 7), (5, 8), (70, 33), (4, 512), (9, 513), (300, 1000), (2, 1025), (7, 4096), (3, 4104), (2, 8193), (5, 20001), (200, 2112), (130, 4160), (257, 2080)])
 def test_codes(dtype, R, C):
     import paper_2203_10991_amd as nm
     gen = torch.Generator().manual_seed(R + C)
