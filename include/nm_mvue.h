@@ -446,8 +446,8 @@ size_t nm_linear_i8_workspace(int64_t T, int64_t I);
  * table [V x D], g and out [N x D] (gradient: out [V x D]), row strides ldt, ldg, ldo in elements; ids of id_bits (32 or 64) bits.  Any sizes, strides and
  * bases on their elements' boundary (rows on 16-byte boundaries are read in vectors); a row stride does not count where there is one row.
  * A token outside 0 .. V-1 is a row of NaN in the lookup and counts for nothing in the gradient, nor does the token `padding` (none: -1).
- * A row's sum runs over its tokens in groups by place, each in the order of the tokens, in binary32: the result depends on ids, N and g
- * only.  accumulate = 0 writes every row of the table, 1 the rows of tokens that are there.  N below 2^31 - 65536, V below 2^31 - 1.
+ * A row's sum runs over its tokens in groups by place, each in the order of the tokens, in binary32: the result depends on the arguments
+ * alone.  accumulate = 0 writes every row of the table, 1 the rows of tokens that are there.  N below 2^31 - 65536, V below 2^31 - 1.
  * workspace: nm_embed_grad_workspace(...) bytes.
  */
 int nm_embed(const void *table, int64_t V, int64_t D, int64_t ldt, int table_dtype, const void *ids, int id_bits, int64_t N, float scale, void *out, int64_t ldo,

@@ -91,6 +91,16 @@ __global__ __launch_bounds__(WG) void gemm_i8_few_kernel(FewArg p)
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int ft = 0; ft < FT; ++ft) w_group(ft, k_first + GROUP * g, wv[ft][g]);
+    // scales and bias of the results a thread will store, ahead of time: feature tid % F of the tokens tid / F + o * WG / F
+    constexpr int OUT = TT * 16 * F / WG;
+    const int64_t my_f = min(f0 + tid % F, a.N - 1);
+    const float my_ws = a.ws[my_f];
+    uint32_t my_add = 0;
+    if (a.bias) my_add = a.bias_dt == NM_DT_F32 ? ((const uint32_t *)a.bias)[my_f] : ((const uint16_t *)a.bias)[my_f];
+    float my_xs[OUT];
+    if constexpr (!FUSED)
+#pragma unroll
+        for (int o = 0; o < OUT; ++o) my_xs[o] = a.xs[min(t0 + tid / F + o * (WG / F), a.M - 1)];
     if constexpr (FUSED) {
         for (int t = 0; t < (int)a.M; ++t) {
             auto take = [&](int c, float (&v)[8]) {
@@ -223,18 +233,19 @@ __global__ __launch_bounds__(WG) void gemm_i8_few_kernel(FewArg p)
                 *at += acc[tt][ft];
             }
     __syncthreads();
-    const int tokens = (int)min(a.M - t0, (int64_t)(16 * TT));
-    for (int i = tid; i < TT * 16 * F; i += WG) {
-        const int tt = i / (16 * F), t = i / F % 16, f = i % F;
-        if (16 * tt + t >= tokens || f0 + f >= a.N) continue;
+    if (f0 + tid % F >= a.N) return;
+    const float add = a.bias_dt == NM_DT_F32 ? __uint_as_float(my_add) : __uint_as_float(my_add << 16);
+#pragma unroll
+    for (int o = 0; o < OUT; ++o) {
+        const int token = tid / F + o * (WG / F), f = tid % F;
+        if (t0 + token >= a.M) break;
         int sum = 0;
 #pragma unroll
-        for (int v = 0; v < NW / 2; ++v) sum += sums[v][tt][t][f];
-        const float xs = FUSED ? row_scale[t] : a.xs[t0 + 16 * tt + t];
-        float v = (float)sum * (xs * a.ws[f0 + f]);
-        if (a.bias) v += a.bias_dt == NM_DT_F32 ? ((const float *)a.bias)[f0 + f] : __uint_as_float((uint32_t)((const uint16_t *)a.bias)[f0 + f] << 16);
+        for (int v = 0; v < NW / 2; ++v) sum += sums[v][token / 16][token % 16][f];
+        const float xs = FUSED ? row_scale[token] : my_xs[o];
+        float v = (float)sum * (xs * my_ws) + add;
         if (a.relu) v = v <= 0.f ? 0.f : v;                                      // (a NaN stays one)
-        const int64_t at = (t0 + 16 * tt + t) * a.ldy + f0 + f;
+        const int64_t at = (t0 + token) * a.ldy + f0 + f;
         if (a.y_dt == NM_DT_F32) ((float *)a.y)[at] = v; else ((uint16_t *)a.y)[at] = (uint16_t)pack_bf16_rne(v, v);
     }
 }
