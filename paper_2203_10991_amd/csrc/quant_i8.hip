@@ -3,7 +3,7 @@
 // (binary32, one rounding an operation).  A row of zeros, and one whose largest magnitude is below 2^-110 (1 / a would overflow), has zero codes and scale
 // 0; a row with a value that is not finite has zero codes and a NaN for its scale, so that every product with it is NaN.
 // Bound: HBM; rows are read once (they stay in registers up to 8192 columns), columns twice.  Rows of bf16, us: 32768 x 8192 145 (805 MB, 5.6 TB/s), 16384 x 4096 37,
-// 16384 x 1024 13.5, 4096 x 1024 6.0; columns, tops and turn: 28672 x 8192 243 (1.17 GB from and to memory, 4.8 TB/s), 4096 x 1024 9.0.
+// 16384 x 1024 13.5, 4096 x 1024 6.0; columns, tops and turn: 28672 x 8192 243 (1.17 GB from and to memory, 4.8 TB/s), 4096 x 1024 9.0 back to back, 15 from memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
