@@ -378,7 +378,7 @@ struct Share {
     bool head, tail;             // the first of their rows began earlier, the last one runs on behind the chunk: both longer than LIGHT
 };
 __device__ __forceinline__ uint32_t lane_of(uint32_t v, int k) { return (uint32_t)__builtin_amdgcn_readlane((int)v, k); }
-__device__ __forceinline__ Share share_of(uint32_t before, uint32_t here, int n)
+__device__ __forceinline__ Share share_of(uint32_t before, uint32_t here, int n, uint32_t V)
 {
     Share s{0, n, false, false};
     const uint32_t first = lane_of(here, 0);
@@ -389,6 +389,7 @@ __device__ __forceinline__ Share share_of(uint32_t before, uint32_t here, int n)
         else s.head = true;
     }
     const uint32_t last = lane_of(here, n - 1);
+    if (last >= V) return s;                                                 // (tokens that count for nothing are no row: none to join, nothing behind the chunk to sum)
     const uint64_t runs = __ballot(here == last) >> (n - 1);                 // from the chunk's last place on
     const int behind = (~runs ? __builtin_ctzll(~runs) : 64) - 1;            // places of the last row behind the chunk
     if (n == CHUNK && behind > 0 && !(last == first && after > n - 1 && earlier > 0)) {      // (a row that began earlier is not this chunk's)
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(Sums s)
     if (from - 64 + lane >= 0) before = s.keys[from - 64 + lane];
     if (from + lane < s.N) { here = s.keys[from + lane]; place = s.perm[from + lane]; }
     if (lane_of(here, 0) >= s.V) return;                                     // (tokens that count for nothing, the last of the list)
-    const Share share = share_of(before, here, n);
+    const Share share = share_of(before, here, n, s.V);
     if (share.tail && blockIdx.y == 0 && threadIdx.x == 0) s.heavy[1 + atomicAdd(s.heavy, 1u)] = blockIdx.x;       // (in any order: each row is joined by itself)
     if (c0 >= s.D || share.begin >= share.end) return;
     float acc[EW];

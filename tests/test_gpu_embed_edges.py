@@ -1,0 +1,70 @@
+"""nm_embed, nm_embed_grad and NMEmbedding where memory ends: what lies around a gradient when many tokens count for nothing, tables and gradients at the limits of
+their sizes, rows that share memory."""
+import pytest
+import torch
+
+from gpu_util import DEV, kernels_of
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+GUARD = 3
+
+
+def _around(V, D, dtype, inside):
+    """V rows of `inside` in the middle of a tensor that this test owns, sevens before and behind them"""
+    hold = torch.full((V + 2 * GUARD, D), 7.0, dtype=dtype, device=DEV)
+    hold[GUARD:GUARD + V] = inside
+    return hold, hold[GUARD:GUARD + V]
+
+
+# tokens that count, the kernel that sorts them (or does it all), rows of the table
+SORTS = [(600, "embed_rank_kernel", 3000), (1000, "embed_rank_kernel", 50), (3000, "embed_rank_kernel", 1), (5000, "embed_merge_kernel", 400), (33000, "embed_move_kernel", 600), (100, "embed_few_kernel", 40), (300, "embed_few_kernel", 300)]
+
+
+@pytest.mark.parametrize("D,out", [(64, F32), (64, BF16), (5, F32)])
+@pytest.mark.parametrize("ignored", [1, 47, 48, 49, 50, 64, 65, 113, 1000])
+@pytest.mark.parametrize("counted,kernel,V", SORTS)
+def test_nothing_behind_the_gradient(counted, kernel, V, ignored, D, out):
+    """Tokens that count for nothing stand last in the sorted list.  Where their run begins inside a chunk of 16 places and however long it is, the rows around the
+    gradient keep their bits.  Gradients are small integers: sums are exact."""
+    import paper_2203_10991_amd as nm
+    gen = torch.Generator().manual_seed(counted + ignored)
+    for more in range(16):
+        n = counted + more
+        ids = torch.randint(0, V, (n,), generator=gen)
+        if V > 4:
+            ids[ids == 3] = 4                                                # 3 is the padding token
+            ids[::3] = 1                                                     # a row of many tokens
+            nothing = torch.tensor([3, -1, V, V + 5, -(1 << 31)])[torch.randint(0, 5, (ignored,), generator=gen)]
+        else:
+            nothing = torch.tensor([-1, V])[torch.randint(0, 2, (ignored,), generator=gen)]
+        ids = torch.cat((ids, nothing))[torch.randperm(n + ignored, generator=gen)]
+        g = torch.randint(-2, 3, (len(ids), D), generator=gen).float()
+        ok = (ids >= 0) & (ids < V) & (ids != (3 if V > 4 else -1))
+        want = torch.zeros(V, D, dtype=torch.float64).index_add_(0, ids[ok], g[ok].double())
+        gd, idd = g.to(DEV), ids.to(DEV)
+        for accumulate, start in ((False, float("nan")), (True, 2.0)):
+            hold, into = _around(V, D, out, start)
+            nm.nm_embed_grad(gd, idd, V, padding_idx=3 if V > 4 else None, out=into, accumulate=accumulate)
+            assert bool((hold[:GUARD] == 7).all()) and bool((hold[GUARD + V:] == 7).all()), (n, accumulate)
+            assert torch.equal(into.cpu(), (want + (2 if accumulate else 0)).to(out)), (n, accumulate)
+    if D >= 8 and ignored < 100:
+        names = kernels_of(lambda: nm.nm_embed_grad(gd, idd, V))
+        assert any(kernel in k for k in names), names
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_layer_whose_batches_are_padded(dtype):
+    """A padded batch through the layer: as many real tokens as any, padding behind them"""
+    from paper_2203_10991_amd.autograd import NMEmbedding
+    layer = NMEmbedding(1000, 40, padding_idx=0, device=DEV, dtype=dtype)
+    gen = torch.Generator().manual_seed(9)
+    for real in (13, 700, 703, 2500, 40001):
+        ids = torch.zeros(real + 500, dtype=torch.int64)
+        ids[:real] = torch.randint(1, 1000, (real,), generator=gen)
+        g = torch.randint(-2, 3, (len(ids), 40), generator=gen).float()
+        layer.weight.grad = None
+        layer(ids.to(DEV)).backward(g.to(dtype).to(DEV))
+        want = torch.zeros(1000, 40, dtype=torch.float64).index_add_(0, ids[:real], g[:real].double())
+        assert torch.equal(layer.weight.grad.cpu(), want.to(dtype))
