@@ -832,7 +832,8 @@ def _ids(ids: torch.Tensor, device) -> Tuple[torch.Tensor, int]:
 
 
 def _unit_columns(t: torch.Tensor) -> torch.Tensor:
-    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+    """A matrix as the kernels read it; a copy where columns are apart or rows share memory (autograd's gradient of a sum over rows has row stride 0)."""
+    return t if (t.stride(1) == 1 or t.shape[1] == 1) and (t.stride(0) >= t.shape[1] or t.shape[0] <= 1) else t.contiguous()
 
 
 def _bf16_or_not(dtype: Optional[torch.dtype]):

@@ -63,6 +63,12 @@ int64_t row_stride(const at::Tensor &t)
     if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) return -1;
     return t.size(0) > 1 ? t.stride(0) : std::max(t.size(1), t.stride(0));
 }
+// ... of rows that share no memory (a matrix expanded along its rows has row stride 0), which api.py copies first
+int64_t distinct_rows(const at::Tensor &t)
+{
+    const int64_t ld = row_stride(t);
+    return ld >= 0 && t.size(0) > 1 && ld < t.size(1) ? -1 : ld;
+}
 // ... whose rows the layer calls read as they are
 int64_t layer_rows(const at::Tensor &t)
 {
@@ -292,7 +298,7 @@ PyObject *embed(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (n != 4) return none();
     const at::Tensor *table = gpu_tensor(a[0]), *ids = gpu_tensor(a[1]);
     if (!table || !ids || !is_float(*table) || !PyFloat_Check(a[2]) || ids->device() != table->device() || !on_current_device(*table)) return none();
-    const int64_t ld = row_stride(*table);
+    const int64_t ld = distinct_rows(*table);
     const int bits = id_bits(*ids);
     if (ld < 0 || !bits) return none();
     const at::ScalarType type = a[3] == Py_None ? table->scalar_type() : a[3] == Py_True ? at::kBFloat16 : at::kFloat;
@@ -326,7 +332,7 @@ PyObject *embed_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int bits = id_bits(*ids);
     if (!bits || g->dim() < 1 || g->size(-1) < 1 || g->dim() != ids->dim() + 1 || g->sizes().slice(0, ids->dim()) != ids->sizes()) return none();
     const int64_t N = ids->numel(), D = g->size(-1), V = PyLong_AsLongLong(a[2]), padding = PyLong_AsLongLong(a[4]);
-    const int64_t ld = g->is_contiguous() ? D : g->dim() == 2 ? row_stride(*g) : -1;
+    const int64_t ld = g->is_contiguous() ? D : g->dim() == 2 ? distinct_rows(*g) : -1;
     if (PyErr_Occurred() || V < 0 || ld < 0) return PyErr_Occurred() ? nullptr : none();
     const at::ScalarType type = a[5] == Py_None ? g->scalar_type() : a[5] == Py_True ? at::kBFloat16 : at::kFloat;
     void *st;
@@ -354,7 +360,7 @@ PyObject *quant_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (n != 2) return none();
     const at::Tensor *x = gpu_tensor(a[0]);
     if (!x || !is_float(*x) || !on_current_device(*x)) return none();
-    const int64_t ld = row_stride(*x);
+    const int64_t ld = distinct_rows(*x);
     const bool turned = a[1] == Py_True;
     void *st;
     if (ld < 0) return none();
@@ -393,7 +399,7 @@ PyObject *linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
         return none();
     const int64_t O = w->size(0), I = w->size(1), T = x->numel() / I;
     if (b && (b->dim() != 1 || b->size(0) != O || !is_float(*b) || !b->is_contiguous() || b->device() != x->device())) return none();
-    const int64_t ldx = x->dim() == 2 ? row_stride(*x) : x->is_contiguous() ? I : -1;
+    const int64_t ldx = x->dim() == 2 ? distinct_rows(*x) : x->is_contiguous() ? I : -1;
     // rows of codes on 16-byte boundaries, whose last one can be read to the end of its last 16 bytes
     const int64_t ldw = O > 1 ? w->stride(0) : (I + 15) / 16 * 16;
     const uintptr_t end = (uintptr_t)w->storage().data() + w->storage().nbytes();
