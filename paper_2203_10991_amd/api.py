@@ -933,7 +933,8 @@ def nm_adamw(params, grads, exp_avgs, exp_avg_sqs, step: int, lr: float = 1e-3, 
     (float8_e4m3fn codes, float32 scales) as alloc_adamw_state makes them; that of exp_avg_sqs then stands for its square
     root.  masters: float32 copies of bfloat16 parameters that take the step, None in the place of one without.  grad_scale: a
     factor on the gradients, a number or a float32 tensor of one element on the GPU.  numbers: each tensor's number in the counter of its random words
-    (8-bit states), its place in the list by default."""
+    (8-bit states), its place in the list by default.  All numbers, `step` and `seed` among them, are arguments of the launch: a graph that captures it
+    repeats that step."""
     lib = load()
     params, grads, exp_avgs, exp_avg_sqs = list(params), list(grads), list(exp_avgs), list(exp_avg_sqs)
     masters = None if masters is None else list(masters)

@@ -13,6 +13,8 @@ class NMAdamW(torch.optim.Optimizer):
     master: float32 copies of bfloat16 parameters take the steps; without them a parameter is rounded to nearest after every step, and
     steps below half of its last place are lost.  seed: of the random words of "q8".
     step(grad_scale=...): a factor on the gradients, a number or a float32 tensor on the GPU (unscaling, a clip coefficient).
+
+    A step is not captured in a graph: its number, bias corrections, rates and random words are arguments of the launch, which every replay would repeat.
     """
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, states: str = "f32", master: bool = False,
@@ -39,6 +41,8 @@ class NMAdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def step(self, closure=None, grad_scale=1.0):
+        if torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("NMAdamW.step cannot be captured in a graph: every replay would take the same step number, bias correction and random words")
         loss = None
         if closure is not None:
             with torch.enable_grad():
