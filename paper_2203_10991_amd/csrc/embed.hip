@@ -30,7 +30,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // Tokens: 32 or 64 bits wide, read as words of 32 without a branch (a branch for each load would have it waited for before the next one is sent)
 struct Ids { const uint32_t *at; int words; };
-// the token at n where it lies in 0 .. V - 1, otherwise V
+// the token at n where it lies in 0 .. V - 1, otherwise V (below 2^32)
 __device__ __forceinline__ uint32_t token_at(const Ids &ids, int64_t n, int64_t V)
 {
     const uint32_t lo = ids.at[n * ids.words], hi = ids.at[n * ids.words + ids.words - 1];
@@ -100,8 +100,9 @@ __global__ __launch_bounds__(256) void embed_kernel(const void *table, int64_t V
 {
     const int64_t n = (int64_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
     if (n >= N) return;
-    const int64_t id = token_at(ids, n, V);
-    const bool there = id < V;                                       // (a token outside the table: a row of NaN, nothing is read)
+    const uint32_t lo = ids.at[n * ids.words], hi = ids.at[n * ids.words + ids.words - 1];
+    const int64_t id = ids.words == 2 ? (int64_t)((uint64_t)hi << 32 | lo) : (int32_t)lo;
+    const bool there = id >= 0 && id < V;                            // (a token outside the table: a row of NaN, nothing is read)
     const int64_t step = (int64_t)EW << shift;
     for (int64_t c0 = (int64_t)(threadIdx.x & ((1 << shift) - 1)) * EW; c0 < D; c0 += step) {
         const int64_t c = NARROW ? c0 : min(c0, D - EW);             // (the row's last elements are written twice, with the same values)

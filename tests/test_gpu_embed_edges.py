@@ -68,3 +68,20 @@ def test_layer_whose_batches_are_padded(dtype):
         layer(ids.to(DEV)).backward(g.to(dtype).to(DEV))
         want = torch.zeros(1000, 40, dtype=torch.float64).index_add_(0, ids[:real], g[:real].double())
         assert torch.equal(layer.weight.grad.cpu(), want.to(dtype))
+
+
+def test_lookup_in_a_table_of_more_than_32_bits_of_rows():
+    """A token outside the table gives NaN and a token inside its row where row numbers pass 32 bits"""
+    import paper_2203_10991_amd as nm
+    V, D = (1 << 32) + 5, 8
+    table = torch.empty(V, D, dtype=BF16, device=DEV)
+    rows = torch.tensor([0, 4, 5, (1 << 31) + 1, (1 << 32) - 1, 1 << 32, V - 1], device=DEV)
+    values = torch.randn(len(rows), D, device=DEV).to(BF16)
+    for k in range(len(rows)):
+        table[int(rows[k])] = values[k]
+    outside = torch.tensor([V, -1, 1 << 40, -(1 << 40), (1 << 33) + 4], device=DEV)
+    got = nm.nm_embed(table, torch.cat((rows, outside)))
+    assert torch.equal(got[:len(rows)], values) and bool(torch.isnan(got[len(rows):]).all())
+    got = nm.nm_embed(table, torch.tensor([5, -1, 0], dtype=torch.int32, device=DEV))
+    assert torch.equal(got[0], values[2]) and bool(torch.isnan(got[1]).all()) and torch.equal(got[2], values[0])
+    assert torch.equal(nm.nm_embed(table[:(1 << 32) - 1], rows[:4]), values[:4]) and bool(torch.isnan(nm.nm_embed(table[:(1 << 32) - 1], rows[4:5])).all())
