@@ -416,7 +416,8 @@ int nm_linear_input_grad(const void *g, int64_t ldg, const void *w, int64_t T, i
 /*
  * Products in 8-bit integers with a scale for each token (row of x) and each output channel (row of w):
  *     y [T x O] = act(float(sum_i xq[t][i] wq[o][i]) * (xs[t] * ws[o]) + bias[o])
- * 32-bit integer sums (I from 1 to 131072, which they hold), binary32 behind them, one rounding to y_dtype; act: max(., 0) where relu != 0 (a NaN
+ * 32-bit integer sums (I from 1 to 131072; they hold codes of -127 .. 127, which the quantisers write, and -128 on one side; -128 against -128 up to
+ * I = 131071), binary32 behind them, one rounding to y_dtype; act: max(., 0) where relu != 0 (a NaN
  * stays one).  bias [O] of bias_dtype, NULL = none.  The input gradient of a layer is the same product, of the gradient's rows with the
  * weights' columns (nm_quant_i8_t).
  *
