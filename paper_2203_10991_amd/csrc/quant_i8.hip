@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "nm_internal.h"
+#include "grid_row.h"
 #include "quant_i8.h"
 
 namespace nm {
@@ -24,7 +25,7 @@ __global__ __launch_bounds__(ROWS_WG) void quant_rows_kernel(const void *x, int6
 {
     __shared__ uint32_t tops[ROWS_WG / T][T / 64];
     const int lane = threadIdx.x % T, mine = threadIdx.x / T;
-    const int64_t r = (int64_t)blockIdx.x * (ROWS_WG / T) + mine;
+    const int64_t r = (int64_t)grid_place(blockIdx.x, blockIdx.y) * (ROWS_WG / T) + mine;
     const bool there = r < R;
     float v[KEEP][8];
     uint32_t top = 0;
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(256) void quant_turn_kernel(const void *x, int64_t 
 hipError_t launch_quant_i8(int dt, const void *x, int64_t R, int64_t C, int64_t ld, int8_t *q, int64_t ldq, float *scale, hipStream_t st)
 {
     if (R == 0) return hipSuccess;
-#define NM_QUANT_D(DT, T, KEEP) hipLaunchKernelGGL((quant_rows_kernel<DT, T, KEEP>), dim3((unsigned)wgs), dim3(ROWS_WG), 0, st, x, R, C, ld, q, ldq, scale)
+#define NM_QUANT_D(DT, T, KEEP) hipLaunchKernelGGL((quant_rows_kernel<DT, T, KEEP>), dim3(grid_row(wgs), grid_rows(wgs)), dim3(ROWS_WG), 0, st, x, R, C, ld, q, ldq, scale)
 #define NM_QUANT(T, KEEP)                                                                       \
     do {                                                                                        \
         const int64_t wgs = (R + ROWS_WG / T - 1) / (ROWS_WG / T);                        \
