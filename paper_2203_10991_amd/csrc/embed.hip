@@ -19,6 +19,7 @@
 #include <algorithm>
 
 #include "nm_internal.h"
+#include "grid_row.h"
 #include "gemm_plan.h"           // NM_CUS
 #include "prune_common.h"        // Row, pack_bf16_rne
 
@@ -98,7 +99,7 @@ template <int DT> __device__ __forceinline__ void store_row(void *p, int64_t at,
 template <int TT, int OT, bool NARROW>
 __global__ __launch_bounds__(256) void embed_kernel(const void *table, int64_t V, int64_t D, int64_t ldt, Ids ids, int64_t N, float scale, void *out, int64_t ldo, int shift)
 {
-    const int64_t n = (int64_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
+    const int64_t n = (int64_t)grid_place(blockIdx.x, blockIdx.y) * (256 >> shift) + (threadIdx.x >> shift);
     if (n >= N) return;
     const uint32_t lo = ids.at[n * ids.words], hi = ids.at[n * ids.words + ids.words - 1];
     const int64_t id = ids.words == 2 ? (int64_t)((uint64_t)hi << 32 | lo) : (int32_t)lo;
@@ -408,13 +409,15 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(Sums s)
 {
     const int64_t c0 = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * EW, c = NARROW ? c0 : min(c0, s.D - EW);
     const int skip = (int)(c0 - c);
-    const int from = (int)blockIdx.x * CHUNK, n = min(CHUNK, s.N - from), lane = threadIdx.x & 63;
+    const uint32_t chunk = grid_place(blockIdx.x, blockIdx.z);
+    if (chunk >= (uint32_t)s.chunks) return;
+    const int from = (int)chunk * CHUNK, n = min(CHUNK, s.N - from), lane = threadIdx.x & 63;
     uint32_t before = 0xffffffffu, here = 0xfffffffeu, place = 0;
     if (from - 64 + lane >= 0) before = s.keys[from - 64 + lane];
     if (from + lane < s.N) { here = s.keys[from + lane]; place = s.perm[from + lane]; }
     if (lane_of(here, 0) >= s.V) return;                                     // (tokens that count for nothing, the last of the list)
     const Share share = share_of(before, here, n, s.V);
-    if (share.tail && blockIdx.y == 0 && threadIdx.x == 0) s.heavy[1 + atomicAdd(s.heavy, 1u)] = blockIdx.x;       // (in any order: each row is joined by itself)
+    if (share.tail && blockIdx.y == 0 && threadIdx.x == 0) s.heavy[1 + atomicAdd(s.heavy, 1u)] = chunk;       // (in any order: each row is joined by itself)
     if (c0 >= s.D || share.begin >= share.end) return;
     float acc[EW];
 #pragma unroll
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(Sums s)
         if (row < s.V) {
             if (!head && !tail) write_sum<OT, NARROW>(s, row, c, skip, acc);
             else {
-                float *to_part = s.part + ((int64_t)blockIdx.x * 2 + (head ? 0 : 1)) * s.part_ld + c0;
+                float *to_part = s.part + ((int64_t)chunk * 2 + (head ? 0 : 1)) * s.part_ld + c0;
                 *(float4 *)to_part = make_float4(acc[0], acc[1], acc[2], acc[3]);
                 *(float4 *)(to_part + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
             }
@@ -640,8 +643,8 @@ hipError_t launch_embed(int table_dt, int out_dt, const void *table, int64_t V, 
     if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
 #define NM_EMBED(TT, OT)                                                                                                                                          \
     do {                                                                                                                                                          \
-        if (D < EW) hipLaunchKernelGGL((embed_kernel<TT, OT, true>), dim3((unsigned)wgs), dim3(256), 0, st, table, V, D, ldt, tokens, N, scale, out, ldo, shift);  \
-        else hipLaunchKernelGGL((embed_kernel<TT, OT, false>), dim3((unsigned)wgs), dim3(256), 0, st, table, V, D, ldt, tokens, N, scale, out, ldo, shift);        \
+        if (D < EW) hipLaunchKernelGGL((embed_kernel<TT, OT, true>), dim3(grid_row(wgs), grid_rows(wgs)), dim3(256), 0, st, table, V, D, ldt, tokens, N, scale, out, ldo, shift);  \
+        else hipLaunchKernelGGL((embed_kernel<TT, OT, false>), dim3(grid_row(wgs), grid_rows(wgs)), dim3(256), 0, st, table, V, D, ldt, tokens, N, scale, out, ldo, shift);        \
     } while (0)
     if (table_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_EMBED(NM_DT_F32, NM_DT_F32); else NM_EMBED(NM_DT_F32, NM_DT_BF16); }
     else                       { if (out_dt == NM_DT_F32) NM_EMBED(NM_DT_BF16, NM_DT_F32); else NM_EMBED(NM_DT_BF16, NM_DT_BF16); }
@@ -656,7 +659,7 @@ hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, c
 {
     const int64_t oe = out_dt == NM_DT_F32 ? 4 : 2;
     const Fill fill{(char *)out, accumulate ? 0 : V, D * oe, ldo * oe};
-    const int fill_wgs = accumulate ? 0 : (int)std::min<int64_t>((V * D * oe + FILL - 1) / FILL, 1 << 24);
+    const int fill_wgs = accumulate ? 0 : (int)std::min<int64_t>((V * D * oe + FILL - 1) / FILL, 1 << GRID_ROW_BITS);
     const GradPlan p = plan_grad(std::max<int64_t>(N, 1), V, D);
     const Ids tokens{(const uint32_t *)ids, wide ? 2 : 1};
     char *w = (char *)workspace;
@@ -672,7 +675,7 @@ hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, c
         const Sums s{g, ldg, D, ldo, (int)N, 0, (uint32_t)V, nullptr, nullptr, out, nullptr, 0, nullptr, scale, accumulate};
 #define NM_FEW_P(GT, OT, PER) hipLaunchKernelGGL((embed_few_kernel<GT, OT, PER>), dim3((unsigned)wgs, (unsigned)((D + 64 * EW - 1) / (64 * EW))), dim3(FEW_WG), 0, st, tokens, V, padding, s, rows, shift)
 #define NM_FEW(GT, OT) do { if (N <= FEW_WG) NM_FEW_P(GT, OT, 1); else NM_FEW_P(GT, OT, 2); } while (0)
-        if (N <= FEW_WG ? wgs <= 0x7fffffff : wgs + N * ((D - 1) / (64 * EW)) <= FEW_WGS) {
+        if (N <= FEW_WG ? wgs * FEW_WG < (int64_t)1 << 32 : wgs + N * ((D - 1) / (64 * EW)) <= FEW_WGS) {
             if (g_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_FEW(NM_DT_F32, NM_DT_F32); else NM_FEW(NM_DT_F32, NM_DT_BF16); }
             else                   { if (out_dt == NM_DT_F32) NM_FEW(NM_DT_BF16, NM_DT_F32); else NM_FEW(NM_DT_BF16, NM_DT_BF16); }
             return hipGetLastError();
@@ -706,7 +709,7 @@ hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, c
     const Sums s{g, ldg, D, ldo, (int)N, p.chunks, (uint32_t)V, keys[now], perm[now], out, (float *)(w + p.part), p.part_ld, heavy, scale, accumulate};
     const int64_t columns = (D + EW - 1) / EW;
     const int threads = (int)std::min<int64_t>((columns + 63) / 64 * 64, 256);
-    const dim3 grid((unsigned)p.chunks, (unsigned)((columns + threads - 1) / threads)), join((unsigned)std::min<int64_t>(N / LIGHT + 1, 64), (unsigned)((columns + 63) / 64));
+    const dim3 grid(grid_row(p.chunks), (unsigned)((columns + threads - 1) / threads), grid_rows(p.chunks)), join((unsigned)std::min<int64_t>(N / LIGHT + 1, 64), (unsigned)((columns + 63) / 64));
 #define NM_SUM_N(GT, OT, NARROW)                                                                 \
     do {                                                                                         \
         hipLaunchKernelGGL((embed_sum_kernel<GT, OT, NARROW>), grid, dim3(threads), 0, st, s);   \

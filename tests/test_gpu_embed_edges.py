@@ -85,3 +85,54 @@ def test_lookup_in_a_table_of_more_than_32_bits_of_rows():
     got = nm.nm_embed(table, torch.tensor([5, -1, 0], dtype=torch.int32, device=DEV))
     assert torch.equal(got[0], values[2]) and bool(torch.isnan(got[1]).all()) and torch.equal(got[2], values[0])
     assert torch.equal(nm.nm_embed(table[:(1 << 32) - 1], rows[:4]), values[:4]) and bool(torch.isnan(nm.nm_embed(table[:(1 << 32) - 1], rows[4:5])).all())
+
+
+def test_lookup_of_more_tokens_than_a_grid_has_workgroups():
+    """A workgroup to a token: 2^24 tokens and more are 2^32 threads, which one dimension of a grid does not hold"""
+    import paper_2203_10991_amd as nm
+    N, D = (1 << 24) + 5, 1032
+    table = torch.randn(64, D, device=DEV).to(BF16)
+    ids = (torch.arange(N, device=DEV, dtype=torch.int32) * 7) % 64
+    got = nm.nm_embed(table, ids)
+    for at in (0, 1 << 23, (1 << 24) - 1000, N - 2000):
+        assert torch.equal(got[at:at + 2000], table[ids[at:at + 2000].long()])
+    assert torch.equal(got[:, 0], table[:, 0][ids.long()])
+    del got
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("N,V,D,out_dtype", [(0, 9_000_011, 2056, F32), (3, 9_000_011, 2056, F32), (300, 9_000_011, 2056, F32), (2000, 9_000_011, 2056, F32), (5000, 9_000_011, 2056, F32),
+                                           (5, (1 << 24) + 9, 4104, BF16)])
+def test_gradient_of_a_table_of_more_than_64_gib(N, V, D, out_dtype):
+    """Its zeros are more workgroups of 1024 threads than a grid has, and the last one's rows more of 256"""
+    import paper_2203_10991_amd as nm
+    ids = torch.randint(0, V, (N,), device=DEV)
+    if N:
+        ids[0] = V - 1
+    g = torch.randint(-2, 3, (N, D), device=DEV).float()
+    out = torch.full((V, D), 7.0, dtype=out_dtype, device=DEV)
+    nm.nm_embed_grad(g, ids, V, out=out)
+    uniq, inverse = ids.unique(return_inverse=True)
+    want = torch.zeros(len(uniq), D, device=DEV).index_add_(0, inverse, g)
+    assert torch.equal(out[uniq], want.to(out_dtype))
+    out[uniq] = 0
+    for at in range(0, V, 1_000_000):
+        assert bool((out[at:at + 1_000_000] == 0).all())
+    del out
+    torch.cuda.empty_cache()
+
+
+def test_gradient_of_2_30_tokens():
+    """67 million workgroups of 64 threads sum 16 tokens each"""
+    import paper_2203_10991_amd as nm
+    N, D, V = (1 << 30) + 40, 1, 1000
+    ids = torch.arange(N, device=DEV, dtype=torch.int32)
+    ids %= V
+    g = torch.ones(N, D, dtype=BF16, device=DEV)
+    got = nm.nm_embed_grad(g, ids, V, out_dtype=F32)
+    # a million ones a row: in binary32 a sum of ones is exact
+    want = torch.full((V, D), float(N // V))
+    want[:N % V] += 1
+    assert torch.equal(got.cpu(), want)
+    del ids, g
+    torch.cuda.empty_cache()
