@@ -18,6 +18,7 @@
 #include <stdint.h>
 
 #include "nm_internal.h"
+#include "grid_row.h"
 #include "prune_common.h"        // philox4x32_10_uniform_c123, pack_bf16_rne
 
 namespace nm {
@@ -85,7 +86,7 @@ __device__ __forceinline__ float code_input(float y, float v)
 
 struct AdamwArg {
     AdamwTensor t[ADAMW_MOST];
-    int first[ADAMW_MOST];       // first workgroup of a tensor
+    uint32_t first[ADAMW_MOST];  // first workgroup of a tensor
     int count;
     float b1, c1, b2, c2, rate, grow, eps, keep, scale;
     const float *scale_dev;
@@ -186,15 +187,16 @@ __device__ __forceinline__ void step_block(const AdamwArg &a, const AdamwTensor 
 template <int PT, int GT, bool Q8, bool MASTER>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwArg a)
 {
+    const uint32_t place = grid_place(blockIdx.x, blockIdx.y);
     int k = 0;
     for (int lo = 0, hi = a.count; lo < hi;) {                                   // the last tensor whose first workgroup is not behind this one
         const int mid = (lo + hi) >> 1;
-        if (a.first[mid] <= (int)blockIdx.x) { k = mid; lo = mid + 1; } else hi = mid;
+        if (a.first[mid] <= place) { k = mid; lo = mid + 1; } else hi = mid;
     }
     const AdamwTensor t = a.t[k];
     const float gs = a.scale_dev ? a.scale * *a.scale_dev : a.scale;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t base = ((int64_t)(blockIdx.x - a.first[k]) * 4 + wave) * AB, at = base + 4 * lane;
+    const int64_t base = ((int64_t)(place - a.first[k]) * 4 + wave) * AB, at = base + 4 * lane;
     if (base >= t.n) return;
     Quad x;
     if (t.aligned && base + AB <= t.n) {
@@ -223,12 +225,12 @@ hipError_t launch_adamw(const AdamwTensor *tensors, int count, int param_dt, int
     int64_t wgs = 0;
     for (int k = 0; k < count; ++k) {
         a.t[k] = tensors[k];
-        a.first[k] = (int)wgs;
+        a.first[k] = (uint32_t)wgs;
         wgs += (tensors[k].n + AB * 4 - 1) / (AB * 4);
         if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
     }
     if (!wgs) return hipSuccess;
-#define NM_ADAMW(PT, GT, Q8, MASTER) hipLaunchKernelGGL((adamw_kernel<PT, GT, Q8, MASTER>), dim3((unsigned)wgs), dim3(256), 0, st, a)
+#define NM_ADAMW(PT, GT, Q8, MASTER) hipLaunchKernelGGL((adamw_kernel<PT, GT, Q8, MASTER>), dim3(grid_row(wgs), grid_rows(wgs)), dim3(256), 0, st, a)
 #define NM_ADAMW_S(PT, GT, MASTER) do { if (q8) NM_ADAMW(PT, GT, true, MASTER); else NM_ADAMW(PT, GT, false, MASTER); } while (0)
     if (param_dt == NM_DT_F32) {
         if (grad_dt == NM_DT_F32) NM_ADAMW_S(NM_DT_F32, NM_DT_F32, false); else NM_ADAMW_S(NM_DT_F32, NM_DT_BF16, false);

@@ -27,3 +27,26 @@ def test_a_step_is_not_captured(states):
     assert bool((x == 3).all()) and torch.equal(w, before) and opt.state[w]["step"] == 1
     opt.step()
     assert opt.state[w]["step"] == 2 and bool((w < before).all())
+
+
+def test_a_tensor_of_more_workgroups_than_a_grid_has():
+    """2^34 elements and more are 2^32 threads"""
+    import paper_2203_10991_amd as nm
+    n = (1 << 34) + 1111
+    p, g = torch.zeros(n, dtype=torch.bfloat16, device=DEV), torch.zeros(n, dtype=torch.bfloat16, device=DEV)
+    m, v = (nm.alloc_adamw_state(p, q8=True) for _ in range(2))
+    tail = 3000
+    parts = [slice(0, tail), slice((1 << 33) - 1024, (1 << 33) - 1024 + tail), slice(n - tail, n)]
+    small = torch.randn(tail, device=DEV).to(torch.bfloat16), torch.randn(tail, device=DEV).to(torch.bfloat16)
+    for at in parts:
+        p[at], g[at] = small
+    nm.nm_adamw([p], [g], [m], [v], 1, lr=0.1, seed=3)
+    ps, gs = small[0].clone(), small[1]
+    ms, vs = (nm.alloc_adamw_state(ps) for _ in range(2))
+    nm.nm_adamw([ps], [gs], [ms], [vs], 1, lr=0.1)
+    for at in parts:
+        assert torch.equal(p[at], ps)
+        assert bool((m[0][at].view(torch.uint8) != 0).any())
+    assert bool((p[tail:1 << 20] == 0).all()) and bool((p[n - (1 << 20):n - tail] == 0).all())
+    del p, g, m, v
+    torch.cuda.empty_cache()
