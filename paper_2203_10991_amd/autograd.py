@@ -31,15 +31,15 @@ class NMConfig:
     # sparse MFMA (Sec. 5, 8-bit rows); "bf16x3": float32 tensors, the update GEMM through three bf16 terms per value
     # on the sparse 16-bit path
     precision: str = "native"
-    # the layer's dense products, linear layers only: "native": the tensors' own dtype; "i8": 8-bit integers with a scale for each token and each
-    # channel, x W^T from the rows of x and W, g W from the rows of g and the columns of W (rounded to nearest; dW is not touched by it)
-    dense: str = "native"
     step: int = 0              # iteration counter; advance() once per optimizer step
     # True: the layer that owns this configuration advances `step` itself after every backward pass (the default
     # configuration a layer makes for itself: a drop-in layer then draws fresh samples every `reuse_every`
     # iterations without any call from the training loop).  False: the caller calls advance() once per iteration,
     # e.g. when several layers share one configuration object.
     auto_advance: bool = False
+    # the layer's dense products, linear layers only: "native": the tensors' own dtype; "i8": 8-bit integers with a scale for each token and each
+    # channel, x W^T from the rows of x and W, g W from the rows of g and the columns of W (rounded to nearest; dW is not touched by it)
+    dense: str = "native"
 
     def current_seed(self) -> int:
         return self.seed + self.step // max(1, self.reuse_every)
