@@ -26,6 +26,9 @@ class NMAdamW(torch.optim.Optimizer):
         self.states, self.master, self.seed = states, master, seed
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
 
+    def __getstate__(self):
+        return {**super().__getstate__(), "states": self.states, "master": self.master, "seed": self.seed}      # (torch's names what it has itself)
+
     def _state(self, p: torch.Tensor) -> dict:
         s = self.state[p]
         if not s:

@@ -8,3 +8,24 @@ def test_configuration_by_position():
     cfg = NMConfig("1:2", 1, 2, 3, 4, "q8", 8, True)
     assert (cfg.nm, cfg.mode, cfg.seed, cfg.stream_id, cfg.reuse_every, cfg.precision, cfg.step, cfg.auto_advance) == ("1:2", 1, 2, 3, 4, "q8", 8, True)
     assert cfg.dense == "native" and cfg.current_seed() == 4
+
+
+def test_optimizer_copied_and_pickled():
+    """(a file of this test's own; plain pickle has no way for e4m3 tensors in this torch.)  A copy keeps how the states are held, the masters and the seed beside what torch's own state has"""
+    import copy
+    import io
+
+    from paper_2203_10991_amd.optim import NMAdamW
+    p = torch.nn.Parameter(torch.ones(300, dtype=torch.bfloat16))
+    opt = NMAdamW([p], lr=0.5, states="q8", master=True, seed=7)
+    opt._state(p)
+    file = io.BytesIO()
+    torch.save(opt, file)
+    file.seek(0)
+    for other in (copy.deepcopy(opt), torch.load(file, weights_only=False)):
+        assert (other.states, other.master, other.seed, other.defaults["lr"]) == ("q8", True, 7, 0.5)
+        q, = other.param_groups[0]["params"]
+        assert q is not p and other._state(q).keys() == opt.state[p].keys() and other._state(q)["exp_avg"].dtype == torch.float8_e4m3fn
+        fresh = torch.nn.Parameter(torch.ones(5, dtype=torch.bfloat16))
+        other.add_param_group({"params": [fresh]})
+        assert "master" in other._state(fresh)
