@@ -60,13 +60,14 @@ class NMAdamW(torch.optim.Optimizer):
                 if p.grad.is_sparse:
                     raise TypeError("NMAdamW takes dense gradients")
                 s = self._state(p)
-                s["step"] += 1
                 pair = lambda k: (s[k], s[k + "_scale"]) if k + "_scale" in s else s[k]        # noqa: E731
-                calls.setdefault((s["step"], "master" in s), []).append((p, p.grad, pair("exp_avg"), pair("exp_avg_sq"), s.get("master"), number - 1))
+                calls.setdefault((s["step"] + 1, "master" in s), []).append((p, p.grad, pair("exp_avg"), pair("exp_avg_sq"), s.get("master"), number - 1))
             for (step, master), tensors in calls.items():
                 p, g, m, v, w, numbers = map(list, zip(*tensors))
                 api.nm_adamw(p, g, m, v, step, lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
                              masters=w if master else None, grad_scale=grad_scale, seed=self.seed, numbers=numbers)
+                for t in p:
+                    self.state[t]["step"] = step                  # (once it has been taken: an error leaves the count)
         return loss
 
     def load_state_dict(self, state_dict):

@@ -29,3 +29,17 @@ def test_optimizer_copied_and_pickled():
         fresh = torch.nn.Parameter(torch.ones(5, dtype=torch.bfloat16))
         other.add_param_group({"params": [fresh]})
         assert "master" in other._state(fresh)
+
+
+def test_a_step_that_fails_is_not_counted():
+    import pytest
+
+    from paper_2203_10991_amd.optim import NMAdamW
+    good, bad = torch.nn.Parameter(torch.ones(4)), torch.nn.Parameter(torch.ones(4, dtype=torch.float16))
+    for p in (good, bad):
+        p.grad = torch.ones_like(p)
+        opt = NMAdamW([p])
+        for _ in range(2):
+            with pytest.raises((ValueError, TypeError)):             # not on the GPU, not a type it takes
+                opt.step()
+        assert opt.state[p]["step"] == 0 and bool((p == 1).all())
