@@ -462,7 +462,8 @@ size_t nm_embed_grad_workspace(int64_t N, int64_t V, int64_t D);
  *     g <- g * grad_scale * (grad_scale_dev ? *grad_scale_dev : 1)
  *     m <- beta1 m + (1 - beta1) g      v <- beta2 v + (1 - beta2) g^2
  *     p <- p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * binary32 throughout, root and quotient to a unit in the last place (a v below 2^-126 has the root 0).  tensors: a HOST array of `count` entries, read before the call returns; arrays contiguous, n elements each:
+ * binary32 throughout, root and quotient to a unit in the last place (a denominator below 2^-126, for which eps has to be, counts as 0).
+ * tensors: a HOST array of `count` entries, read before the call returns; arrays contiguous, n elements each:
  *   param, grad    of param_dtype and grad_dtype (NM_F32 or NM_BF16, one for all tensors of a call)
  *   master         binary32 copy of a bf16 parameter that takes the step in its place, the parameter is then its rounding; NULL = none,
  *                  for all tensors of a call

@@ -137,8 +137,14 @@ __device__ __forceinline__ void step_block(const AdamwArg &a, const AdamwTensor 
         x.v[i] = x.v[i] * a.b2 + (g * g) * a.c2;
         // (the root and the quotient to a unit in the last place: correctly rounded they took a quarter of the kernel's instructions)
         r[i] = __builtin_amdgcn_sqrtf(x.v[i]);
-        x.p[i] = x.p[i] * a.keep - (x.m[i] * a.rate) * __builtin_amdgcn_rcpf(r[i] * a.grow + a.eps);
     }
+    // The instruction takes numbers below 2^-126 for zeros, over which a step is infinite where eps is small
+    if (min(min(__float_as_uint(x.v[0]), __float_as_uint(x.v[1])), min(__float_as_uint(x.v[2]), __float_as_uint(x.v[3]))) < 0x800000u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (x.v[i] < 0x1p-126f) r[i] = __builtin_amdgcn_sqrtf(x.v[i] * 0x1p64f) * 0x1p-32f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.p[i] = x.p[i] * a.keep - (x.m[i] * a.rate) * __builtin_amdgcn_rcpf(r[i] * a.grow + a.eps);
     if constexpr (Q8) {
         uint32_t mt = 0, vt = 0;
 #pragma unroll

@@ -50,3 +50,24 @@ def test_a_tensor_of_more_workgroups_than_a_grid_has():
     assert bool((p[tail:1 << 20] == 0).all()) and bool((p[n - (1 << 20):n - tail] == 0).all())
     del p, g, m, v
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [4096, 4099])
+@pytest.mark.parametrize("param", [torch.float32, torch.bfloat16])
+def test_second_moments_below_the_normal_numbers(n, param):
+    """v from 2^-148 to 2^-90, halved exactly by beta2 = 0.5 with a gradient of zero, m near its root, eps = 0: the step is lr m' / (sqrt(v') sqrt(2)) twice over, to a few
+    roundings of binary32 (and half a unit of a bf16 parameter)."""
+    import paper_2203_10991_amd as nm
+    gen = torch.Generator().manual_seed(n)
+    v = torch.exp2(torch.randint(-148, -90, (n,), generator=gen).double()) * (1 + torch.randint(0, 2, (n,), generator=gen))
+    m = (v.sqrt() * torch.randn(n, generator=gen).double()).float()
+    v = v.float()
+    assert bool((v > 0).all()) and int((v < 2.0 ** -126).sum()) > n // 4
+    p0 = torch.randn(n, generator=gen).to(param)
+    p, md, vd = p0.to(DEV), m.to(DEV), v.to(DEV)
+    nm.nm_adamw([p], [torch.zeros(n, device=DEV)], [md], [vd], 1, lr=0.5, betas=(0.5, 0.5), eps=0.0, weight_decay=0.0)
+    assert torch.equal(vd.cpu(), v / 2) and torch.equal(md.cpu(), m / 2)
+    up = 0.5 / 0.5 * (m.double() / 2) / ((v.double() / 2).sqrt() * 2.0 ** 0.5)
+    want = p0.double() - up
+    eps = 2.0 ** -21 + (2.0 ** -8 if param == torch.bfloat16 else 0)
+    assert bool(((p.cpu().double() - want).abs() <= eps * (p0.double().abs() + up.abs())).all())
