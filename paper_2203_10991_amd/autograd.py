@@ -166,11 +166,15 @@ def _one_call(g2: torch.Tensor, h2: torch.Tensor, weight: torch.Tensor, cfg: NMC
             and api.nm_linear_update_workspace(g2.shape[0], g2.shape[1], h2.shape[1], cfg.precision == "q8", bias) > 0)
 
 
+def _dense(cfg: NMConfig) -> str:
+    if cfg.dense not in ("native", "i8"):
+        raise ValueError(f"unknown dense product {cfg.dense!r}")
+    return cfg.dense
+
+
 def _linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor], relu: bool = False, cfg: Optional[NMConfig] = None) -> torch.Tensor:
     """x W^T + b of eq. (1), and the ReLU behind it: the library's product where it takes the call, otherwise the framework's."""
-    if cfg is not None and cfg.dense != "native":
-        if cfg.dense != "i8":
-            raise ValueError(f"unknown dense product {cfg.dense!r}")
+    if cfg is not None and _dense(cfg) == "i8":
         return api.nm_linear_i8(x, *api.nm_quant_i8(weight), bias, relu=relu)
     y = api.own_linear_forward(x, weight, bias, relu)
     if y is None:
@@ -292,6 +296,7 @@ class NMLinearReLU(torch.nn.Linear):
 class _NMConv2dFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, stride, padding, dilation, cfg):
+        _dense(cfg)                                       # (a value that linear layers would refuse; the dense products here are torch's)
         ctx.save_for_backward(x, weight)
         ctx.conv = (stride, padding, dilation)
         ctx.cfg, ctx.has_bias = cfg, bias is not None
@@ -329,7 +334,7 @@ class NMConv2d(torch.nn.Conv2d):
     """torch.nn.Conv2d (groups = 1, zero padding) whose weight gradient comes from the pruned neural gradient.
 
     bf16, odd square kernel, stride 1, 'same' padding, MVUE 2:4: no im2col matrix is built (row-shifted views of the
-    padded activation grid); anything else goes through an explicit im2col matrix."""
+    padded activation grid); anything else goes through an explicit im2col matrix.  The dense products are torch's, also where cfg.dense is "i8"."""
 
     def __init__(self, *args, cfg: Optional[NMConfig] = None, **kw):
         super().__init__(*args, **kw)

@@ -43,3 +43,16 @@ def test_a_step_that_fails_is_not_counted():
             with pytest.raises((ValueError, TypeError)):             # not on the GPU, not a type it takes
                 opt.step()
         assert opt.state[p]["step"] == 0 and bool((p == 1).all())
+
+
+def test_convolution_knows_the_dense_products():
+    """A convolution's dense products are torch's whatever linear layers of the same configuration take; a value that no layer knows is refused, as linear layers do"""
+    import pytest
+
+    from paper_2203_10991_amd.autograd import NMConfig, NMConv2d
+    x = torch.randn(2, 8, 5, 5)
+    layer = NMConv2d(8, 16, 3, padding=1, cfg=NMConfig(dense="i8"))
+    assert torch.equal(layer(x), torch.nn.functional.conv2d(x, layer.weight, layer.bias, padding=1))
+    layer.cfg.dense = "i4"
+    with pytest.raises(ValueError, match="dense"):
+        layer(x)
