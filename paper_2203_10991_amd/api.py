@@ -879,6 +879,7 @@ def nm_embed_grad(g: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float =
     ids, bits = _ids(ids, g.device)
     D, N = g.shape[-1], ids.numel()
     g = _unit_columns(g.reshape(N, D))
+    given = out
     if out is None:
         out = torch.empty((vocab, D), dtype=out_dtype or g.dtype, device=g.device)
     elif tuple(out.shape) != (vocab, D) or out.device != g.device or (out_dtype is not None and out.dtype != out_dtype):
@@ -888,6 +889,8 @@ def nm_embed_grad(g: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float =
     with torch.cuda.device(g.device):
         _check(lib.nm_embed_grad(_ptr(g), _rowmajor(g, "g"), dt, _ptr(ids), bits, N, vocab, D, float(scale), padding, int(accumulate), _ptr(out), _rowmajor(out, "out"),
                                  _dtype_code(out), _ptr(ws), need, _stream(g)))
+    if given is not None and not given.is_inference():
+        torch.autograd.graph.increment_version([given])                      # (a graph that has saved it then says so)
     return out
 
 

@@ -136,3 +136,18 @@ def test_gradient_of_2_30_tokens():
     assert torch.equal(got.cpu(), want)
     del ids, g
     torch.cuda.empty_cache()
+
+
+def test_a_given_gradient_is_known_to_have_changed():
+    """A graph that has saved the tensor that the gradient goes into says so, as after any operation in place"""
+    import paper_2203_10991_amd as nm
+    out, x = torch.ones(5, 8, device=DEV), torch.ones(5, 8, device=DEV, requires_grad=True)
+    loss = (out * x).sum()
+    version = out._version
+    nm.nm_embed_grad(torch.ones(3, 8, device=DEV), torch.arange(3, device=DEV), 5, out=out, accumulate=True)
+    assert out._version > version
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        given = torch.ones(5, 8, device=DEV)
+        assert bool((nm.nm_embed_grad(torch.ones(3, 8, device=DEV), torch.arange(3, device=DEV), 5, out=given, accumulate=True)[:3] == 2).all())
