@@ -367,7 +367,7 @@ hipError_t launch_grid(const ConvShape &cs, const void *x, int64_t margin, int64
     PruneTask b{(const uint16_t *)gy, grid_geom(cs, cs.O), cs.g_channels_last, T / (q8 ? 32 : 16), q8 ? *sg : LayerScale{}, vals, meta, (T + TILE_ROWS - 1) / TILE_ROWS, 0};
     a.blocks = a.rows * ((cs.C + TILE_COLS - 1) / TILE_COLS);
     b.blocks = b.rows * ((cs.O + TILE_COLS - 1) / TILE_COLS);
-    if (a.blocks + b.blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(a.blocks + b.blocks, 256)) return hipErrorInvalidConfiguration;
     // call indices are at most T*O/8 + 1 (approx-MVUE; a quarter block row less otherwise)
     const bool hi0 = (uint64_t)T * (uint64_t)cs.O <= ((uint64_t)1 << 34);
     const dim3 grid((unsigned)(a.blocks + b.blocks));

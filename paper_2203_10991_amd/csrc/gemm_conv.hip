@@ -326,7 +326,7 @@ hipError_t launch_conv_gemm(const ConvShape &cs, bool q8, const ConvGemmPlan &p,
     ShiftArg sh{};
     for (int t = 0; t < 9; ++t) sh.rows[t] = (t / 3 - 1) * Wp + (t % 3 - 1);
     const int64_t wgs = (int64_t)((cs.O + CG_TM - 1) / CG_TM) * tiles_n * slabs;
-    if (wgs > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(wgs, CG_WAVES * 64)) return hipErrorInvalidConfiguration;
 #define NM_CONV(Q8, CB)                                                                                                                       \
     hipLaunchKernelGGL((conv_gemm_kernel<Q8, CB>), dim3((unsigned)wgs), dim3(CG_WAVES * 64), 0, st, (const char *)vals, (const char *)meta, \
                        (const char *)x_full, part, p.T, (int)((n_ss + slabs - 1) / slabs), cs.O, cs.C, tiles_n, margin, sh)

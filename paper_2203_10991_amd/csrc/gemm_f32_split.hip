@@ -367,7 +367,7 @@ hipError_t launch_update_gemm_f32_split(const void *vals, const uint16_t *meta, 
     sa.blocks = (sa.out_rows * (sa.cols / 8) + 255) / 256;
     sb.blocks = (sb.out_rows * (sb.cols / 8) + 255) / 256;
     const int64_t wgs = (int64_t)p.tiles_m * p.tiles_n;
-    if (sa.blocks + sb.blocks > 0x7fffffffll || wgs > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(sa.blocks + sb.blocks, 256) || wgs > 0x7fffffffll) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(split3_kernel, dim3((unsigned)(sa.blocks + sb.blocks)), dim3(256), 0, st, sa, sb);
     const OutTarget tg = splitk_target(p.slabs, dW, lddw, w + l.part, O, I, beta != 0.f);
     const dim3 grid((unsigned)wgs, 1, (unsigned)p.slabs);

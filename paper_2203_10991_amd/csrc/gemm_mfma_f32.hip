@@ -371,7 +371,7 @@ hipError_t launch_update_gemm_f32(const void *vals, const uint16_t *meta, const 
     if (p.slabs > 1) { out = (float *)workspace; ldo = I; slab_stride = O * I; acc_flag = 0; }
     if (p.small) {
         const int64_t wgs = (int64_t)p.tiles_m * p.tiles_n * p.slabs;
-        if (wgs > 0x7fffffffll) return hipErrorInvalidConfiguration;
+        if (!grid_holds(wgs, 1024)) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL(update_gemm_f32_small_kernel, dim3((unsigned)wgs), dim3(1024), 0, st, (const float *)vals, meta, (const float *)h,
                            ldh, out, ldo, slab_stride, T / 16, p.groups_per_slab, O, I, acc_flag, p.tiles_n);
     } else

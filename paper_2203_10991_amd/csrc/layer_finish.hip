@@ -113,7 +113,7 @@ hipError_t launch_finish_linear(const float *part, int slabs, int64_t O, int64_t
     const SlabSum form = slab_sum_form(O * I / 4, slabs);
     const int R = form == SlabSum::shared ? 8 : 1;
     const int64_t dw_blocks = (O * I / 4 + 256 / R - 1) / (256 / R), db_blocks = db ? (O + DB_COLS - 1) / DB_COLS : 0;
-    if (dw_blocks + db_blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(dw_blocks + db_blocks, 256)) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)(dw_blocks + db_blocks));
 #define NM_FINISH(R, CHAINS)                                                                                                                  \
     hipLaunchKernelGGL((finish_linear_kernel<R, CHAINS>), grid, dim3(256), 0, st, part, slabs, O, I, (uint16_t *)dW, alpha, (int)db_blocks, csum, \
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const uint16_t *__restric
 hipError_t launch_pad_rows(const void *h, int64_t rows, int64_t C, int64_t ld, void *out, int64_t out_rows, hipStream_t st)
 {
     const int64_t blocks = (out_rows * (C / 8) + 255) / 256;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)blocks), dim3(256), 0, st, (const uint16_t *)h, rows, C, ld, (uint16_t *)out, out_rows);
     return hipGetLastError();
 }

@@ -18,6 +18,9 @@ struct AlphaArg {
     AlphaArg(float v = 1.0f, const float *a = nullptr, const float *b = nullptr) : value(v), inv_a(a), inv_b(b) {}
 };
 
+// A dimension of a grid holds fewer than 2^32 threads; of a longer launch the runtime takes what is left modulo 2^32, without an error.
+inline bool grid_holds(int64_t workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
+
 hipError_t launch_prune(int dt, int m, int est, const void *g, int64_t T, int64_t O, int64_t ldg, uint64_t seed,
                         uint32_t stream_id, void *vals, uint16_t *meta, void *dense, int64_t ldd, hipStream_t st);
 

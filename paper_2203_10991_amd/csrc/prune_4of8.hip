@@ -193,7 +193,7 @@ hipError_t launch_prune_4of8_approx(int dt, const void *g, int64_t T, int64_t O,
     const int64_t octets = T / 8, threads = octets * O;
     if (threads == 0) return hipSuccess;
     const int64_t blocks = (threads + 255) / 256;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
 #define NM_P48(DT, DENSE)                                                                                              \
     hipLaunchKernelGGL((prune_4of8_approx_kernel<DT, DENSE>), dim3((unsigned)blocks), dim3(256), 0, st, g, octets, O, ldg, \
                        (uint32_t)seed, (uint32_t)(seed >> 32), stream_id, vals, meta32, dense, ldd)

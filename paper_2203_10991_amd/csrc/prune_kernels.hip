@@ -825,7 +825,7 @@ static hipError_t launch_prune_q8_t(const void *g, int64_t T, int64_t O, int64_t
     constexpr int VEC = 4;
     const int64_t threads = groups * (O / VEC);
     if (threads == 0) return hipSuccess;
-    if ((threads + 255) / 256 > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds((threads + 255) / 256, 256)) return hipErrorInvalidConfiguration;
     if (T * O <= quad_q8_most<EST>()) {
         hipLaunchKernelGGL((prune_compress_q8_quad_kernel<DT, EST>), dim3((unsigned)((groups * O * 2 + 255) / 256)), dim3(256), 0, st,
                            g, groups, O, ldg, (uint32_t)seed, (uint32_t)(seed >> 32), stream_id, scale, scale_dev, vals8, meta32, LayerArg{});
@@ -849,7 +849,7 @@ hipError_t launch_prune_q8_layer(int est, const void *g, int64_t ldg, int64_t T,
 {
     const int64_t groups = (T + 31) / 32, threads = groups * (O / 4), blocks = (threads + 255) / 256;
     if (threads == 0) return hipSuccess;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
 #define NM_Q8L(EST)                                                                                                                     \
     do {                                                                                                                                \
         if (T * O <= quad_q8_most<EST>())                                                                                               \
@@ -996,7 +996,7 @@ static hipError_t launch_prune_t_t(const void *gT, int64_t T, int64_t O, int64_t
     const int64_t groups = T / 16;
     if (groups == 0 || O == 0) return hipSuccess;
     const int64_t blocks = ((groups + 15) / 16) * ((O + 15) / 16);
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((prune_compress_t_kernel<DT, EST>), dim3((unsigned)blocks), dim3(256), 0, st, gT, groups, O, ldt, (uint32_t)seed,
                        (uint32_t)(seed >> 32), stream_id, vals, meta);
     return hipGetLastError();
@@ -1134,7 +1134,7 @@ static hipError_t launch_prune_q8_t_t(const void *gT, int64_t T, int64_t O, int6
     const int64_t groups = T / 32;
     if (groups == 0 || O == 0) return hipSuccess;
     const int64_t blocks = ((groups + 15) / 16) * ((O + 15) / 16);
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((prune_compress_q8_t_kernel<DT, EST>), dim3((unsigned)blocks), dim3(256), 0, st, gT, groups, O, ldt, (uint32_t)seed,
                        (uint32_t)(seed >> 32), stream_id, scale, scale_dev, vals8, meta32);
     return hipGetLastError();
@@ -1274,7 +1274,7 @@ static hipError_t launch_prune_t(const void *g, int64_t T, int64_t O, int64_t ld
     const int64_t groups = T / 16, threads = groups * (O / Row<DT>::VEC);
     if (threads == 0) return hipSuccess;
     const int64_t blocks = (threads + 255) / 256;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     // hi0: every call index (block / 4, or block / 2 for approx-MVUE's two words per block) lies below 2^32
     const bool hi0 = EST != 4 && (uint64_t)(T / M) * (uint64_t)O <= ((uint64_t)1 << (EST == 1 ? 33 : 34));
     const dim3 grid((unsigned)blocks);
@@ -1291,7 +1291,7 @@ static hipError_t launch_prune_t(const void *g, int64_t T, int64_t O, int64_t ld
         }
     if constexpr (DT == NM_DT_BF16 && EST == 0) {
         const dim3 half_grid((unsigned)((2 * threads + 255) / 256));
-        if (M == 2 && (2 * threads + 255) / 256 > 0x7fffffffll) return hipErrorInvalidConfiguration;
+        if (M == 2 && !grid_holds((2 * threads + 255) / 256, 256)) return hipErrorInvalidConfiguration;
         if (M == 2 || T * O <= HALF_MOST) {                       // (M = 4: hi0 holds at these sizes)
             if (threads % 32 && T * O <= CACHED_MOST) hipLaunchKernelGGL((prune_compress_half_kernel<M, EST, true, true>), half_grid, dim3(256), 0, st, NM_ARGS);
             else if (hi0) hipLaunchKernelGGL((prune_compress_half_kernel<M, EST, true>), half_grid, dim3(256), 0, st, NM_ARGS);
@@ -1315,7 +1315,7 @@ hipError_t launch_prune_producer(int dt, int m, int est, const void *u, int64_t 
     const int64_t groups = T / 16, threads = groups * (O / (dt == NM_DT_F32 ? 4 : 8));
     if (threads == 0) return hipSuccess;
     const int64_t blocks = (threads + 255) / 256;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     const ProdArg pa{d, ldd, gout, ldgo};
     const bool plain = threads % 64 && T * O <= PRODUCER_PLAIN_MOST;
 #define NM_PROD(DT, M, EST)                                                                                                             \
@@ -1341,7 +1341,7 @@ hipError_t launch_prune_layer(int m, int est, const void *g, int64_t ldg, const 
 {
     const int64_t groups = (T + 15) / 16, threads = groups * (O / 4), blocks = (threads + 255) / 256;
     if (threads == 0) return hipSuccess;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     const ProdArg pa{act, lda, gout, ldgo};
     const LayerArg la{T, csum};
     const bool cached = threads % 64 && T * O <= CACHED_MOST;
@@ -1387,7 +1387,7 @@ static hipError_t launch_compress_t(const void *d, int64_t T, int64_t O, int64_t
 {
     const int64_t groups = T / 16, threads = groups * (O / Row<DT>::VEC);
     if (threads == 0) return hipSuccess;
-    if ((threads + 255) / 256 > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds((threads + 255) / 256, 256)) return hipErrorInvalidConfiguration;
     if (threads % 64 == 0)          // whole waves: streaming loads, stores of whole lines through the per-wave transpose
         hipLaunchKernelGGL((compress_kernel<DT, M, true>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st,
                            d, groups, O, ld, vals, meta, bad);

@@ -230,7 +230,7 @@ hipError_t launch_cast_e4m3_layer(const void *h, int64_t R, int64_t C, int64_t l
                                   hipStream_t st)
 {
     const int64_t blocks = (out_rows * (C / 16) + 255) / 256;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((cast_e4m3_kernel<NM_DT_BF16, true>), dim3((unsigned)blocks), dim3(256), 0, st, h, R, C, ld, (const float *)nullptr, ls, h8, ld8, out_rows);
     return hipGetLastError();
 }
@@ -241,7 +241,7 @@ hipError_t launch_cast_e4m3(int dt, const void *h, int64_t R, int64_t C, int64_t
     const int64_t threads = R * (C / 16);
     if (threads == 0) return hipSuccess;
     const int64_t blocks = (threads + 255) / 256;
-    if (blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(blocks, 256)) return hipErrorInvalidConfiguration;
     if (dt == NM_DT_F32) hipLaunchKernelGGL(cast_e4m3_kernel<NM_DT_F32>, dim3((unsigned)blocks), dim3(256), 0, st, h, R, C, ld, rec, LayerScale{}, h8, ld8, R);
     else hipLaunchKernelGGL(cast_e4m3_kernel<NM_DT_BF16>, dim3((unsigned)blocks), dim3(256), 0, st, h, R, C, ld, rec, LayerScale{}, h8, ld8, R);
     return hipGetLastError();

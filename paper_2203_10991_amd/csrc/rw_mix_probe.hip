@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void rw_mix_probe_kernel(const uint4 *__restri
 hipError_t launch_rw_mix_probe(const void *src, void *dst, int64_t n_blocks, hipStream_t st)
 {
     if (n_blocks == 0) return hipSuccess;
-    if (n_blocks > 0x7fffffffll) return hipErrorInvalidConfiguration;
+    if (!grid_holds(n_blocks, 256)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(rw_mix_probe_kernel, dim3((unsigned)n_blocks), dim3(256), 0, st, (const uint4 *)src, (uint4 *)dst, n_blocks);
     return hipGetLastError();
 }
