@@ -11,8 +11,8 @@
 // vanished r would be a step of any size.  What is not finite gets the NaN code and stays out of the block's scale.
 //
 // Bound: HBM.  A wave takes 256 elements, each lane a quad of them with one load per array, and all tensors of up to ADAMW_MOST share a launch.  A transformer
-// block of width 768 with binary32 states and masters: 213 MB in 36 us (5.9 TB/s; a copy reaches 4.75); of width 4096 with 8-bit states: 2.43 GB in 410 to 470 us
-// (5.2 to 5.9 TB/s); of width 768 with 8-bit states and bf16 gradients 71 MB in 18 us, where the launch's fill and the arithmetic (Philox, rounding) show.
+// block of width 768 with binary32 states and masters: 213 MB in 36 us (5.9 TB/s; a copy reaches 4.75); of width 4096 with 8-bit states: 2.43 GB in 410 to 480 us
+// (5.0 to 5.9 TB/s); of width 768 with 8-bit states and bf16 gradients 71 MB in 17 to 19 us, where the launch's fill and the arithmetic (Philox, rounding) show.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

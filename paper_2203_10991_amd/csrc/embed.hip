@@ -1,14 +1,15 @@
 // Embedding: rows of a table by token, scaled, and the table's gradient.
-//     out[n] = scale E[id_n]                     dE[v] = scale * sum over the tokens n with id_n = v of g[n], in the order of n
-// The gradient's tokens are sorted by id, stably, and each row's sum runs over its tokens in their order in binary32: the result does not depend on the
-// launch, and a row that half of the tokens share costs no more than as many rows with a token each.
+//     out[n] = scale E[id_n]                     dE[v] = scale * sum over the tokens n with id_n = v of g[n]
+// The gradient's tokens are sorted by id, stably.  A row's sum is binary32, in an order that follows from the arguments alone, so that the same call gives the same bits: up to
+// LIGHT tokens in their order, more of them in parts by place in the sorted list, each in order, and the parts in 16 groups, each in order (the one-launch form: quarters of
+// the row's tokens, each in order).
 // Up to FEW_MOST tokens take one launch (embed_few_kernel), more of them:
 //   sort    up to RANK_MOST tokens, one launch: the rank of a token is the number of tokens whose (id, position) is smaller, which 16 waves count
 //           for 64 tokens from LDS.  Up to MERGE_MOST, two: chunks of 256 tokens sorted that way, and merged.  Beyond, radix passes of at most 9 bits, a counting
 //           launch and a moving one each.  Workgroups behind those of the first launch fill the gradient with zeros meanwhile.
 //   sum     a workgroup takes CHUNK consecutive tokens of the sorted list and a slab of columns.  A row with at most LIGHT tokens is summed, and written, where
 //           it begins; of a longer one each chunk leaves its part in the workspace.
-//   join    those rows: the chunk where a row begins adds up its parts, chunk after chunk.
+//   join    those rows: a workgroup for 512 columns of a row adds up its parts in 16 groups.  Tokens that count for nothing stand last and are no row.
 // Bound: HBM.  32768 tokens of 120001 x 4096 in bf16: lookup 69 us (441 MB moved, 6.4 TB/s), sort and zeros 145 + 13 (983 MB, 6.8 TB/s), sums 112 (359 MB; the
 // zeros that still wait to be written back are in their way: 69 with zeros that bypass the caches, which take 224 instead of 145), join 14.  16384 tokens of 50001 x
 // 1024 with a binary32 gradient: 14.3, 26 + 5, 18, 5.2: half of that is launches and latency.  Sorts in us: rank 256 / 1024 / 4096 tokens 2.6 / 5.1 / 9.5; chunks and

@@ -1,6 +1,7 @@
 // Product of 8-bit integers with a scale for each token and each output channel (T = M tokens, N outputs, K inputs):
 //     y[M x N] = act((x[M x K] w[N x K]^T) xs[M] ws[N] + bias[N])
-// 32-bit integer sums (K at most 131072: 127 * 128 K stays below 2^31; -128 against -128 does up to K = 131071), then one conversion, the product with xs ws, bias and ReLU in binary32, one rounding.
+// 32-bit integer sums (K at most 131072: 127 * 128 K stays below 2^31; -128 against -128 does up to K = 131071), then one conversion, the product with xs ws, bias
+// and ReLU in binary32, one rounding.
 //
 // Instruction: v_mfma_i32_32x32x32_i8, both operands with 32 rows (lane % 32) and 16 consecutive bytes of the reduction axis to a lane.  Which of the 32 steps
 // of the axis those are does not matter, since both operands hold the same ones.  bf16 results: the weights are the first operand, so a lane holds four
