@@ -358,6 +358,7 @@ struct Sums {
     uint32_t *heavy;             // how many rows have more than LIGHT tokens, and the chunks where they begin
     float scale;
     int accumulate;
+    int later;                   // the columns behind those of another launch, which has counted the long rows
 };
 
 template <int OT, bool NARROW> __device__ __forceinline__ void write_sum(const Sums &s, uint32_t row, int64_t c, int skip, float (&v)[EW])
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(Sums s)
     if (from + lane < s.N) { here = s.keys[from + lane]; place = s.perm[from + lane]; }
     if (lane_of(here, 0) >= s.V) return;                                     // (tokens that count for nothing, the last of the list)
     const Share share = share_of(before, here, n, s.V);
-    if (share.tail && blockIdx.y == 0 && threadIdx.x == 0) s.heavy[1 + atomicAdd(s.heavy, 1u)] = chunk;       // (in any order: each row is joined by itself)
+    if (share.tail && !s.later && blockIdx.y == 0 && threadIdx.x == 0) s.heavy[1 + atomicAdd(s.heavy, 1u)] = chunk;       // (in any order: each row is joined by itself)
     if (c0 >= s.D || share.begin >= share.end) return;
     float acc[EW];
 #pragma unroll
@@ -458,6 +459,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(Sums s)
 
 // The rows with more than LIGHT tokens: their parts in 16 groups, each chunk after chunk, and the groups in order
 constexpr int GROUPS = 16;
+constexpr int64_t SLAB = 65535ll * 64 * EW;  // columns of a launch: a workgroup of the join takes 64 EW of them
 template <int OT, bool NARROW>
 __global__ __launch_bounds__(64 * GROUPS) void embed_join_kernel(Sums s)
 {
@@ -673,7 +675,7 @@ hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, c
         int shift = 0;
         while (shift < 8 && ((int64_t)EW << shift) < D) ++shift;
         const int64_t wgs = N + (accumulate ? 0 : (V + rows - 1) / rows);
-        const Sums s{g, ldg, D, ldo, (int)N, 0, (uint32_t)V, nullptr, nullptr, out, nullptr, 0, nullptr, scale, accumulate};
+        const Sums s{g, ldg, D, ldo, (int)N, 0, (uint32_t)V, nullptr, nullptr, out, nullptr, 0, nullptr, scale, accumulate, 0};
 #define NM_FEW_P(GT, OT, PER) hipLaunchKernelGGL((embed_few_kernel<GT, OT, PER>), dim3((unsigned)wgs, (unsigned)((D + 64 * EW - 1) / (64 * EW))), dim3(FEW_WG), 0, st, tokens, V, padding, s, rows, shift)
 #define NM_FEW(GT, OT) do { if (N <= FEW_WG) NM_FEW_P(GT, OT, 1); else NM_FEW_P(GT, OT, 2); } while (0)
         if (N <= FEW_WG ? wgs * FEW_WG < (int64_t)1 << 32 : wgs + N * ((D - 1) / (64 * EW)) <= FEW_WGS) {
@@ -707,18 +709,23 @@ hipError_t launch_embed_grad(int g_dt, int out_dt, const void *g, int64_t ldg, c
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (N == 0) return hipSuccess;
-    const Sums s{g, ldg, D, ldo, (int)N, p.chunks, (uint32_t)V, keys[now], perm[now], out, (float *)(w + p.part), p.part_ld, heavy, scale, accumulate};
-    const int64_t columns = (D + EW - 1) / EW;
-    const int threads = (int)std::min<int64_t>((columns + 63) / 64 * 64, 256);
-    const dim3 grid(grid_row(p.chunks), (unsigned)((columns + threads - 1) / threads), grid_rows(p.chunks)), join((unsigned)std::min<int64_t>(N / LIGHT + 1, 64), (unsigned)((columns + 63) / 64));
 #define NM_SUM_N(GT, OT, NARROW)                                                                 \
     do {                                                                                         \
         hipLaunchKernelGGL((embed_sum_kernel<GT, OT, NARROW>), grid, dim3(threads), 0, st, s);   \
         hipLaunchKernelGGL((embed_join_kernel<OT, NARROW>), join, dim3(64 * GROUPS), 0, st, s);  \
     } while (0)
-#define NM_SUM(GT, OT) do { if (D < EW) NM_SUM_N(GT, OT, true); else NM_SUM_N(GT, OT, false); } while (0)
-    if (g_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_SUM(NM_DT_F32, NM_DT_F32); else NM_SUM(NM_DT_F32, NM_DT_BF16); }
-    else                   { if (out_dt == NM_DT_F32) NM_SUM(NM_DT_BF16, NM_DT_F32); else NM_SUM(NM_DT_BF16, NM_DT_BF16); }
+#define NM_SUM(GT, OT) do { if (width < EW) NM_SUM_N(GT, OT, true); else NM_SUM_N(GT, OT, false); } while (0)
+    // (a dimension of a grid but the first has at most 65535 workgroups: wider rows in slabs)
+    const int64_t ge = g_dt == NM_DT_F32 ? 4 : 2;
+    for (int64_t from = 0; from < D; from += SLAB) {
+        const int64_t width = std::min(D - from, SLAB), columns = (width + EW - 1) / EW;
+        const Sums s{(const char *)g + from * ge, ldg, width, ldo, (int)N, p.chunks, (uint32_t)V, keys[now], perm[now], (char *)out + from * oe, (float *)(w + p.part) + from, p.part_ld, heavy,
+                     scale, accumulate, from > 0};
+        const int threads = (int)std::min<int64_t>((columns + 63) / 64 * 64, 256);
+        const dim3 grid(grid_row(p.chunks), (unsigned)((columns + threads - 1) / threads), grid_rows(p.chunks)), join((unsigned)std::min<int64_t>(N / LIGHT + 1, 64), (unsigned)((columns + 63) / 64));
+        if (g_dt == NM_DT_F32) { if (out_dt == NM_DT_F32) NM_SUM(NM_DT_F32, NM_DT_F32); else NM_SUM(NM_DT_F32, NM_DT_BF16); }
+        else                   { if (out_dt == NM_DT_F32) NM_SUM(NM_DT_BF16, NM_DT_F32); else NM_SUM(NM_DT_BF16, NM_DT_BF16); }
+    }
 #undef NM_SUM
 #undef NM_SUM_N
     return hipGetLastError();

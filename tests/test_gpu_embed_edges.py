@@ -151,3 +151,25 @@ def test_a_given_gradient_is_known_to_have_changed():
     with torch.inference_mode():
         given = torch.ones(5, 8, device=DEV)
         assert bool((nm.nm_embed_grad(torch.ones(3, 8, device=DEV), torch.arange(3, device=DEV), 5, out=given, accumulate=True)[:3] == 2).all())
+
+
+@pytest.mark.parametrize("D", [65535 * 512 + 5, 65535 * 512 + 1000])
+def test_gradient_of_rows_of_more_columns_than_a_launch_takes(D):
+    """Rows in slabs of 65535 x 512 columns: a row of 49 tokens and more in parts, one of few, one of none, the rows behind them untouched"""
+    import paper_2203_10991_amd as nm
+    N, V = 60, 3
+    ids = torch.zeros(N, dtype=torch.int64, device=DEV)
+    ids[::9] = 2
+    g = torch.ones(N, D, dtype=BF16, device=DEV)
+    g[4, -7:] = 3
+    g[9, -2:] = 5
+    hold, into = _around(V, D, F32, 1.0)
+    for accumulate in (False, True):
+        nm.nm_embed_grad(g, ids, V, out=into, accumulate=accumulate)
+        want = torch.tensor([53.0, 0.0, 7.0], device=DEV)[:, None].expand(V, D).clone()
+        want[0, -7:] += 2
+        want[2, -2:] += 4
+        assert torch.equal(into, want * (2 if accumulate else 1))
+        assert bool((hold[:GUARD] == 7).all()) and bool((hold[GUARD + V:] == 7).all())
+    del g, hold, into, want
+    torch.cuda.empty_cache()
