@@ -458,6 +458,55 @@ int nm_embed_grad(const void *g, int64_t ldg, int g_dtype, const void *ids, int 
 size_t nm_embed_grad_workspace(int64_t N, int64_t V, int64_t D);
 
 /*
+ * Layer norm of the rows of x [R x C]:  y = (x - mean) rstd w + b, rstd = 1 / sqrt(variance + eps), in binary32, rounded once; and its gradients
+ *     with h = (x - mean) rstd, u = g w:   dx = rstd (u - mean(u) - h mean(u h)),   dw = sum over the rows of g h,   db = sum of g
+ * x, y, g, dx of x_dtype, w, b, dw, db of w_dtype; w NULL: ones, b NULL: zeros, dw or db NULL: not wanted.  mean and rstd (binary32 [R]): what the forward pass
+ * leaves (each may be NULL there) and the gradients read.  C from 1 to 32768; any row strides and bases on their elements' boundary (a row stride does not count where
+ * there is one row).  Sums run in an order that follows from the sizes alone.  R = 0: dw and db become zeros.  workspace: nm_layer_norm_grad_workspace(R, C) bytes,
+ * needed where dw or db is wanted.
+ */
+int nm_layer_norm(const void *x, int64_t ldx, int x_dtype, const void *w, const void *b, int w_dtype, int64_t R, int64_t C, float eps, void *y, int64_t ldy, float *mean, float *rstd,
+                  void *hip_stream);
+int nm_layer_norm_grad(const void *g, int64_t ldg, const void *x, int64_t ldx, int x_dtype, const void *w, int w_dtype, const float *mean, const float *rstd, int64_t R, int64_t C,
+                       void *dx, int64_t lddx, void *dw, void *db, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t nm_layer_norm_grad_workspace(int64_t R, int64_t C);
+
+/*
+ * Heads [B][T][H][D] of a batch: a base and the strides, in elements, of a sequence, a token and a head; a head's elements lie side by side.  A stride does not count
+ * where its size is 1.  Inputs may have strides of 0; outputs have no element twice.
+ */
+typedef struct { void *data; int64_t batch, token, head; } nm_heads;
+
+/*
+ * Rotary positions: of each head's first `part` elements (even), the pairs (x[2j], x[2j + 1]) where interleaved, otherwise (x[j], x[j + part / 2]), become
+ *     scale * (a cos t - b sin t),  scale * (a sin t + b cos t),      t = position * freqs[j]
+ * and the elements behind them stay.  inverse: t negated, which is the gradient with respect to x of what the call without it makes.  The angle is formed in
+ * binary64, the rest in binary32.  freqs: binary64 [part / 2], radians to a position.  positions: of position_bits (32 or 64) bits, those of sequence b from
+ * b * position_stride on (0: the same for all); NULL: 0 .. T - 1.  D from 2 to 1024; bases and strides on their elements' boundary; y may be x itself.
+ */
+int nm_rotary(const nm_heads *x, const nm_heads *y, int dtype, int64_t B, int64_t T, int64_t H, int64_t D, int64_t part, const double *freqs, const void *positions, int position_bits,
+              int64_t position_stride, int interleaved, float scale, int inverse, void *hip_stream);
+
+/*
+ * Attention: o = softmax(scale q k^T) v for each head over the keys that a query sees, and its gradients.  q, o, g, dq [B][Tq][Hq][D], k, v, dk, dv [B][Tk][Hk][D];
+ * Hq is a multiple of Hk, and Hq / Hk heads of queries in a row share a head of keys and values.  D a multiple of 8 up to 128, bases and strides multiples of 16 bytes.
+ * q_lens, k_lens (device, int32 [B], NULL: all): queries and keys of each sequence, from the front of the tensors; what lies behind them does not count, whatever it
+ * holds, and o, dq, dk and dv are zeros there.  (Lengths beyond the tensors count as the tensors'.)  causal: query i of n sees the keys j <= i + m - n of m, so that the last query
+ * sees the last key.  A query that sees no key: o = 0, lse = -infinity, and it adds nothing to any gradient.  What a query does not see of its own sequence has to be finite.
+ * lse: binary32 [B][Hq][Tq], the logarithm of the sum of the exponentials; NULL: not wanted; the gradients need it, and o as the forward pass left it.
+ * scale > 0.  Scores, probabilities and all sums are binary32; with bf16 tensors probabilities (not those of the sum) and their gradients are rounded to bf16 for the
+ * products that follow.  The gradients recompute the probabilities; no sum's order depends on anything but the sizes.
+ * workspaces: nm_attention_workspace(...) and nm_attention_grad_workspace(...) bytes.
+ */
+int nm_attention(const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, float *lse, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype,
+                 int causal, float scale, const int32_t *q_lens, const int32_t *k_lens, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t nm_attention_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype);
+int nm_attention_grad(const nm_heads *g, const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, const float *lse, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq,
+                      int64_t Hk, int64_t D, int dtype, int causal, float scale, const int32_t *q_lens, const int32_t *k_lens, const nm_heads *dq, const nm_heads *dk, const nm_heads *dv,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t nm_attention_grad_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype);
+
+/*
  * One AdamW step over many tensors (decoupled weight decay), one launch for every 48 of them:
  *     g <- g * grad_scale * (grad_scale_dev ? *grad_scale_dev : 1)
  *     m <- beta1 m + (1 - beta1) g      v <- beta2 v + (1 - beta2) g^2

@@ -7,6 +7,7 @@ is missing, or a call returns an error status, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import warnings
 from typing import Optional, Tuple
@@ -120,6 +121,22 @@ def load():
     lib.nm_embed_grad.restype = i32
     lib.nm_embed_grad_workspace.argtypes = [i64, i64, i64]
     lib.nm_embed_grad_workspace.restype = sz
+    lib.nm_layer_norm.argtypes = [vp, i64, i32, vp, vp, i32, i64, i64, f32, vp, i64, vp, vp, vp]
+    lib.nm_layer_norm.restype = i32
+    lib.nm_layer_norm_grad.argtypes = [vp, i64, vp, i64, i32, vp, i32, vp, vp, i64, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.nm_layer_norm_grad.restype = i32
+    lib.nm_layer_norm_grad_workspace.argtypes = [i64, i64]
+    lib.nm_layer_norm_grad_workspace.restype = sz
+    heads = C.POINTER(_Heads)
+    lib.nm_rotary.argtypes = [heads, heads, i32, i64, i64, i64, i64, i64, vp, vp, i32, i64, i32, f32, i32, vp]
+    lib.nm_rotary.restype = i32
+    sizes = [i64] * 6 + [i32]                                                # B, Tq, Tk, Hq, Hk, D, dtype
+    lib.nm_attention.argtypes = [heads] * 4 + [vp, *sizes, i32, f32, vp, vp, vp, sz, vp]
+    lib.nm_attention.restype = i32
+    lib.nm_attention_grad.argtypes = [heads] * 5 + [vp, *sizes, i32, f32, vp, vp, heads, heads, heads, vp, sz, vp]
+    lib.nm_attention_grad.restype = i32
+    for f in (lib.nm_attention_workspace, lib.nm_attention_grad_workspace):
+        f.argtypes, f.restype = sizes, sz
     lib.nm_adamw.argtypes = [vp, i32, i32, i32, i32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, i64, f32, vp, u64, vp]
     lib.nm_adamw.restype = i32
     for f in (lib.mvue_prune_1of2, lib.mvue_prune_2of4, lib.nm_compress, lib.nm_update_gemm, lib.mvue_prune_2of4_q8,
@@ -142,6 +159,10 @@ def load():
     global _native
     _native, _lib = native, lib
     return lib
+
+
+class _Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
 
 
 class _NoNative:
@@ -892,6 +913,211 @@ def nm_embed_grad(g: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float =
     if given is not None and not given.is_inference():
         torch.autograd.graph.increment_version([given])                      # (a graph that has saved it then says so)
     return out
+
+
+# ---- between a block's linear layers: layer norm, rotary positions, attention
+
+def _norm_weights(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], x: torch.Tensor):
+    width = x.shape[-1]
+    for t in (weight, bias):
+        if t is not None and (tuple(t.shape) != (width,) or t.device != x.device):
+            raise ValueError(f"weight and bias of rows of {width} have one element for each, on the tensor's device")
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("weight and bias are of one type")
+    known = weight if weight is not None else bias
+    return None if weight is None else weight.contiguous(), None if bias is None else bias.contiguous(), NM_F32 if known is None else _dtype_code(known)
+
+
+def nm_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, want_stats: bool = False):
+    """(x - mean) / sqrt(variance + eps) * weight + bias over the last dimension (1 to 32768), of x's type; x, weight and bias float32 or bfloat16.
+    want_stats: (y, mean, rstd), the last two float32 of x's shape without its last dimension, as nm_layer_norm_grad reads them."""
+    lib = load()
+    if not x.is_cuda or x.dim() < 1:
+        raise ValueError("x is a tensor on the GPU with at least one dimension")
+    dt = _dtype_code(x)
+    w, b, wt = _norm_weights(weight, bias, x)
+    shape, C = x.shape, x.shape[-1]
+    x = _unit_columns(x.reshape(-1, C) if C else x.reshape(0, C))
+    R = x.shape[0]
+    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    mean, rstd = (torch.empty(shape[:-1], dtype=torch.float32, device=x.device) for _ in range(2)) if want_stats else (None, None)
+    with torch.cuda.device(x.device):
+        _check(lib.nm_layer_norm(_ptr(x), _rowmajor(x, "x"), dt, _ptr(w), _ptr(b), wt, R, C, float(eps), _ptr(y), C, _ptr(mean), _ptr(rstd), _stream(x)))
+    return (y, mean, rstd) if want_stats else y
+
+
+def nm_layer_norm_grad(g: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor, want_weight: bool = True,
+                       want_bias: bool = True):
+    """(dx, dweight, dbias) of nm_layer_norm from the gradient g of its result, its x and weight (None: ones), and the mean and rstd that it left.  dx is of
+    x's type, dweight and dbias of weight's (float32 without one); None where not wanted."""
+    lib = load()
+    if not x.is_cuda or x.dim() < 1 or g.shape != x.shape or g.dtype != x.dtype or g.device != x.device:
+        raise ValueError("x and g are tensors of one shape and type on one GPU")
+    dt = _dtype_code(x)
+    w, _, wt = _norm_weights(weight, None, x)
+    for t in (mean, rstd):
+        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or t.device != x.device:
+            raise ValueError("mean and rstd are float32, one for each row, on the tensor's device")
+    mean, rstd = mean.contiguous(), rstd.contiguous()
+    shape, C = x.shape, x.shape[-1]
+    x, g = (_unit_columns(t.reshape(-1, C) if C else t.reshape(0, C)) for t in (x, g))
+    R = x.shape[0]
+    dx = torch.empty(shape, dtype=x.dtype, device=x.device)
+    kind = torch.float32 if weight is None else weight.dtype
+    dw = torch.empty(C, dtype=kind, device=x.device) if want_weight else None
+    db = torch.empty(C, dtype=kind, device=x.device) if want_bias else None
+    need = int(lib.nm_layer_norm_grad_workspace(R, C)) if want_weight or want_bias else 0
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    with torch.cuda.device(x.device):
+        _check(lib.nm_layer_norm_grad(_ptr(g), _rowmajor(g, "g"), _ptr(x), _rowmajor(x, "x"), dt, _ptr(w), wt, _ptr(mean), _ptr(rstd), R, C, _ptr(dx), C, _ptr(dw), _ptr(db),
+                                      _ptr(ws), need, _stream(x)))
+    return dx, dw, db
+
+
+def rotary_freqs(width: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0, original_length: int = 0, slow: float = 1.0, fast: float = 32.0,
+                 device=None) -> torch.Tensor:
+    """Radians to a position of `width` turned elements, for nm_rotary: float64 [width / 2], base ** (-2 j / width).  For contexts `factor` times as long as the
+    ones trained on, scaling is "linear": all divided by factor; "base": the base raised so that the slowest pair is divided by factor and the fastest kept;
+    "parts": pairs that turn more than `fast` times over original_length positions kept, those that turn less than `slow` times divided, a line between."""
+    if width < 2 or width % 2 or not base > 0 or not factor > 0:
+        raise ValueError("width is an even number from 2 on, base and factor are positive")
+    if scaling == "base" and width > 2:
+        base = base * factor ** (width / (width - 2))
+    f = base ** (-torch.arange(0, width, 2, dtype=torch.float64) / width)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "parts":
+        if not (original_length > 0 and fast > slow):
+            raise ValueError('"parts" needs original_length, and fast > slow')
+        turns = f * original_length / (2 * math.pi)
+        keep = ((turns - slow) / (fast - slow)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+    elif scaling not in (None, "base"):
+        raise ValueError(f'scaling is None, "linear", "base" or "parts", got {scaling!r}')
+    return f.to(device) if device is not None else f
+
+
+def _heads(t: torch.Tensor) -> _Heads:
+    return _Heads(t.data_ptr(), *t.stride()[:3])
+
+
+def nm_rotary(x: torch.Tensor, freqs: torch.Tensor, positions: Optional[torch.Tensor] = None, interleaved: bool = False, scale: float = 1.0, inverse: bool = False,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [batch x length x heads x D] (float32 or bfloat16, D up to 1024) with the pairs of each head's first 2 * len(freqs) elements turned by position times
+    frequency and multiplied by scale; what lies behind them stays.  freqs: float64 on the GPU (rotary_freqs); positions: int32 or int64, [length] or
+    [batch x length], 0 .. length - 1 without.  Pairs: neighbours where interleaved, otherwise half the turned elements apart.  inverse: turned back, which is the
+    gradient with respect to x of the call without it.  out: a tensor for the result, x itself among them."""
+    lib = load()
+    if not x.is_cuda or x.dim() != 4:
+        raise ValueError("x is a 4-D tensor on the GPU: batch, length, heads, elements")
+    dt = _dtype_code(x)
+    B, T, H, D = x.shape
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or freqs.device != x.device:
+        raise TypeError("freqs is a float64 vector on the tensor's device")
+    if x.stride(3) != 1 and D > 1:
+        if out is x:
+            raise ValueError("elements of a head lie side by side in a tensor that is turned in place")
+        x = x.contiguous()
+    bits, pos_stride = 32, 0
+    if positions is not None:
+        if positions.dtype not in (torch.int32, torch.int64):
+            raise TypeError(f"positions are int32 or int64, got {positions.dtype}")
+        if positions.device != x.device or tuple(positions.shape) not in ((T,), (B, T)):
+            raise ValueError(f"positions of {B} x {T} tokens have shape [{T}] or [{B}, {T}], on the tensor's device")
+        bits = 64 if positions.dtype == torch.int64 else 32
+        positions = positions.contiguous()
+        pos_stride = T if positions.dim() == 2 else 0
+    y = torch.empty((B, T, H, D), dtype=x.dtype, device=x.device) if out is None else out
+    if y.shape != x.shape or y.dtype != x.dtype or y.device != x.device or (D > 1 and y.stride(3) != 1):
+        raise ValueError("out has x's shape, type and device, and elements of a head side by side")
+    freqs = freqs.contiguous()
+    with torch.cuda.device(x.device):
+        _check(lib.nm_rotary(_heads(x), _heads(y), dt, B, T, H, D, 2 * freqs.numel(), _ptr(freqs), _ptr(positions), bits, pos_stride, int(interleaved), float(scale), int(inverse),
+                             _stream(x)))
+    if out is not None and not out.is_inference():
+        torch.autograd.graph.increment_version([out])
+    return y
+
+
+def _attention_input(t: torch.Tensor, what: str, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A tensor of heads as the kernels read it: a copy where elements are apart or rows off a 16-byte boundary."""
+    if not t.is_cuda or t.dim() != 4:
+        raise ValueError(f"{what} is a 4-D tensor on the GPU: batch, length, heads, elements")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise TypeError(f"{what} is of another type or on another device than q")
+    size = t.element_size()
+    fits = t.stride(3) == 1 and t.data_ptr() % 16 == 0 and all(n < 2 or s * size % 16 == 0 for n, s in zip(t.shape, t.stride()[:3]))
+    return t if fits else t.clone(memory_format=torch.contiguous_format)
+
+
+def _attention_sizes(q, k, v):
+    B, Tq, Hq, D = q.shape
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)}: k and v are alike, with q's batch and elements")
+    return B, Tq, k.shape[1], Hq, k.shape[2], D
+
+
+def _lengths_of(lens: Optional[torch.Tensor], B: int, device) -> Optional[torch.Tensor]:
+    if lens is None:
+        return None
+    if lens.dtype not in (torch.int32, torch.int64) or tuple(lens.shape) != (B,) or lens.device != device:
+        raise ValueError(f"lengths of {B} sequences are int32 or int64 [{B}] on the tensors' device")
+    return lens.clamp(-1, 0x7fffffff).to(torch.int32) if lens.dtype == torch.int64 else lens.contiguous()
+
+
+def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None, q_lens: Optional[torch.Tensor] = None,
+                 k_lens: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """softmax(scale q k^T) v for each head.  q [batch x queries x heads x D], k and v [batch x keys x kv_heads x D], float32 or bfloat16 of one type, D a multiple of
+    8 up to 128; heads / kv_heads heads of q in a row share one of k and v.  scale: D ** -0.5 by default.  causal: query i of n sees the keys up to i + m - n of m, the last
+    query the last key, so that one query over a cache of keys sees all of them.  q_lens, k_lens (int32 or int64 [batch], on the GPU): the tokens of each sequence, from
+    the front; what lies behind counts for nothing, and the result is zero there, as for a query that sees no key.
+    want_lse: (o, lse), lse float32 [batch x heads x queries], the logarithm of the sum of exponentials, which nm_attention_grad reads."""
+    lib = load()
+    q = _attention_input(q, "q")
+    k, v = _attention_input(k, "k", q), _attention_input(v, "v", q)
+    dt = _dtype_code(q)
+    sizes = B, Tq, Tk, Hq, Hk, D = _attention_sizes(q, k, v)
+    ql, kl = _lengths_of(q_lens, B, q.device), _lengths_of(k_lens, B, q.device)
+    o = torch.empty((B, Tq, Hq, D), dtype=q.dtype, device=q.device)
+    lse = torch.empty((B, Hq, Tq), dtype=torch.float32, device=q.device) if want_lse else None
+    need = int(lib.nm_attention_workspace(*sizes, dt))
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    with torch.cuda.device(q.device):
+        _check(lib.nm_attention(_heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), D ** -0.5 if scale is None else float(scale), _ptr(ql), _ptr(kl),
+                                _ptr(ws), need, _stream(q)))
+    return (o, lse) if want_lse else o
+
+
+def nm_attention_grad(g: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor, causal: bool = False,
+                      scale: Optional[float] = None, q_lens: Optional[torch.Tensor] = None, k_lens: Optional[torch.Tensor] = None, out=None):
+    """(dq, dk, dv) of nm_attention from the gradient g of its result o; the other arguments as they were given to it, and the lse that it left.  The probabilities
+    are computed again.  The same call gives the same bits.  out: three tensors for the results, of q's, k's and v's shapes, parts of one tensor among them."""
+    lib = load()
+    q = _attention_input(q, "q")
+    k, v, g, o = (_attention_input(t, what, q) for t, what in ((k, "k"), (v, "v"), (g, "g"), (o, "o")))
+    dt = _dtype_code(q)
+    sizes = B, Tq, Tk, Hq, Hk, D = _attention_sizes(q, k, v)
+    if g.shape != q.shape or o.shape != q.shape:
+        raise ValueError("g and o have q's shape")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, Tq) or lse.device != q.device:
+        raise ValueError(f"lse is float32 [{B}, {Hq}, {Tq}] on the tensors' device")
+    lse = lse.contiguous()
+    ql, kl = _lengths_of(q_lens, B, q.device), _lengths_of(k_lens, B, q.device)
+    if out is None:
+        dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+    else:
+        dq, dk, dv = out
+        for d, t in ((dq, q), (dk, k), (dv, v)):
+            if d.shape != t.shape or d.dtype != t.dtype or d.device != t.device or d.stride(3) != 1:
+                raise ValueError("out: tensors of q's, k's and v's shapes, type and device, elements of a head side by side")
+    need = int(lib.nm_attention_grad_workspace(*sizes, dt))
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(lib.nm_attention_grad(_heads(g), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), D ** -0.5 if scale is None else float(scale),
+                                     _ptr(ql), _ptr(kl), _heads(dq), _heads(dk), _heads(dv), _ptr(ws), need, _stream(q)))
+    if out is not None:
+        torch.autograd.graph.increment_version([t for t in out if not t.is_inference()])
+    return dq, dk, dv
 
 
 # ---- the optimizer's step

@@ -1,0 +1,231 @@
+// Attention, forward: for each head o = softmax(scale q k^T) v over the keys that a query sees, lse = log of the sum of exponentials.
+//
+// One pass over the keys with the running maximum and sum.  A wave keeps 32 rows (attention.h) as columns: S^T = K Q^T from rows of K in LDS, P^T = 2^(c S^T - m) where it
+// lies, O^T += V^T P^T from columns of V in LDS.  The maximum m of a column moves only when a score is 2^8 times beyond it (P then stays below 2^8, sums and products in
+// binary32 are as near), so that the sums O are scaled only a few times.  Tiles of keys go through the registers of the workgroup into one of two LDS buffers while the
+// other is read; one barrier a tile.  A row that sees no key: o = 0, lse = -infinity.  Rows behind their sequence's queries: the same.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "attention.h"
+#include "gemm_plan.h"           // NM_CUS
+
+namespace nm {
+
+namespace attn {
+
+constexpr float MOVE = 8.0f;     // a maximum moves when it is beaten by this power of two
+
+template <int DT, int BLOCKS, int WAVES, int KEYS>
+__global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2) void attention_kernel(const AttnArg p, int row_tiles)
+{
+    typedef Tile<DT, BLOCKS> L;
+    constexpr int ES = L::ES, THREADS = 64 * WAVES, ROWS = 32 * WAVES, SB = KEYS / 32;
+    __shared__ __align__(16) char lds[2][2][KEYS * L::ROW];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
+    // the tiles of a head side by side, those with most keys first
+    const int64_t place = place_of(blockIdx.x, gridDim.x);
+    const int tile = row_tiles - 1 - (int)(place / p.splits % row_tiles), split = (int)(place % p.splits);
+    const Sequence s(p, (int)(place / p.splits / row_tiles));
+    const int total = p.Tq * p.group, r0 = tile * ROWS;
+    const int row = r0 + wave * 32 + (lane & 31), query = query_of(min(row, total - 1), p), head = s.h * p.group + min(row, total - 1) - query * p.group;
+    const bool there = row < total && query < s.nq;
+    // keys that the workgroup, the wave (its last and its first row) and the lane see
+    const int last_query = query_of(min(r0 + ROWS, total) - 1, p);
+    const int most = s.nq == 0 || query_of(r0, p) >= s.nq ? 0 : s.seen(p, min(last_query, s.nq - 1));
+    const int wave_first = query_of(min(r0 + wave * 32, total - 1), p), wave_last = query_of(min(r0 + wave * 32 + 31, total - 1), p);
+    const int wave_most = r0 + wave * 32 >= total || wave_first >= s.nq ? 0 : s.seen(p, min(wave_last, s.nq - 1)), wave_least = s.seen(p, wave_first);
+    const int seen = s.seen(p, query);
+    const int tiles = (most + KEYS - 1) / KEYS;
+    const int first_tile = (int)((int64_t)tiles * split / p.splits), end_tile = (int)((int64_t)tiles * (split + 1) / p.splits);
+
+    Frag<DT> q[2 * BLOCKS];
+    load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
+    f32x16 o[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) o[b] = f32x16{};
+    float m = -INFINITY, sum = 0.0f;
+    const float c = p.scale * LOG2E;
+
+    const char *k0 = row_at(p.k, p.sk, s.b, 0, s.h, ES), *v0 = row_at(p.v, p.sv, s.b, 0, s.h, ES);
+    Stage<DT, BLOCKS, KEYS, THREADS> ks, vs;
+    auto load = [&](int t) {
+        const int64_t key0 = (int64_t)t * KEYS;
+        const int rows = min(KEYS, s.nk - t * KEYS);
+        ks.load([&](int r) { return k0 + (key0 + r) * p.sk.t * ES; }, rows, p.D);
+        vs.load([&](int r) { return v0 + (key0 + r) * p.sv.t * ES; }, rows, p.D);
+    };
+    if (first_tile < end_tile) {
+        load(first_tile);
+        ks.store(lds[0][0]);
+        vs.store(lds[0][1]);
+    }
+    __syncthreads();
+    for (int t = first_tile; t < end_tile; ++t) {
+        const char *kt = lds[t - first_tile & 1][0], *vt = lds[t - first_tile & 1][1];
+        if (t + 1 < end_tile) load(t + 1);
+        if (t * KEYS < wave_most) {
+            f32x16 x[SB];
+#pragma unroll
+            for (int a = 0; a < SB; ++a) {
+                x[a] = f32x16{};
+#pragma unroll
+                for (int kk = 0; kk < 2 * BLOCKS; ++kk) mma(x[a], row_fragment<DT, BLOCKS>(kt, 32 * a, kk, lane), q[kk]);
+            }
+            if ((t + 1) * KEYS > wave_least) {
+#pragma unroll
+                for (int a = 0; a < SB; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t * KEYS + 32 * a + row_of(i, hi) >= seen) x[a][i] = -INFINITY;
+            }
+            float top = x[0][0];
+#pragma unroll
+            for (int a = 0; a < SB; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[a][i]);
+            top = fmaxf(top, other_half(top)) * c;
+            const bool move = top > m + MOVE;                            // (m = -infinity: any score)
+            if (__any(move)) {
+                const float by = move ? exp2_of(m - top) : 1.0f;
+                if (move) m = top;
+                sum *= by;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[b][i] *= by;
+            }
+            const float base = m == -INFINITY ? 0.0f : m;                // (nothing seen so far)
+#pragma unroll
+            for (int a = 0; a < SB; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[a][i] = exp2_of(__builtin_fmaf(x[a][i], c, -base));
+                    sum += x[a][i];
+                }
+#pragma unroll
+            for (int a = 0; a < SB; ++a)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const Frag<DT> w = as_fragment<DT>(x[a], 8 * g);
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b) mma(o[b], column_fragment<DT, BLOCKS>(vt, 32 * a + 16 * g, b, lane), w);
+                }
+        }
+        if (t + 1 < end_tile) {
+            ks.store(lds[(t - first_tile & 1) ^ 1][0]);
+            vs.store(lds[(t - first_tile & 1) ^ 1][1]);
+        }
+        __syncthreads();
+    }
+    sum += other_half(sum);
+    if (row >= total) return;
+    if (!there) {                                                        // (a column that was not there has taken part with zeros)
+        m = -INFINITY;
+        sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) o[b] = f32x16{};
+    }
+    const int64_t at = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
+    if (p.splits == 1) {
+        store_column<DT, BLOCKS>((char *)row_at(p.o, p.so, s.b, query, head, ES), o, sum != 0.0f ? 1.0f / sum : 0.0f, p.D, lane);
+        if (p.lse && hi == 0) p.lse[at] = (m + __builtin_amdgcn_logf(sum)) * LN2;             // (log2; -infinity of a sum of zero)
+    } else {
+        // O, m and the sum of this part of the keys
+        const int64_t rows = (int64_t)p.B * p.Hq * p.Tq;
+        float *to = p.part + ((int64_t)split * rows + at) * p.D;
+        store_column<NM_DT_F32, BLOCKS>((char *)to, o, 1.0f, p.D, lane);
+        if (hi == 0) {
+            float *st = p.part + (int64_t)p.splits * rows * p.D + ((int64_t)split * rows + at) * 2;
+            st[0] = m;
+            st[1] = sum;
+        }
+    }
+}
+
+// the parts of a row together: 2^shift threads to a row, 4 elements each
+template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArg p, int shift)
+{
+    const int64_t rows = (int64_t)p.B * p.Hq * p.Tq, at = (int64_t)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift);
+    const int e = ((int)threadIdx.x & ((1 << shift) - 1)) * 4;
+    if (at >= rows || e >= p.D) return;
+    const int64_t bh = at / p.Tq;
+    const int query = (int)(at - bh * p.Tq), b = (int)(bh / p.Hq), head = (int)(bh - (int64_t)b * p.Hq);
+    const float *st = p.part + (int64_t)p.splits * rows * p.D;
+    float m = -INFINITY;
+    for (int k = 0; k < p.splits; ++k) m = fmaxf(m, st[(k * rows + at) * 2]);
+    const float base = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    for (int k = 0; k < p.splits; ++k) {
+        const float w = exp2_of(st[(k * rows + at) * 2] - base);
+        const f32x4 x = *(const f32x4 *)(p.part + (k * rows + at) * p.D + e);
+        sum += w * st[(k * rows + at) * 2 + 1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += w * x[i];
+    }
+    const float by = sum != 0.0f ? 1.0f / sum : 0.0f;
+    char *to = (char *)row_at(p.o, p.so, b, query, head, DT == NM_DT_BF16 ? 2 : 4);
+    if constexpr (DT == NM_DT_BF16) *(u32x2 *)(to + e * 2) = u32x2{pack_bf16_rne(o[0] * by, o[1] * by), pack_bf16_rne(o[2] * by, o[3] * by)};
+    else *(f32x4 *)(to + e * 4) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
+    if (p.lse && e == 0) p.lse[at] = (base + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// how many rows a workgroup takes, and in how many parts the keys go
+struct Plan { int waves, keys, splits; int64_t row_tiles; };
+inline Plan plan_of(const AttnArg &a)
+{
+    Plan p;
+    const int64_t total = (int64_t)a.Tq * a.group, heads = (int64_t)a.B * a.Hk;
+    p.waves = total <= 32 ? 1 : 4;
+    p.keys = p.waves == 1 ? 32 : a.dt == NM_DT_F32 ? 32 : 64;
+    p.row_tiles = (total + 32 * p.waves - 1) / (32 * p.waves);
+    const int64_t wgs = heads * p.row_tiles, want = (p.waves == 1 ? 8 : 2) * NM_CUS;
+    p.splits = wgs >= want / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, (a.Tk + 4 * p.keys - 1) / (4 * p.keys), 64}));
+    return p;
+}
+
+template <int DT, int BLOCKS> hipError_t launch(const AttnArg &a, const Plan &p, hipStream_t st)
+{
+    const int64_t wgs = (int64_t)a.B * a.Hk * p.row_tiles * p.splits;
+    if (!grid_holds(wgs, 64 * p.waves) || wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (p.waves == 1) attention_kernel<DT, BLOCKS, 1, 32><<<dim3((unsigned)wgs), dim3(64), 0, st>>>(a, (int)p.row_tiles);
+    else attention_kernel<DT, BLOCKS, 4, DT == NM_DT_F32 ? 32 : 64><<<dim3((unsigned)wgs), dim3(256), 0, st>>>(a, (int)p.row_tiles);
+    return hipGetLastError();
+}
+template <int DT> hipError_t launch(const AttnArg &a, const Plan &p, hipStream_t st)
+{
+    switch ((a.D + 31) / 32) {
+        case 1: return launch<DT, 1>(a, p, st);
+        case 2: return launch<DT, 2>(a, p, st);
+        case 3: return launch<DT, 3>(a, p, st);
+        default: return launch<DT, 4>(a, p, st);
+    }
+}
+
+}  // namespace attn
+
+size_t attention_workspace(const AttnArg &a)
+{
+    const attn::Plan p = attn::plan_of(a);
+    return p.splits == 1 ? 0 : (size_t)p.splits * a.B * a.Hq * a.Tq * (a.D + 2) * 4;
+}
+
+hipError_t launch_attention(AttnArg a, void *workspace, hipStream_t st)
+{
+    const attn::Plan p = attn::plan_of(a);
+    a.splits = p.splits;
+    a.part = (float *)workspace;
+    hipError_t e = a.dt == NM_DT_BF16 ? attn::launch<NM_DT_BF16>(a, p, st) : attn::launch<NM_DT_F32>(a, p, st);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int shift = a.D <= 32 ? 3 : a.D <= 64 ? 4 : 5;
+    const int64_t rows = (int64_t)a.B * a.Hq * a.Tq, wgs = (rows + (256 >> shift) - 1) / (256 >> shift);
+    if (!grid_holds(wgs, 256)) return hipErrorInvalidConfiguration;
+    if (a.dt == NM_DT_BF16) attn::attention_join_kernel<NM_DT_BF16><<<dim3((unsigned)wgs), dim3(256), 0, st>>>(a, shift);
+    else attn::attention_join_kernel<NM_DT_F32><<<dim3((unsigned)wgs), dim3(256), 0, st>>>(a, shift);
+    return hipGetLastError();
+}
+
+}  // namespace nm

@@ -1,0 +1,308 @@
+// Attention, gradients.  With P = 2^(c S - lse) recomputed from q, k and the forward pass's lse, delta = sum over the head of g o, dP = g v^T:
+//     dS = P (dP - delta)      dq = scale dS k      dk = scale dS^T q      dv = P^T g
+// Two kernels, each with its results in registers from beginning to end, so that no sum crosses workgroups and the same call gives the same bits:
+//   dq      a wave keeps 32 rows (attention.h) of q and g as columns: S^T = K Q^T, dP^T = V G^T, dQ^T += K^T dS^T over tiles of keys; delta comes from its own rows first
+//   dk dv   a wave keeps 32 keys as columns: S = Q K^T, dP = G V^T, dV^T += G^T P, dK^T += Q^T dS over tiles of the rows of all heads that share the keys
+// Both recompute S and dP: seven products instead of five, and neither atomics nor a matrix in memory (dS of a pair, written and read in bf16, would take 4 bytes
+// at about 5 TB/s against 4 D operations).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "attention.h"
+#include "gemm_plan.h"           // NM_CUS
+
+namespace nm {
+
+namespace attn {
+
+template <int DT, int BLOCKS, int KEYS>
+__global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void attention_dq_kernel(const AttnArg p, int row_tiles)
+{
+    typedef Tile<DT, BLOCKS> L;
+    constexpr int ES = L::ES, ROWS = 128, SB = KEYS / 32;
+    __shared__ __align__(16) char lds[2][2][KEYS * L::ROW];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
+    const int64_t place = place_of(blockIdx.x, gridDim.x);
+    const int tile = row_tiles - 1 - (int)(place % row_tiles);
+    const Sequence s(p, (int)(place / row_tiles));
+    const int total = p.Tq * p.group, r0 = tile * ROWS;
+    const int row = r0 + wave * 32 + (lane & 31), query = query_of(min(row, total - 1), p), head = s.h * p.group + min(row, total - 1) - query * p.group;
+    const bool there = row < total && query < s.nq;
+    const int last_query = query_of(min(r0 + ROWS, total) - 1, p);
+    const int most = s.nq == 0 || query_of(r0, p) >= s.nq ? 0 : s.seen(p, min(last_query, s.nq - 1));
+    const int wave_first = query_of(min(r0 + wave * 32, total - 1), p), wave_last = query_of(min(r0 + wave * 32 + 31, total - 1), p);
+    const int wave_most = r0 + wave * 32 >= total || wave_first >= s.nq ? 0 : s.seen(p, min(wave_last, s.nq - 1)), wave_least = s.seen(p, wave_first);
+    const int seen = s.seen(p, query), tiles = (most + KEYS - 1) / KEYS;
+    const int64_t at = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
+
+    Frag<DT> q[2 * BLOCKS], g[2 * BLOCKS];
+    load_fragments<DT, BLOCKS>(g, row_at(p.o, p.so, s.b, query, head, ES), there, p.D, lane);
+    load_fragments<DT, BLOCKS>(q, row_at(p.g, p.sg, s.b, query, head, ES), there, p.D, lane);
+    float delta = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 2 * BLOCKS; ++kk)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)q[kk].v[j], (float)g[kk].v[j], delta);
+    delta += other_half(delta);
+#pragma unroll
+    for (int kk = 0; kk < 2 * BLOCKS; ++kk) g[kk] = q[kk];
+    if (hi == 0 && row < total) p.delta[at] = delta;
+    load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
+    // (a row that sees nothing has lse = -infinity: with +infinity in its place P is zero)
+    const float l = there ? p.lse[at] : -INFINITY, lse = l == -INFINITY ? INFINITY : l * LOG2E, c = p.scale * LOG2E;
+    f32x16 dq[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) dq[b] = f32x16{};
+
+    const char *k0 = row_at(p.k, p.sk, s.b, 0, s.h, ES), *v0 = row_at(p.v, p.sv, s.b, 0, s.h, ES);
+    Stage<DT, BLOCKS, KEYS, 256> ks, vs;
+    auto load = [&](int t) {
+        const int64_t key0 = (int64_t)t * KEYS;
+        const int rows = min(KEYS, s.nk - t * KEYS);
+        ks.load([&](int r) { return k0 + (key0 + r) * p.sk.t * ES; }, rows, p.D);
+        vs.load([&](int r) { return v0 + (key0 + r) * p.sv.t * ES; }, rows, p.D);
+    };
+    if (tiles > 0) {
+        load(0);
+        ks.store(lds[0][0]);
+        vs.store(lds[0][1]);
+    }
+    __syncthreads();
+    for (int t = 0; t < tiles; ++t) {
+        const char *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+        if (t + 1 < tiles) load(t + 1);
+        if (t * KEYS < wave_most) {
+            f32x16 x[SB], dp[SB];
+#pragma unroll
+            for (int a = 0; a < SB; ++a) {
+                x[a] = dp[a] = f32x16{};
+#pragma unroll
+                for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+                    mma(x[a], row_fragment<DT, BLOCKS>(kt, 32 * a, kk, lane), q[kk]);
+                    mma(dp[a], row_fragment<DT, BLOCKS>(vt, 32 * a, kk, lane), g[kk]);
+                }
+            }
+            const bool edge = (t + 1) * KEYS > wave_least;
+#pragma unroll
+            for (int a = 0; a < SB; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = exp2_of(__builtin_fmaf(x[a][i], c, -lse));
+                    x[a][i] = w * (dp[a][i] - delta);
+                }
+            if (edge) {
+#pragma unroll
+                for (int a = 0; a < SB; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t * KEYS + 32 * a + row_of(i, hi) >= seen) x[a][i] = 0.0f;
+            }
+#pragma unroll
+            for (int a = 0; a < SB; ++a)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const Frag<DT> w = as_fragment<DT>(x[a], 8 * h);
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b) mma(dq[b], column_fragment<DT, BLOCKS>(kt, 32 * a + 16 * h, b, lane), w);
+                }
+        }
+        if (t + 1 < tiles) {
+            ks.store(lds[(t & 1) ^ 1][0]);
+            vs.store(lds[(t & 1) ^ 1][1]);
+        }
+        __syncthreads();
+    }
+    if (!there)
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) dq[b] = f32x16{};
+    if (row < total) store_column<DT, BLOCKS>((char *)row_at(p.dq, p.sdq, s.b, query, head, ES), dq, p.scale, p.D, lane);
+}
+
+template <int DT, int BLOCKS, int ROWS>
+__global__ __launch_bounds__(256, DT == NM_DT_F32 || BLOCKS > 2 ? 1 : 2) void attention_dkdv_kernel(const AttnArg p, int key_tiles)
+{
+    typedef Tile<DT, BLOCKS> L;
+    constexpr int ES = L::ES, KEYS = 128, SB = ROWS / 32;
+    __shared__ __align__(16) char lds[2][2][ROWS * L::ROW];
+    __shared__ float lse_of[2][ROWS], delta_of[2][ROWS];
+    __shared__ int seen_of[2][ROWS];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
+    const int64_t place = place_of(blockIdx.x, gridDim.x);
+    const int tile = (int)(place / p.splits % key_tiles), split = (int)(place % p.splits);       // (the first keys have most rows)
+    const Sequence s(p, (int)(place / p.splits / key_tiles));
+    const int key0 = tile * KEYS, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
+    const bool there = key < s.nk;
+    // rows that see any of the keys: those of queries from first_query on
+    const int total = s.nq * p.group, first_query = p.causal ? max(0, key0 - (s.nk - s.nq)) : 0;
+    const int first = min((int64_t)total, (int64_t)first_query * p.group) / ROWS, tiles = key0 < s.nk ? max(0, (total + ROWS - 1) / ROWS - first) : 0;
+    const int first_tile = first + (int)((int64_t)tiles * split / p.splits), end_tile = first + (int)((int64_t)tiles * (split + 1) / p.splits);
+
+    Frag<DT> k[2 * BLOCKS], v[2 * BLOCKS];
+    const int safe_key = min(key, p.Tk - 1);
+    load_fragments<DT, BLOCKS>(k, row_at(p.k, p.sk, s.b, safe_key, s.h, ES), there, p.D, lane);
+    load_fragments<DT, BLOCKS>(v, row_at(p.v, p.sv, s.b, safe_key, s.h, ES), there, p.D, lane);
+    f32x16 dk[BLOCKS], dv[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) dk[b] = dv[b] = f32x16{};
+    const float c = p.scale * LOG2E;
+    const int blind = p.causal ? max(0, s.nq - s.nk) * p.group : 0;       // rows that see nothing: what their q and g hold does not count
+
+    const char *q0 = row_at(p.q, p.sq, s.b, 0, s.h * p.group, ES), *g0 = row_at(p.g, p.sg, s.b, 0, s.h * p.group, ES);
+    Stage<DT, BLOCKS, ROWS, 256> qs, gs;
+    float lse_next = 0.0f, delta_next = 0.0f;
+    int seen_next = 0;
+    auto load = [&](int t) {
+        const int r0 = t * ROWS, rows = min(ROWS, total - r0);
+        auto at = [&](const char *from, const AttnStride &st, int r) {
+            const int query = query_of(r0 + r, p);
+            return from + (query * st.t + (r0 + r - query * p.group) * st.h) * ES;
+        };
+        qs.load([&](int r) { return at(q0, p.sq, r); }, rows, p.D, blind - r0);
+        gs.load([&](int r) { return at(g0, p.sg, r); }, rows, p.D, blind - r0);
+        if ((int)threadIdx.x < ROWS) {
+            const int r = r0 + min((int)threadIdx.x, rows - 1), query = query_of(r, p), head = s.h * p.group + r - query * p.group;
+            const int64_t where = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
+            const bool ok = (int)threadIdx.x < rows;
+            const float l = p.lse[where];
+            lse_next = ok && l != -INFINITY ? l * LOG2E : INFINITY;       // (P = 0)
+            delta_next = ok ? p.delta[where] : 0.0f;
+            seen_next = ok ? s.seen(p, query) : 0;
+        }
+    };
+    auto store = [&](int to) {
+        qs.store(lds[to][0]);
+        gs.store(lds[to][1]);
+        if ((int)threadIdx.x < ROWS) {
+            lse_of[to][threadIdx.x] = lse_next;
+            delta_of[to][threadIdx.x] = delta_next;
+            seen_of[to][threadIdx.x] = seen_next;
+        }
+    };
+    if (first_tile < end_tile) {
+        load(first_tile);
+        store(0);
+    }
+    __syncthreads();
+    for (int t = first_tile; t < end_tile; ++t) {
+        const int buf = t - first_tile & 1;
+        const char *qt = lds[buf][0], *gt = lds[buf][1];
+        if (t + 1 < end_tile) load(t + 1);
+        // the tile's last row sees most keys, its first one fewest
+        const int tile_most = s.seen(p, query_of(min(t * ROWS + ROWS, total) - 1, p)), tile_least = s.seen(p, query_of(t * ROWS, p));
+        if (wave_key < tile_most) {
+            const bool edge = tile_least < wave_key + 32;
+#pragma unroll
+            for (int a = 0; a < SB; ++a) {
+                f32x16 x = f32x16{}, dp = f32x16{};
+#pragma unroll
+                for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+                    mma(x, row_fragment<DT, BLOCKS>(qt, 32 * a, kk, lane), k[kk]);
+                    mma(dp, row_fragment<DT, BLOCKS>(gt, 32 * a, kk, lane), v[kk]);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x4 l = *(const f32x4 *)&lse_of[buf][32 * a + row_of(i, hi)], d = *(const f32x4 *)&delta_of[buf][32 * a + row_of(i, hi)];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        x[i + j] = exp2_of(__builtin_fmaf(x[i + j], c, -l[j]));
+                        dp[i + j] = x[i + j] * (dp[i + j] - d[j]);
+                        if (edge && key >= seen_of[buf][32 * a + row_of(i + j, hi)]) x[i + j] = dp[i + j] = 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const Frag<DT> w = as_fragment<DT>(x, 8 * h), ds = as_fragment<DT>(dp, 8 * h);
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b) {
+                        mma(dv[b], column_fragment<DT, BLOCKS>(gt, 32 * a + 16 * h, b, lane), w);
+                        mma(dk[b], column_fragment<DT, BLOCKS>(qt, 32 * a + 16 * h, b, lane), ds);
+                    }
+                }
+            }
+        }
+        if (t + 1 < end_tile) store(buf ^ 1);
+        __syncthreads();
+    }
+    if (key >= p.Tk) return;
+    if (!there)                                                          // (what stands in the columns of keys that are not there)
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) dk[b] = dv[b] = f32x16{};
+    if (p.splits == 1) {
+        store_column<DT, BLOCKS>((char *)row_at(p.dk, p.sdk, s.b, key, s.h, ES), dk, p.scale, p.D, lane);
+        store_column<DT, BLOCKS>((char *)row_at(p.dv, p.sdv, s.b, key, s.h, ES), dv, 1.0f, p.D, lane);
+    } else {
+        const int64_t keys = (int64_t)p.B * p.Hk * p.Tk, at = ((int64_t)s.b * p.Hk + s.h) * p.Tk + key;
+        store_column<NM_DT_F32, BLOCKS>((char *)(p.part + ((int64_t)split * 2 * keys + at) * p.D), dk, p.scale, p.D, lane);
+        store_column<NM_DT_F32, BLOCKS>((char *)(p.part + ((int64_t)(split * 2 + 1) * keys + at) * p.D), dv, 1.0f, p.D, lane);
+    }
+}
+
+// the parts of dk and dv added up in their order: 4 elements to a thread; blockIdx.y: dk, dv
+template <int DT> __global__ __launch_bounds__(256) void attention_sum_kernel(const AttnArg p)
+{
+    const int64_t keys = (int64_t)p.B * p.Hk * p.Tk, n4 = keys * p.D / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n4) return;
+    const int which = (int)blockIdx.y;
+    f32x4 x = {0, 0, 0, 0};
+    for (int k = 0; k < p.splits; ++k) {
+        const f32x4 y = *(const f32x4 *)(p.part + (int64_t)(2 * k + which) * keys * p.D + 4 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] += y[j];
+    }
+    const int64_t at = 4 * i / p.D, bh = at / p.Tk;
+    const int e = (int)(4 * i - at * p.D), b = (int)(bh / p.Hk);
+    const AttnStride st = which ? p.sdv : p.sdk;
+    char *to = (char *)row_at(which ? p.dv : p.dk, st, b, at - bh * p.Tk, bh - (int64_t)b * p.Hk, DT == NM_DT_BF16 ? 2 : 4);
+    if constexpr (DT == NM_DT_BF16) *(u32x2 *)(to + e * 2) = u32x2{pack_bf16_rne(x[0], x[1]), pack_bf16_rne(x[2], x[3])};
+    else *(f32x4 *)(to + e * 4) = x;
+}
+
+inline int64_t key_tiles(const AttnArg &a) { return ((int64_t)a.Tk + 127) / 128; }
+inline int key_splits(const AttnArg &a)
+{
+    const int64_t wgs = (int64_t)a.B * a.Hk * key_tiles(a), rows = (int64_t)a.Tq * a.group;
+    return wgs >= NM_CUS || wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({2 * NM_CUS / wgs, rows / 256, 16}));
+}
+
+template <int DT, int BLOCKS> hipError_t launch_grads(const AttnArg &a, hipStream_t st)
+{
+    constexpr int KEYS = DT == NM_DT_F32 ? 32 : 64, ROWS = 32;
+    const int64_t heads = (int64_t)a.B * a.Hk, row_tiles = ((int64_t)a.Tq * a.group + 127) / 128, kt = key_tiles(a);
+    const int64_t wq = heads * row_tiles, wk = heads * kt * a.splits;
+    if (std::max(wq, wk) > 0x7fffffff || !grid_holds(std::max(wq, wk), 256)) return hipErrorInvalidConfiguration;
+    if (wq > 0) attention_dq_kernel<DT, BLOCKS, KEYS><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || wk == 0) return e;
+    attention_dkdv_kernel<DT, BLOCKS, ROWS><<<dim3((unsigned)wk), dim3(256), 0, st>>>(a, (int)kt);
+    return hipGetLastError();
+}
+
+}  // namespace attn
+
+size_t attention_grad_workspace(const AttnArg &a)
+{
+    const int splits = attn::key_splits(a);
+    const size_t delta = ((size_t)a.B * a.Hq * a.Tq * 4 + 15) / 16 * 16;
+    return delta + (splits == 1 ? 0 : (size_t)splits * 2 * a.B * a.Hk * a.Tk * a.D * 4);
+}
+
+hipError_t launch_attention_grad(AttnArg a, void *workspace, hipStream_t st)
+{
+    a.splits = attn::key_splits(a);
+    a.delta = (float *)workspace;
+    a.part = (float *)((char *)workspace + ((size_t)a.B * a.Hq * a.Tq * 4 + 15) / 16 * 16);
+    hipError_t e;
+    const int blocks = (a.D + 31) / 32;
+    if (a.dt == NM_DT_BF16) e = blocks == 1 ? attn::launch_grads<NM_DT_BF16, 1>(a, st) : blocks == 2 ? attn::launch_grads<NM_DT_BF16, 2>(a, st) : blocks == 3 ? attn::launch_grads<NM_DT_BF16, 3>(a, st) : attn::launch_grads<NM_DT_BF16, 4>(a, st);
+    else e = blocks == 1 ? attn::launch_grads<NM_DT_F32, 1>(a, st) : blocks == 2 ? attn::launch_grads<NM_DT_F32, 2>(a, st) : blocks == 3 ? attn::launch_grads<NM_DT_F32, 3>(a, st) : attn::launch_grads<NM_DT_F32, 4>(a, st);
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t wgs = ((int64_t)a.B * a.Hk * a.Tk * a.D / 4 + 255) / 256;
+    if (!grid_holds(wgs, 256)) return hipErrorInvalidConfiguration;
+    if (a.dt == NM_DT_BF16) attn::attention_sum_kernel<NM_DT_BF16><<<dim3((unsigned)wgs, 2), dim3(256), 0, st>>>(a);
+    else attn::attention_sum_kernel<NM_DT_F32><<<dim3((unsigned)wgs, 2), dim3(256), 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace nm

@@ -213,6 +213,67 @@ struct AdamwRates { double lr, beta1, beta2, eps, weight_decay; int64_t step; fl
 hipError_t launch_adamw(const AdamwTensor *tensors, int count, int param_dt, int grad_dt, bool q8, bool master, const AdamwRates &r, uint64_t seed,
                         hipStream_t st);
 
+// ---- layer norm (layer_norm.hip).  mean, rstd: binary32 [R], may be null in the forward pass
+struct NormArg {
+    const void *x, *w, *b;
+    void *y;
+    float *mean, *rstd;
+    int64_t R, C, ldx, ldy;
+    int x_dt, w_dt;
+    float eps;
+};
+hipError_t launch_layer_norm(const NormArg &a, hipStream_t st);
+struct NormGradArg {
+    const void *g, *x, *w;
+    const float *mean, *rstd;
+    void *dx, *dw, *db;                       // dw, db: of w's type, may be null
+    int64_t R, C, ldg, ldx, lddx;
+    int x_dt, w_dt;
+    float *part;
+};
+size_t layer_norm_grad_workspace(int64_t R, int64_t C);
+hipError_t launch_layer_norm_grad(const NormGradArg &a, hipStream_t st);
+
+// ---- rotary positions (rotary.hip): x [B][T][H][D], strides in elements, the last one 1
+struct AttnStride { int64_t b, t, h; };
+struct RotaryArg {
+    const void *x;
+    void *y;
+    AttnStride sx, sy;
+    const double *freqs;
+    const void *positions;                    // null: 0 .. T - 1
+    int64_t pos_b;                            // between the positions of two sequences; 0: the same for all
+    int64_t B, T;
+    int H, D, part, wide, interleaved, dt;
+    float scale, sign;
+};
+hipError_t launch_rotary(const RotaryArg &a, hipStream_t st);
+
+// ---- attention (attention.hip, attention_grad.hip): q, o [B][Tq][Hq][D], k, v [B][Tk][Hk][D]
+struct AttnArg {
+    const void *q, *k, *v;
+    AttnStride sq, sk, sv, so;
+    void *o;
+    float *lse;                               // [B][Hq][Tq], may be null in the forward pass
+    const int *q_lens, *k_lens;               // may be null
+    int B, Tq, Tk, Hq, Hk, D, dt, causal;
+    int group;                                // Hq / Hk, and r / group as r * group_mul >> group_shift
+    uint32_t group_mul;
+    int group_shift;
+    float scale;
+    int splits;                               // of the keys (forward) or of the rows (gradients of k and v)
+    float *part;                              // their partial results
+    // gradients
+    const void *g;
+    AttnStride sg, sdq, sdk, sdv;
+    void *dq, *dk, *dv;
+    float *delta;                             // [B][Hq][Tq]
+};
+size_t attention_workspace(const AttnArg &a);
+hipError_t launch_attention(AttnArg a, void *workspace, hipStream_t st);
+size_t attention_grad_workspace(const AttnArg &a);
+hipError_t launch_attention_grad(AttnArg a, void *workspace, hipStream_t st);
+
 // The library's static device scratch array (nm_static.hip): its size, and its address on the current device
 // (looked up once per device; no allocation).
 size_t static_scratch_bytes();

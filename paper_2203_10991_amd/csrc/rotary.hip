@@ -1,0 +1,106 @@
+// Rotary positions: pairs (a, b) of a head's first `part` elements become s (a cos - b sin, a sin + b cos), the angle being position times the pair's frequency; pairs are
+// neighbours (interleaved) or lie half of `part` apart.  The gradient is the same with the angle negated (sign).
+//
+// The angle is formed in binary64 turns and brought into half a turn before it is rounded: at position 10^6 a binary32 angle would be off by 0.06.  Cosines and sines are
+// made once for a token, in LDS, and serve all its heads; a thread then turns 8 pairs (two vectors of 8 elements), or 4 interleaved ones, at a time, fewer at the end of the part.  Bound: HBM.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "grid_row.h"
+#include "nm_internal.h"
+#include "row_vec.h"
+
+namespace nm {
+
+namespace {
+
+constexpr int V = EW;            // elements of a vector
+
+// the first `left` of V elements at an element's boundary
+template <int DT> __device__ __forceinline__ void load_v(float (&v)[V], const void *p, int64_t at, int left)
+{
+    const Raw<DT> r = left >= V ? load_raw<DT>(p, at) : load_raw<DT, true>(p, at, left);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = element(r, i);
+}
+
+// 2^lane_bits threads to a head, 2^head_bits heads, and what is left of 256 threads as tokens of a workgroup; `turned` vectors (or pairs of them), `copied` vectors behind the part
+template <int DT, bool INTERLEAVED> __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArg p, int lane_bits, int head_bits, int turned, int copied)
+{
+    extern __shared__ float2 turns[];
+    const int tokens = 256 >> (lane_bits + head_bits), pairs = p.part / 2;
+    const int64_t first = (int64_t)grid_place(blockIdx.x, blockIdx.y) * tokens, n = p.B * p.T;
+    for (int i = threadIdx.x; i < tokens * pairs; i += 256) {
+        const int k = i / pairs, j = i - k * pairs;
+        if (first + k >= n) break;
+        const int64_t b = (first + k) / p.T, t = first + k - b * p.T;
+        const int64_t pos = !p.positions ? t : p.wide ? ((const int64_t *)p.positions)[b * p.pos_b + t] : ((const int32_t *)p.positions)[b * p.pos_b + t];
+        const double turn = (double)pos * (p.freqs[j] * 0.15915494309189533577);
+        float sn, cs;
+        sincospif(2.0f * (float)(turn - rint(turn)), &sn, &cs);
+        turns[i] = make_float2(cs * p.scale, sn * p.scale * p.sign);
+    }
+    __syncthreads();
+    const int lane = (int)threadIdx.x & ((1 << lane_bits) - 1), head0 = (int)threadIdx.x >> lane_bits & ((1 << head_bits) - 1), token = (int)threadIdx.x >> (lane_bits + head_bits);
+    if (first + token >= n) return;
+    const int64_t b = (first + token) / p.T, t = first + token - b * p.T;
+    const float2 *cs = turns + token * pairs;
+    for (int head = head0; head < p.H; head += 1 << head_bits) {
+        const int64_t x0 = b * p.sx.b + t * p.sx.t + head * p.sx.h, y0 = b * p.sy.b + t * p.sy.t + head * p.sy.h;
+        for (int c = lane; c < turned + copied; c += 1 << lane_bits) {
+            float v[V], y[V];
+            if (c >= turned) {
+                const int at = p.part + (c - turned) * V, left = p.D - at;
+                load_v<DT>(v, p.x, x0 + at, left);
+                store_row<DT>(p.y, y0 + at, 0, left, v);
+            } else if constexpr (INTERLEAVED) {
+                const int at = c * V, left = p.part - at;
+                load_v<DT>(v, p.x, x0 + at, left);
+#pragma unroll
+                for (int i = 0; i < V; i += 2) {
+                    const float2 k = cs[min(at / 2 + i / 2, pairs - 1)];
+                    y[i] = v[i] * k.x - v[i + 1] * k.y;
+                    y[i + 1] = v[i] * k.y + v[i + 1] * k.x;
+                }
+                store_row<DT>(p.y, y0 + at, 0, left, y);
+            } else {
+                const int at = c * V, left = pairs - at;
+                float w[V], z[V];
+                load_v<DT>(v, p.x, x0 + at, left);
+                load_v<DT>(w, p.x, x0 + pairs + at, left);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float2 k = cs[min(at + i, pairs - 1)];
+                    y[i] = v[i] * k.x - w[i] * k.y;
+                    z[i] = v[i] * k.y + w[i] * k.x;
+                }
+                store_row<DT>(p.y, y0 + at, 0, left, y);
+                store_row<DT>(p.y, y0 + pairs + at, 0, left, z);
+            }
+        }
+    }
+}
+
+inline int bits_for(int n) { int b = 0; while ((1 << b) < n) ++b; return b; }
+
+template <int DT, bool IL> hipError_t launch_rotary_as(const RotaryArg &a, hipStream_t st)
+{
+    const int turned = ((IL ? a.part : a.part / 2) + V - 1) / V, copied = a.x == a.y ? 0 : (a.D - a.part + V - 1) / V;
+    const int lane_bits = std::min(8, bits_for(turned + copied)), head_bits = std::min(8 - lane_bits, bits_for(a.H)), tokens = 256 >> (lane_bits + head_bits);
+    const int64_t wgs = (a.B * a.T + tokens - 1) / tokens;
+    if (wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
+    rotary_kernel<DT, IL><<<dim3(grid_row(wgs), grid_rows(wgs)), dim3(256), (size_t)tokens * (a.part / 2) * sizeof(float2), st>>>(a, lane_bits, head_bits, turned, copied);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArg &a, hipStream_t st)
+{
+    if (a.dt == NM_DT_BF16) return a.interleaved ? launch_rotary_as<NM_DT_BF16, true>(a, st) : launch_rotary_as<NM_DT_BF16, false>(a, st);
+    return a.interleaved ? launch_rotary_as<NM_DT_F32, true>(a, st) : launch_rotary_as<NM_DT_F32, false>(a, st);
+}
+
+}  // namespace nm
