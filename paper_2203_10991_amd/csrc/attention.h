@@ -58,41 +58,58 @@ __device__ __forceinline__ void mma(f32x16 &d, const Frag<NM_DT_F32> &a, const F
     for (int j = 0; j < 8; ++j) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], d, 0, 0, 0);
 }
 
-// A fragment of rows r0 .. r0 + 31 and elements 16 kk .. 16 kk + 15 (here k in its plain order)
-template <int DT, int BLOCKS> __device__ __forceinline__ Frag<DT> row_fragment(const char *tile, int r0, int kk, int lane)
-{
-    typedef Tile<DT, BLOCKS> L;
-    const int r = r0 + (lane & 31), hi = lane >> 5;
-    Frag<DT> f;
-    if constexpr (DT == NM_DT_BF16) f.v = *(const bf16x8 *)(tile + L::at(r, 2 * kk + hi));
-    else {
-        const f32x4 a = *(const f32x4 *)(tile + L::at(r, 4 * kk + 2 * hi)), b = *(const f32x4 *)(tile + L::at(r, 4 * kk + 2 * hi + 1));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { f.v[j] = a[j]; f.v[4 + j] = b[j]; }
-    }
-    return f;
-}
+// Where a lane's fragments lie in LDS: the turns of rows and chunks are exclusive-ors, so the address of row r + r', chunk c + c' is the lane's own (r, c) with
+// (c' ^ turn(r')) << 4 turned in, plus r' rows, as long as no bits meet.  Two registers and an exclusive-or before a read then take the place of a register for every
+// read, which the kernels do not have: held in registers, addresses of 128-element heads made 27 to 45 spills in the dk dv kernel, whose reloads wait for the tiles on
+// their way (2 x 8192 tokens, 64 heads over 8: 8.1 to 12.8 ms).
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const lds_char *)p; }
+template <typename T> __device__ __forceinline__ T lds_read(uint32_t at) { return *(const __attribute__((address_space(3))) T *)(uintptr_t)at; }
 
-// A fragment of the transposed tile: elements 32 b .. 32 b + 31 as its rows, the tile's rows r0 .. r0 + 15 as k in the slots' order
-template <int DT, int BLOCKS> __device__ __forceinline__ Frag<DT> column_fragment(const char *tile, int r0, int b, int lane)
-{
+template <int DT, int BLOCKS> struct Lane {
     typedef Tile<DT, BLOCKS> L;
-    const int hi = lane >> 5;
-    Frag<DT> f;
-    if constexpr (DT == NM_DT_BF16) {
-        // 16 lanes bring 4 rows x 16 elements, 8 bytes each, and get an element's 4 rows each
-        const int r = r0 + 4 * hi + (lane >> 2 & 3), c = 4 * b + (lane >> 4 & 1) * 2 + (lane >> 1 & 1), within = (lane & 1) * 8;
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + L::at(r, c) + within));
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + L::at(r + 8, c) + within));
-        f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-        const int e = lane & 31, c = 8 * b + (e >> 2);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f.v[j] = *(const float *)(tile + L::at(r0 + 8 * (j >> 2) + 4 * hi + (j & 3), c) + (e & 3) * 4);
+    uint32_t row, col;               // relative to a tile
+    __device__ __forceinline__ Lane(int lane)
+    {
+        const int hi = lane >> 5, e = lane & 31;
+        row = (uint32_t)L::at(e, DT == NM_DT_BF16 ? hi : 2 * hi);
+        // bf16: 16 lanes bring 4 rows x 16 elements, 8 bytes each, and get an element's 4 rows each
+        if constexpr (DT == NM_DT_BF16) col = (uint32_t)(L::at(4 * hi + (lane >> 2 & 3), (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) + (lane & 1) * 8);
+        else col = (uint32_t)(L::at(4 * hi, e >> 2) + (e & 3) * 4);
     }
-    return f;
-}
+    static __device__ __forceinline__ uint32_t moved(uint32_t at, int r, int c) { return (at ^ (uint32_t)((c ^ L::turn(r)) << 4)) + (uint32_t)(r * L::ROW); }
+    // the addresses in a tile, as the compiler shall not know them from the last tile's
+    __device__ __forceinline__ uint32_t rows_of(uint32_t tile) const { uint32_t at = tile + row; asm volatile("" : "+v"(at)); return at; }
+    __device__ __forceinline__ uint32_t columns_of(uint32_t tile) const { uint32_t at = tile + col; asm volatile("" : "+v"(at)); return at; }
+
+    // A fragment of rows r0 .. r0 + 31 (r0 a multiple of 32) and elements 16 kk .. 16 kk + 15 (here k in its plain order); from: rows_of(tile)
+    static __device__ __forceinline__ Frag<DT> rows(uint32_t from, int r0, int kk)
+    {
+        Frag<DT> f;
+        if constexpr (DT == NM_DT_BF16) f.v = lds_read<bf16x8>(moved(from, r0, 2 * kk));
+        else {
+            const f32x4 a = lds_read<f32x4>(moved(from, r0, 4 * kk)), b = lds_read<f32x4>(moved(from, r0, 4 * kk + 1));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { f.v[j] = a[j]; f.v[4 + j] = b[j]; }
+        }
+        return f;
+    }
+    // A fragment of the transposed tile: elements 32 b .. 32 b + 31 as its rows, the tile's rows r0 .. r0 + 15 (r0 a multiple of 16) as k in the slots' order
+    static __device__ __forceinline__ Frag<DT> columns(uint32_t from, int r0, int b)
+    {
+        Frag<DT> f;
+        if constexpr (DT == NM_DT_BF16) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)moved(from, r0, 4 * b));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)moved(from, r0 + 8, 4 * b));
+            f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f.v[j] = lds_read<float>(moved(from, r0 + 8 * (j >> 2) + (j & 3), 8 * b));
+        }
+        return f;
+    }
+};
 
 // eight values of a D block as a B fragment.  bf16: probabilities and their gradients are rounded to the operands' own type for the second product, to nearest; sums of
 // probabilities take them before that
@@ -122,7 +139,7 @@ struct Sequence {
     int b, h, nq, nk;
     __device__ __forceinline__ Sequence(const AttnArg &p, int bh)
     {
-        b = bh / p.Hk; h = bh - b * p.Hk;
+        b = (int)((uint32_t)bh / (uint32_t)p.Hk); h = bh - b * p.Hk;
         // (lengths outside the tensors count as the nearest inside)
         nq = p.q_lens ? min(max(p.q_lens[b], 0), p.Tq) : p.Tq;
         nk = p.k_lens ? min(max(p.k_lens[b], 0), p.Tk) : p.Tk;
@@ -131,11 +148,14 @@ struct Sequence {
     __device__ __forceinline__ int seen(const AttnArg &p, int i) const { return p.causal ? max(0, min(nk, i + 1 + nk - nq)) : nk; }
 };
 // Workgroups go round-robin to the XCDs; each XCD takes a run of the list, so that the workgroups that read the same keys and values share an L2.
-__device__ __forceinline__ int64_t place_of(int64_t id, int64_t n)
+__device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t n)
 {
-    const int64_t x = id % 8;
+    const uint32_t x = id % 8;
     return x * (n / 8) + min(x, n % 8) + id / 8;
 }
+
+// the first of part k of n parts of some tiles (2^26 at most)
+__device__ __forceinline__ int part_of(int tiles, int k, int n) { return n == 1 ? k * tiles : k * (tiles / n) + min(k, tiles % n); }
 
 __device__ __forceinline__ const char *row_at(const void *p, const AttnStride &s, int64_t b, int64_t t, int64_t h, int es) { return (const char *)p + (b * s.b + t * s.t + h * s.h) * es; }
 
@@ -167,23 +187,24 @@ template <int DT, int BLOCKS, int ROWS, int THREADS> struct Stage {
     typedef Tile<DT, BLOCKS> L;
     static constexpr int PIECES = ROWS * L::USED, N = (PIECES + THREADS - 1) / THREADS;
     u32x4 v[N];
-    // at(row): the row's address; rows `from` .. rows - 1 of the tile are there, rows > 0
-    template <typename At> __device__ __forceinline__ void load(const At &at, int rows, int D, int from = 0)
+    // at(row): the row's address; rows `from` .. rows - 1 of the tile are there, rows > 0.  What is not there is read from a row that is, and left out by store: a choice
+    // made here would wait for the loads.
+    template <typename At> __device__ __forceinline__ void load(const At &at, int rows, int D)
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int piece = (int)threadIdx.x + n * THREADS, r = piece / L::USED, c = piece % L::USED;
+            v[n] = *(const u32x4 *)(at(min(r, rows - 1)) + (c * L::EC < D ? c : 0) * 16);
+        }
+    }
+    __device__ __forceinline__ void store(char *tile, int rows, int D, int from = 0) const
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int piece = (int)threadIdx.x + n * THREADS, r = piece / L::USED, c = piece % L::USED;
             const bool ok = r < rows && r >= from && c * L::EC < D;
-            v[n] = *(const u32x4 *)(at(min(r, rows - 1)) + (ok ? c : 0) * 16);
-            if (!ok) v[n] = u32x4{0, 0, 0, 0};
-        }
-    }
-    __device__ __forceinline__ void store(char *tile) const
-    {
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int piece = (int)threadIdx.x + n * THREADS, r = piece / L::USED, c = piece % L::USED;
-            if (PIECES % THREADS == 0 || piece < PIECES) *(u32x4 *)(tile + L::at(r, c)) = v[n];
+            const u32x4 w = {ok ? v[n][0] : 0u, ok ? v[n][1] : 0u, ok ? v[n][2] : 0u, ok ? v[n][3] : 0u};
+            if (PIECES % THREADS == 0 || piece < PIECES) *(u32x4 *)(tile + L::at(r, c)) = w;
         }
     }
 };

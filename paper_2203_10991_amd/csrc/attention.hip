@@ -26,9 +26,9 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
     __shared__ __align__(16) char lds[2][2][KEYS * L::ROW];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
     // the tiles of a head side by side, those with most keys first
-    const int64_t place = place_of(blockIdx.x, gridDim.x);
-    const int tile = row_tiles - 1 - (int)(place / p.splits % row_tiles), split = (int)(place % p.splits);
-    const Sequence s(p, (int)(place / p.splits / row_tiles));
+    const uint32_t place = place_of(blockIdx.x, gridDim.x), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)row_tiles;
+    const int tile = row_tiles - 1 - (int)(whole - bh * row_tiles), split = (int)(place - whole * p.splits);
+    const Sequence s(p, (int)bh);
     const int total = p.Tq * p.group, r0 = tile * ROWS;
     const int row = r0 + wave * 32 + (lane & 31), query = query_of(min(row, total - 1), p), head = s.h * p.group + min(row, total - 1) - query * p.group;
     const bool there = row < total && query < s.nq;
@@ -39,15 +39,7 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
     const int wave_most = r0 + wave * 32 >= total || wave_first >= s.nq ? 0 : s.seen(p, min(wave_last, s.nq - 1)), wave_least = s.seen(p, wave_first);
     const int seen = s.seen(p, query);
     const int tiles = (most + KEYS - 1) / KEYS;
-    const int first_tile = (int)((int64_t)tiles * split / p.splits), end_tile = (int)((int64_t)tiles * (split + 1) / p.splits);
-
-    Frag<DT> q[2 * BLOCKS];
-    load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
-    f32x16 o[BLOCKS];
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) o[b] = f32x16{};
-    float m = -INFINITY, sum = 0.0f;
-    const float c = p.scale * LOG2E;
+    const int first_tile = part_of(tiles, split, p.splits), end_tile = part_of(tiles, split + 1, p.splits);
 
     const char *k0 = row_at(p.k, p.sk, s.b, 0, s.h, ES), *v0 = row_at(p.v, p.sv, s.b, 0, s.h, ES);
     Stage<DT, BLOCKS, KEYS, THREADS> ks, vs;
@@ -57,14 +49,25 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
         ks.load([&](int r) { return k0 + (key0 + r) * p.sk.t * ES; }, rows, p.D);
         vs.load([&](int r) { return v0 + (key0 + r) * p.sv.t * ES; }, rows, p.D);
     };
-    if (first_tile < end_tile) {
-        load(first_tile);
-        ks.store(lds[0][0]);
-        vs.store(lds[0][1]);
-    }
+    auto store = [&](int t, int to) {
+        const int rows = min(KEYS, s.nk - t * KEYS);
+        ks.store(lds[to][0], rows, p.D);
+        vs.store(lds[to][1], rows, p.D);
+    };
+    if (first_tile < end_tile) load(first_tile);
+    Frag<DT> q[2 * BLOCKS];
+    load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
+    f32x16 o[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) o[b] = f32x16{};
+    float m = -INFINITY, sum = 0.0f;
+    const float c = p.scale * LOG2E;
+    const Lane<DT, BLOCKS> at_lane(lane);
+    typedef Lane<DT, BLOCKS> F;
+    if (first_tile < end_tile) store(first_tile, 0);
     __syncthreads();
     for (int t = first_tile; t < end_tile; ++t) {
-        const char *kt = lds[t - first_tile & 1][0], *vt = lds[t - first_tile & 1][1];
+        const uint32_t kt = at_lane.rows_of(lds_address(lds[t - first_tile & 1][0])), vt = at_lane.columns_of(lds_address(lds[t - first_tile & 1][1]));
         if (t + 1 < end_tile) load(t + 1);
         if (t * KEYS < wave_most) {
             f32x16 x[SB];
@@ -72,7 +75,7 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
             for (int a = 0; a < SB; ++a) {
                 x[a] = f32x16{};
 #pragma unroll
-                for (int kk = 0; kk < 2 * BLOCKS; ++kk) mma(x[a], row_fragment<DT, BLOCKS>(kt, 32 * a, kk, lane), q[kk]);
+                for (int kk = 0; kk < 2 * BLOCKS; ++kk) mma(x[a], F::rows(kt, 32 * a, kk), q[kk]);
             }
             if ((t + 1) * KEYS > wave_least) {
 #pragma unroll
@@ -111,13 +114,10 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
                 for (int g = 0; g < 2; ++g) {
                     const Frag<DT> w = as_fragment<DT>(x[a], 8 * g);
 #pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b) mma(o[b], column_fragment<DT, BLOCKS>(vt, 32 * a + 16 * g, b, lane), w);
+                    for (int b = 0; b < BLOCKS; ++b) mma(o[b], F::columns(vt, 32 * a + 16 * g, b), w);
                 }
         }
-        if (t + 1 < end_tile) {
-            ks.store(lds[(t - first_tile & 1) ^ 1][0]);
-            vs.store(lds[(t - first_tile & 1) ^ 1][1]);
-        }
+        if (t + 1 < end_tile) store(t + 1, (t - first_tile & 1) ^ 1);
         __syncthreads();
     }
     sum += other_half(sum);

@@ -24,9 +24,9 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     constexpr int ES = L::ES, ROWS = 128, SB = KEYS / 32;
     __shared__ __align__(16) char lds[2][2][KEYS * L::ROW];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
-    const int64_t place = place_of(blockIdx.x, gridDim.x);
-    const int tile = row_tiles - 1 - (int)(place % row_tiles);
-    const Sequence s(p, (int)(place / row_tiles));
+    const uint32_t place = place_of(blockIdx.x, gridDim.x), bh = place / (uint32_t)row_tiles;
+    const int tile = row_tiles - 1 - (int)(place - bh * row_tiles);
+    const Sequence s(p, (int)bh);
     const int total = p.Tq * p.group, r0 = tile * ROWS;
     const int row = r0 + wave * 32 + (lane & 31), query = query_of(min(row, total - 1), p), head = s.h * p.group + min(row, total - 1) - query * p.group;
     const bool there = row < total && query < s.nq;
@@ -37,6 +37,20 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     const int seen = s.seen(p, query), tiles = (most + KEYS - 1) / KEYS;
     const int64_t at = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
 
+    const char *k0 = row_at(p.k, p.sk, s.b, 0, s.h, ES), *v0 = row_at(p.v, p.sv, s.b, 0, s.h, ES);
+    Stage<DT, BLOCKS, KEYS, 256> ks, vs;
+    auto load = [&](int t) {
+        const int64_t key0 = (int64_t)t * KEYS;
+        const int rows = min(KEYS, s.nk - t * KEYS);
+        ks.load([&](int r) { return k0 + (key0 + r) * p.sk.t * ES; }, rows, p.D);
+        vs.load([&](int r) { return v0 + (key0 + r) * p.sv.t * ES; }, rows, p.D);
+    };
+    auto store = [&](int t) {
+        const int rows = min(KEYS, s.nk - t * KEYS);
+        ks.store(lds[t & 1][0], rows, p.D);
+        vs.store(lds[t & 1][1], rows, p.D);
+    };
+    if (tiles > 0) load(0);
     Frag<DT> q[2 * BLOCKS], g[2 * BLOCKS];
     load_fragments<DT, BLOCKS>(g, row_at(p.o, p.so, s.b, query, head, ES), there, p.D, lane);
     load_fragments<DT, BLOCKS>(q, row_at(p.g, p.sg, s.b, query, head, ES), there, p.D, lane);
@@ -56,62 +70,39 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) dq[b] = f32x16{};
 
-    const char *k0 = row_at(p.k, p.sk, s.b, 0, s.h, ES), *v0 = row_at(p.v, p.sv, s.b, 0, s.h, ES);
-    Stage<DT, BLOCKS, KEYS, 256> ks, vs;
-    auto load = [&](int t) {
-        const int64_t key0 = (int64_t)t * KEYS;
-        const int rows = min(KEYS, s.nk - t * KEYS);
-        ks.load([&](int r) { return k0 + (key0 + r) * p.sk.t * ES; }, rows, p.D);
-        vs.load([&](int r) { return v0 + (key0 + r) * p.sv.t * ES; }, rows, p.D);
-    };
-    if (tiles > 0) {
-        load(0);
-        ks.store(lds[0][0]);
-        vs.store(lds[0][1]);
-    }
+    const Lane<DT, BLOCKS> at_lane(lane);
+    typedef Lane<DT, BLOCKS> F;
+    if (tiles > 0) store(0);
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
-        const char *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+        const uint32_t kt = at_lane.rows_of(lds_address(lds[t & 1][0])), vt = at_lane.rows_of(lds_address(lds[t & 1][1])), kc = at_lane.columns_of(lds_address(lds[t & 1][0]));
         if (t + 1 < tiles) load(t + 1);
         if (t * KEYS < wave_most) {
-            f32x16 x[SB], dp[SB];
-#pragma unroll
-            for (int a = 0; a < SB; ++a) {
-                x[a] = dp[a] = f32x16{};
-#pragma unroll
-                for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
-                    mma(x[a], row_fragment<DT, BLOCKS>(kt, 32 * a, kk, lane), q[kk]);
-                    mma(dp[a], row_fragment<DT, BLOCKS>(vt, 32 * a, kk, lane), g[kk]);
-                }
-            }
             const bool edge = (t + 1) * KEYS > wave_least;
 #pragma unroll
-            for (int a = 0; a < SB; ++a)
+            for (int a = 0; a < SB; ++a) {
+                f32x16 x = f32x16{}, dp = f32x16{};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float w = exp2_of(__builtin_fmaf(x[a][i], c, -lse));
-                    x[a][i] = w * (dp[a][i] - delta);
+                for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+                    mma(x, F::rows(kt, 32 * a, kk), q[kk]);
+                    mma(dp, F::rows(vt, 32 * a, kk), g[kk]);
                 }
-            if (edge) {
 #pragma unroll
-                for (int a = 0; a < SB; ++a)
+                for (int i = 0; i < 16; ++i) x[i] = exp2_of(__builtin_fmaf(x[i], c, -lse)) * (dp[i] - delta);
+                if (edge) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (t * KEYS + 32 * a + row_of(i, hi) >= seen) x[a][i] = 0.0f;
-            }
-#pragma unroll
-            for (int a = 0; a < SB; ++a)
+                        if (t * KEYS + 32 * a + row_of(i, hi) >= seen) x[i] = 0.0f;
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const Frag<DT> w = as_fragment<DT>(x[a], 8 * h);
+                    const Frag<DT> w = as_fragment<DT>(x, 8 * h);
 #pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b) mma(dq[b], column_fragment<DT, BLOCKS>(kt, 32 * a + 16 * h, b, lane), w);
+                    for (int b = 0; b < BLOCKS; ++b) mma(dq[b], F::columns(kc, 32 * a + 16 * h, b), w);
                 }
+            }
         }
-        if (t + 1 < tiles) {
-            ks.store(lds[(t & 1) ^ 1][0]);
-            vs.store(lds[(t & 1) ^ 1][1]);
-        }
+        if (t + 1 < tiles) store(t + 1);
         __syncthreads();
     }
     if (!there)
@@ -120,74 +111,82 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     if (row < total) store_column<DT, BLOCKS>((char *)row_at(p.dq, p.sdq, s.b, query, head, ES), dq, p.scale, p.D, lane);
 }
 
-template <int DT, int BLOCKS, int ROWS>
-__global__ __launch_bounds__(256, DT == NM_DT_F32 || BLOCKS > 2 ? 1 : 2) void attention_dkdv_kernel(const AttnArg p, int key_tiles)
+template <int DT, int BLOCKS, int ROWS, int WAVES, int PER_SIMD, bool VL>
+__global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(const AttnArg p, int key_tiles)
 {
     typedef Tile<DT, BLOCKS> L;
-    constexpr int ES = L::ES, KEYS = 128, SB = ROWS / 32;
+    typedef Lane<DT, BLOCKS> F;
+    constexpr int ES = L::ES, KEYS = 32 * WAVES, SB = ROWS / 32, THREADS = 64 * WAVES;
+    constexpr uint32_t G = ROWS * L::ROW;                                // from q's tile to g's
     __shared__ __align__(16) char lds[2][2][ROWS * L::ROW];
+    __shared__ __align__(16) char v_lds[VL ? KEYS * L::ROW : 16];
     __shared__ float lse_of[2][ROWS], delta_of[2][ROWS];
     __shared__ int seen_of[2][ROWS];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
-    const int64_t place = place_of(blockIdx.x, gridDim.x);
-    const int tile = (int)(place / p.splits % key_tiles), split = (int)(place % p.splits);       // (the first keys have most rows)
-    const Sequence s(p, (int)(place / p.splits / key_tiles));
+    const uint32_t place = place_of(blockIdx.x, gridDim.x), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)key_tiles;
+    const int tile = (int)(whole - bh * key_tiles), split = (int)(place - whole * p.splits);       // (the first keys have most rows)
+    const Sequence s(p, (int)bh);
     const int key0 = tile * KEYS, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
-    const bool there = key < s.nk;
     // rows that see any of the keys: those of queries from first_query on
     const int total = s.nq * p.group, first_query = p.causal ? max(0, key0 - (s.nk - s.nq)) : 0;
     const int first = min((int64_t)total, (int64_t)first_query * p.group) / ROWS, tiles = key0 < s.nk ? max(0, (total + ROWS - 1) / ROWS - first) : 0;
-    const int first_tile = first + (int)((int64_t)tiles * split / p.splits), end_tile = first + (int)((int64_t)tiles * (split + 1) / p.splits);
-
-    Frag<DT> k[2 * BLOCKS], v[2 * BLOCKS];
-    const int safe_key = min(key, p.Tk - 1);
-    load_fragments<DT, BLOCKS>(k, row_at(p.k, p.sk, s.b, safe_key, s.h, ES), there, p.D, lane);
-    load_fragments<DT, BLOCKS>(v, row_at(p.v, p.sv, s.b, safe_key, s.h, ES), there, p.D, lane);
-    f32x16 dk[BLOCKS], dv[BLOCKS];
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) dk[b] = dv[b] = f32x16{};
-    const float c = p.scale * LOG2E;
+    const int first_tile = first + part_of(tiles, split, p.splits), end_tile = first + part_of(tiles, split + 1, p.splits);
     const int blind = p.causal ? max(0, s.nq - s.nk) * p.group : 0;       // rows that see nothing: what their q and g hold does not count
 
     const char *q0 = row_at(p.q, p.sq, s.b, 0, s.h * p.group, ES), *g0 = row_at(p.g, p.sg, s.b, 0, s.h * p.group, ES);
-    Stage<DT, BLOCKS, ROWS, 256> qs, gs;
+    Stage<DT, BLOCKS, ROWS, THREADS> qs, gs;
     float lse_next = 0.0f, delta_next = 0.0f;
-    int seen_next = 0;
     auto load = [&](int t) {
         const int r0 = t * ROWS, rows = min(ROWS, total - r0);
         auto at = [&](const char *from, const AttnStride &st, int r) {
             const int query = query_of(r0 + r, p);
             return from + (query * st.t + (r0 + r - query * p.group) * st.h) * ES;
         };
-        qs.load([&](int r) { return at(q0, p.sq, r); }, rows, p.D, blind - r0);
-        gs.load([&](int r) { return at(g0, p.sg, r); }, rows, p.D, blind - r0);
+        qs.load([&](int r) { return at(q0, p.sq, r); }, rows, p.D);
+        gs.load([&](int r) { return at(g0, p.sg, r); }, rows, p.D);
         if ((int)threadIdx.x < ROWS) {
             const int r = r0 + min((int)threadIdx.x, rows - 1), query = query_of(r, p), head = s.h * p.group + r - query * p.group;
             const int64_t where = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
-            const bool ok = (int)threadIdx.x < rows;
-            const float l = p.lse[where];
-            lse_next = ok && l != -INFINITY ? l * LOG2E : INFINITY;       // (P = 0)
-            delta_next = ok ? p.delta[where] : 0.0f;
-            seen_next = ok ? s.seen(p, query) : 0;
+            lse_next = p.lse[where];
+            delta_next = p.delta[where];
         }
     };
-    auto store = [&](int to) {
-        qs.store(lds[to][0]);
-        gs.store(lds[to][1]);
+    auto store = [&](int t, int to) {
+        const int r0 = t * ROWS, rows = min(ROWS, total - r0);
+        qs.store(lds[to][0], rows, p.D, blind - r0);
+        gs.store(lds[to][1], rows, p.D, blind - r0);
         if ((int)threadIdx.x < ROWS) {
-            lse_of[to][threadIdx.x] = lse_next;
-            delta_of[to][threadIdx.x] = delta_next;
-            seen_of[to][threadIdx.x] = seen_next;
+            const bool ok = (int)threadIdx.x < rows;
+            lse_of[to][threadIdx.x] = ok && lse_next != -INFINITY ? lse_next * LOG2E : INFINITY;        // (P = 0)
+            delta_of[to][threadIdx.x] = ok ? delta_next : 0.0f;
+            seen_of[to][threadIdx.x] = ok ? s.seen(p, query_of(r0 + (int)threadIdx.x, p)) : 0;
         }
     };
+    Frag<DT> k[2 * BLOCKS], v[VL ? 1 : 2 * BLOCKS];
+    f32x16 dk[BLOCKS], dv[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) dk[b] = dv[b] = f32x16{};
     if (first_tile < end_tile) {
+        const int safe_key = min(key, s.nk - 1);
         load(first_tile);
-        store(0);
+        load_fragments<DT, BLOCKS>(k, row_at(p.k, p.sk, s.b, safe_key, s.h, ES), key < s.nk, p.D, lane);
+        if constexpr (VL) {
+            const char *v0 = row_at(p.v, p.sv, s.b, key0, s.h, ES);
+            const int rows = min(KEYS, s.nk - key0);
+            Stage<DT, BLOCKS, KEYS, THREADS> vs;
+            vs.load([&](int r) { return v0 + r * p.sv.t * ES; }, rows, p.D);
+            vs.store(v_lds, rows, p.D);
+        } else load_fragments<DT, BLOCKS>(v, row_at(p.v, p.sv, s.b, safe_key, s.h, ES), key < s.nk, p.D, lane);
+        store(first_tile, 0);
     }
+    const float c = p.scale * LOG2E;
+    const F at_lane(lane);
     __syncthreads();
     for (int t = first_tile; t < end_tile; ++t) {
         const int buf = t - first_tile & 1;
-        const char *qt = lds[buf][0], *gt = lds[buf][1];
+        // (one register for the rows of both tiles and one for their columns: the second tile is a constant away)
+        [[maybe_unused]] const uint32_t v_rows = VL ? at_lane.rows_of(lds_address(v_lds) + (uint32_t)(wave * 32 * L::ROW)) : 0u;
+        const uint32_t rows = at_lane.rows_of(lds_address(lds[buf][0])), columns = at_lane.columns_of(lds_address(lds[buf][0]));
         if (t + 1 < end_tile) load(t + 1);
         // the tile's last row sees most keys, its first one fewest
         const int tile_most = s.seen(p, query_of(min(t * ROWS + ROWS, total) - 1, p)), tile_least = s.seen(p, query_of(t * ROWS, p));
@@ -198,8 +197,9 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 || BLOCKS > 2 ? 1 : 2) void at
                 f32x16 x = f32x16{}, dp = f32x16{};
 #pragma unroll
                 for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
-                    mma(x, row_fragment<DT, BLOCKS>(qt, 32 * a, kk, lane), k[kk]);
-                    mma(dp, row_fragment<DT, BLOCKS>(gt, 32 * a, kk, lane), v[kk]);
+                    mma(x, F::rows(rows, 32 * a, kk), k[kk]);
+                    if constexpr (VL) mma(dp, F::rows(rows + G, 32 * a, kk), F::rows(v_rows, 0, kk));
+                    else mma(dp, F::rows(rows + G, 32 * a, kk), v[kk]);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
@@ -208,25 +208,29 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 || BLOCKS > 2 ? 1 : 2) void at
                     for (int j = 0; j < 4; ++j) {
                         x[i + j] = exp2_of(__builtin_fmaf(x[i + j], c, -l[j]));
                         dp[i + j] = x[i + j] * (dp[i + j] - d[j]);
-                        if (edge && key >= seen_of[buf][32 * a + row_of(i + j, hi)]) x[i + j] = dp[i + j] = 0.0f;
                     }
+                }
+                if (edge) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (key >= seen_of[buf][32 * a + row_of(i, hi)]) x[i] = dp[i] = 0.0f;
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const Frag<DT> w = as_fragment<DT>(x, 8 * h), ds = as_fragment<DT>(dp, 8 * h);
 #pragma unroll
                     for (int b = 0; b < BLOCKS; ++b) {
-                        mma(dv[b], column_fragment<DT, BLOCKS>(gt, 32 * a + 16 * h, b, lane), w);
-                        mma(dk[b], column_fragment<DT, BLOCKS>(qt, 32 * a + 16 * h, b, lane), ds);
+                        mma(dv[b], F::columns(columns + G, 32 * a + 16 * h, b), w);
+                        mma(dk[b], F::columns(columns, 32 * a + 16 * h, b), ds);
                     }
                 }
             }
         }
-        if (t + 1 < end_tile) store(buf ^ 1);
+        if (t + 1 < end_tile) store(t + 1, buf ^ 1);
         __syncthreads();
     }
     if (key >= p.Tk) return;
-    if (!there)                                                          // (what stands in the columns of keys that are not there)
+    if (key >= s.nk)                                                     // (what stands in the columns of keys that are not there)
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) dk[b] = dv[b] = f32x16{};
     if (p.splits == 1) {
@@ -259,7 +263,19 @@ template <int DT> __global__ __launch_bounds__(256) void attention_sum_kernel(co
     else *(f32x4 *)(to + e * 4) = x;
 }
 
-inline int64_t key_tiles(const AttnArg &a) { return ((int64_t)a.Tk + 127) / 128; }
+// Waves of a workgroup of the dk dv kernel, waves to a SIMD, rows of a tile, and whether v's fragments come from LDS each time instead of staying in registers.
+// In bf16: 128 elements to a head have 128 registers of sums; with v in LDS the rest fits two waves to a SIMD (2 x 8192 tokens, 64 heads over 8: one wave with everything in
+// registers 8.1 ms, four waves 5.1, eight 4.6), with 64 three fit (32 x 512 tokens, 16 heads: 105 -> 94 us).
+template <int DT, int BLOCKS> struct KeyShape { static constexpr int waves = 4, per_simd = DT == NM_DT_F32 ? 1 : 2, rows = 32; static constexpr bool v_in_lds = false; };
+template <> struct KeyShape<NM_DT_BF16, 2> { static constexpr int waves = 4, per_simd = 3, rows = 32; static constexpr bool v_in_lds = true; };
+template <> struct KeyShape<NM_DT_BF16, 3> { static constexpr int waves = 8, per_simd = 2, rows = 32; static constexpr bool v_in_lds = true; };
+template <> struct KeyShape<NM_DT_BF16, 4> { static constexpr int waves = 8, per_simd = 2, rows = 32; static constexpr bool v_in_lds = true; };
+inline int keys_to_workgroup(const AttnArg &a)
+{
+    if (a.dt != NM_DT_BF16) return 32 * KeyShape<NM_DT_F32, 1>::waves;
+    return 32 * (a.D > 96 ? KeyShape<NM_DT_BF16, 4>::waves : a.D > 64 ? KeyShape<NM_DT_BF16, 3>::waves : KeyShape<NM_DT_BF16, 2>::waves);
+}
+inline int64_t key_tiles(const AttnArg &a) { return ((int64_t)a.Tk + keys_to_workgroup(a) - 1) / keys_to_workgroup(a); }
 inline int key_splits(const AttnArg &a)
 {
     const int64_t wgs = (int64_t)a.B * a.Hk * key_tiles(a), rows = (int64_t)a.Tq * a.group;
@@ -268,14 +284,15 @@ inline int key_splits(const AttnArg &a)
 
 template <int DT, int BLOCKS> hipError_t launch_grads(const AttnArg &a, hipStream_t st)
 {
-    constexpr int KEYS = DT == NM_DT_F32 ? 32 : 64, ROWS = 32;
+    constexpr int KEYS = DT == NM_DT_F32 ? 32 : 64;
+    typedef KeyShape<DT, BLOCKS> W;
     const int64_t heads = (int64_t)a.B * a.Hk, row_tiles = ((int64_t)a.Tq * a.group + 127) / 128, kt = key_tiles(a);
     const int64_t wq = heads * row_tiles, wk = heads * kt * a.splits;
     if (std::max(wq, wk) > 0x7fffffff || !grid_holds(std::max(wq, wk), 256)) return hipErrorInvalidConfiguration;
     if (wq > 0) attention_dq_kernel<DT, BLOCKS, KEYS><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || wk == 0) return e;
-    attention_dkdv_kernel<DT, BLOCKS, ROWS><<<dim3((unsigned)wk), dim3(256), 0, st>>>(a, (int)kt);
+    attention_dkdv_kernel<DT, BLOCKS, W::rows, W::waves, W::per_simd, W::v_in_lds><<<dim3((unsigned)wk), dim3(64 * W::waves), 0, st>>>(a, (int)kt);
     return hipGetLastError();
 }
 
