@@ -151,7 +151,9 @@ def load():
         native.bind({f: C.cast(getattr(lib, f), vp).value for f in (
             "mvue_prune_1of2", "mvue_prune_2of4", "nm_update_gemm", "nm_update_gemm_workspace", "nm_linear_update", "nm_linear_update_workspace",
             "nm_linear_forward", "nm_linear_input_grad", "nm_adamw", "nm_embed", "nm_embed_grad", "nm_embed_grad_workspace",
-            "nm_quant_i8", "nm_quant_i8_t", "nm_quant_i8_t_workspace", "nm_linear_i8", "nm_linear_i8_workspace")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
+            "nm_quant_i8", "nm_quant_i8_t", "nm_quant_i8_t_workspace", "nm_linear_i8", "nm_linear_i8_workspace",
+            "nm_layer_norm", "nm_layer_norm_grad", "nm_layer_norm_grad_workspace", "nm_rotary", "nm_attention", "nm_attention_workspace",
+            "nm_attention_grad", "nm_attention_grad_workspace")}, _raw_stream or (lambda d: torch.cuda.current_stream(d).cuda_stream))
     except ImportError as e:
         warnings.warn(f"_nm_torch.so is not built for this torch ({e}): every call takes the slower way through ctypes and linear layers take the "
                       "framework's products until `python -m paper_2203_10991_amd.build` has run")
@@ -168,6 +170,7 @@ class _Heads(C.Structure):
 class _NoNative:
     """In the place of _nm_torch: no call is its own."""
     prune = update_gemm = linear_update = linear_forward = linear_input_grad = adamw = embed = embed_grad = quant_i8 = linear_i8 = staticmethod(lambda *a: None)
+    layer_norm = layer_norm_grad = rotary = attention = attention_grad = staticmethod(lambda *a: None)
 
 
 def _native_result(r):
@@ -932,6 +935,9 @@ def nm_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: 
     """(x - mean) / sqrt(variance + eps) * weight + bias over the last dimension (1 to 32768), of x's type; x, weight and bias float32 or bfloat16.
     want_stats: (y, mean, rstd), the last two float32 of x's shape without its last dimension, as nm_layer_norm_grad reads them."""
     lib = load()
+    r = _native_result(_native.layer_norm(x, weight, bias, float(eps), want_stats))
+    if r is not None:
+        return r
     if not x.is_cuda or x.dim() < 1:
         raise ValueError("x is a tensor on the GPU with at least one dimension")
     dt = _dtype_code(x)
@@ -951,6 +957,10 @@ def nm_layer_norm_grad(g: torch.Tensor, x: torch.Tensor, weight: Optional[torch.
     """(dx, dweight, dbias) of nm_layer_norm from the gradient g of its result, its x and weight (None: ones), and the mean and rstd that it left.  dx is of
     x's type, dweight and dbias of weight's (float32 without one); None where not wanted."""
     lib = load()
+    if want_weight and want_bias:
+        r = _native_result(_native.layer_norm_grad(g, x, weight, mean, rstd))
+        if r is not None:
+            return r
     if not x.is_cuda or x.dim() < 1 or g.shape != x.shape or g.dtype != x.dtype or g.device != x.device:
         raise ValueError("x and g are tensors of one shape and type on one GPU")
     dt = _dtype_code(x)
@@ -1008,6 +1018,10 @@ def nm_rotary(x: torch.Tensor, freqs: torch.Tensor, positions: Optional[torch.Te
     [batch x length], 0 .. length - 1 without.  Pairs: neighbours where interleaved, otherwise half the turned elements apart.  inverse: turned back, which is the
     gradient with respect to x of the call without it.  out: a tensor for the result, x itself among them."""
     lib = load()
+    if out is None:
+        r = _native_result(_native.rotary(x, freqs, positions, interleaved, float(scale), inverse))
+        if r is not None:
+            return r
     if not x.is_cuda or x.dim() != 4:
         raise ValueError("x is a 4-D tensor on the GPU: batch, length, heads, elements")
     dt = _dtype_code(x)
@@ -1057,6 +1071,10 @@ def _attention_sizes(q, k, v):
     return B, Tq, k.shape[1], Hq, k.shape[2], D
 
 
+def _scale_of(scale: Optional[float], q: torch.Tensor) -> float:
+    return float(scale) if scale is not None else q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
+
+
 def _lengths_of(lens: Optional[torch.Tensor], B: int, device) -> Optional[torch.Tensor]:
     if lens is None:
         return None
@@ -1073,6 +1091,10 @@ def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool
     the front; what lies behind counts for nothing, and the result is zero there, as for a query that sees no key.
     want_lse: (o, lse), lse float32 [batch x heads x queries], the logarithm of the sum of exponentials, which nm_attention_grad reads."""
     lib = load()
+    scale = _scale_of(scale, q)
+    r = _native_result(_native.attention(q, k, v, causal, scale, q_lens, k_lens, want_lse))
+    if r is not None:
+        return r
     q = _attention_input(q, "q")
     k, v = _attention_input(k, "k", q), _attention_input(v, "v", q)
     dt = _dtype_code(q)
@@ -1083,7 +1105,7 @@ def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool
     need = int(lib.nm_attention_workspace(*sizes, dt))
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     with torch.cuda.device(q.device):
-        _check(lib.nm_attention(_heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), D ** -0.5 if scale is None else float(scale), _ptr(ql), _ptr(kl),
+        _check(lib.nm_attention(_heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), scale, _ptr(ql), _ptr(kl),
                                 _ptr(ws), need, _stream(q)))
     return (o, lse) if want_lse else o
 
@@ -1093,6 +1115,11 @@ def nm_attention_grad(g: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torc
     """(dq, dk, dv) of nm_attention from the gradient g of its result o; the other arguments as they were given to it, and the lse that it left.  The probabilities
     are computed again.  The same call gives the same bits.  out: three tensors for the results, of q's, k's and v's shapes, parts of one tensor among them."""
     lib = load()
+    scale = _scale_of(scale, q)
+    if out is None:
+        r = _native_result(_native.attention_grad(g, q, k, v, o, lse, causal, scale, q_lens, k_lens))
+        if r is not None:
+            return r
     q = _attention_input(q, "q")
     k, v, g, o = (_attention_input(t, what, q) for t, what in ((k, "k"), (v, "v"), (g, "g"), (o, "o")))
     dt = _dtype_code(q)
@@ -1113,7 +1140,7 @@ def nm_attention_grad(g: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torc
     need = int(lib.nm_attention_grad_workspace(*sizes, dt))
     ws = torch.empty(need, dtype=torch.uint8, device=q.device)
     with torch.cuda.device(q.device):
-        _check(lib.nm_attention_grad(_heads(g), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), D ** -0.5 if scale is None else float(scale),
+        _check(lib.nm_attention_grad(_heads(g), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), scale,
                                      _ptr(ql), _ptr(kl), _heads(dq), _heads(dk), _heads(dv), _ptr(ws), need, _stream(q)))
     if out is not None:
         torch.autograd.graph.increment_version([t for t in out if not t.is_inference()])

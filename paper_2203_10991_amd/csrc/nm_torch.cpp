@@ -43,6 +43,14 @@ decltype(&nm_linear_i8) p_linear_i8;
 decltype(&nm_linear_i8_workspace) p_linear_i8_workspace;
 decltype(&nm_embed_grad) p_embed_grad;
 decltype(&nm_embed_grad_workspace) p_embed_grad_workspace;
+decltype(&nm_layer_norm) p_layer_norm;
+decltype(&nm_layer_norm_grad) p_layer_norm_grad;
+decltype(&nm_layer_norm_grad_workspace) p_layer_norm_grad_workspace;
+decltype(&nm_rotary) p_rotary;
+decltype(&nm_attention) p_attention;
+decltype(&nm_attention_workspace) p_attention_workspace;
+decltype(&nm_attention_grad) p_attention_grad;
+decltype(&nm_attention_grad_workspace) p_attention_grad_workspace;
 PyObject *stream_of = nullptr;
 
 struct NoGil {                                                       // as a ctypes call does: a launch may wait for the queue
@@ -426,6 +434,211 @@ PyObject *linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- between a block's linear layers
+// the rows of a tensor's last dimension as the norms read them: their stride, or -1
+int64_t last_rows(const at::Tensor &t)
+{
+    if (t.dim() < 1 || t.size(-1) < 1) return -1;
+    return t.dim() == 2 ? distinct_rows(t) : t.is_contiguous() ? t.size(-1) : -1;
+}
+// a vector of C values (or None, nullptr) beside x; false: not the common form
+bool vector_of(PyObject *o, const at::Tensor &x, int64_t C, const at::Tensor *&out)
+{
+    out = o == Py_None ? nullptr : gpu_tensor(o);
+    return o == Py_None || (out && out->dim() == 1 && out->size(0) == C && is_float(*out) && out->is_contiguous() && out->device() == x.device());
+}
+
+// layer_norm(x, weight or None, bias or None, eps, stats) -> y, or (y, mean, rstd)
+PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 5) return none();
+    const at::Tensor *x = gpu_tensor(a[0]), *w, *b;
+    if (!x || !is_float(*x)) return none();
+    const int64_t ld = last_rows(*x);
+    if (ld < 0 || !vector_of(a[1], *x, x->size(-1), w) || !vector_of(a[2], *x, x->size(-1), b) || (w && b && w->scalar_type() != b->scalar_type()) || !on_current_device(*x)) return none();
+    const double eps = PyFloat_AsDouble(a[3]);
+    const int stats = PyObject_IsTrue(a[4]);
+    void *st;
+    if (PyErr_Occurred() || stats < 0 || !stream(*x, st)) return nullptr;
+    const int64_t C = x->size(-1), R = x->numel() / C;
+    at::Tensor y = empty(x->sizes(), x->scalar_type(), *x), mean, rstd;
+    if (stats) {
+        const at::IntArrayRef rows = x->sizes().slice(0, x->dim() - 1);
+        mean = empty(rows, at::kFloat, *x);
+        rstd = empty(rows, at::kFloat, *x);
+    }
+    const void *px = x->data_ptr(), *pw = w ? w->data_ptr() : nullptr, *pb = b ? b->data_ptr() : nullptr;
+    void *py = y.data_ptr();
+    float *pm = stats ? (float *)mean.data_ptr() : nullptr, *pr = stats ? (float *)rstd.data_ptr() : nullptr;
+    const int dt = code_of(x->scalar_type()), wt = w ? code_of(w->scalar_type()) : b ? code_of(b->scalar_type()) : NM_F32;
+    int rc;
+    {
+        NoGil free;
+        rc = p_layer_norm(px, ld, dt, pw, pb, wt, R, C, (float)eps, py, C, pm, pr, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    if (!stats) return THPVariable_Wrap(std::move(y));
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(y)), THPVariable_Wrap(std::move(mean)), THPVariable_Wrap(std::move(rstd)));
+    END_HANDLE_TH_ERRORS
+}
+
+// layer_norm_grad(g, x, weight, mean, rstd) -> (dx, dweight, dbias)
+PyObject *layer_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 5) return none();
+    const at::Tensor *g = gpu_tensor(a[0]), *x = gpu_tensor(a[1]), *w, *mean = gpu_tensor(a[3]), *rstd = gpu_tensor(a[4]);
+    if (!g || !x || !mean || !rstd || !is_float(*x) || g->scalar_type() != x->scalar_type() || g->sizes() != x->sizes() || g->device() != x->device()) return none();
+    const int64_t ldx = last_rows(*x), ldg = last_rows(*g);
+    if (ldx < 0 || ldg < 0 || a[2] == Py_None || !vector_of(a[2], *x, x->size(-1), w) || !on_current_device(*x)) return none();
+    for (const at::Tensor *t : {mean, rstd})
+        if (t->scalar_type() != at::kFloat || t->sizes() != x->sizes().slice(0, x->dim() - 1) || !t->is_contiguous() || t->device() != x->device()) return none();
+    const int64_t C = x->size(-1), R = x->numel() / C;
+    const size_t need = p_layer_norm_grad_workspace(R, C);
+    void *st;
+    if (!stream(*x, st)) return nullptr;
+    at::Tensor dx = empty(x->sizes(), x->scalar_type(), *x), dw = empty({C}, w->scalar_type(), *x), db = empty({C}, w->scalar_type(), *x), ws = empty({(int64_t)need}, at::kByte, *x);
+    const void *pg = g->data_ptr(), *px = x->data_ptr(), *pw = w->data_ptr();
+    const float *pm = (const float *)mean->data_ptr(), *pr = (const float *)rstd->data_ptr();
+    void *pdx = dx.data_ptr(), *pdw = dw.data_ptr(), *pdb = db.data_ptr(), *pk = ws.data_ptr();
+    const int dt = code_of(x->scalar_type()), wt = code_of(w->scalar_type());
+    int rc;
+    {
+        NoGil free;
+        rc = p_layer_norm_grad(pg, ldg, px, ldx, dt, pw, wt, pm, pr, R, C, pdx, C, pdw, pdb, pk, need, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(dx)), THPVariable_Wrap(std::move(dw)), THPVariable_Wrap(std::move(db)));
+    END_HANDLE_TH_ERRORS
+}
+
+nm_heads heads_of(const at::Tensor &t) { return nm_heads{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)}; }
+
+// rotary(x, freqs, positions or None, interleaved, scale, inverse) -> the turned tensor
+PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) return none();
+    const at::Tensor *x = gpu_tensor(a[0]), *f = gpu_tensor(a[1]), *pos = a[2] == Py_None ? nullptr : gpu_tensor(a[2]);
+    if (!x || !f || (a[2] != Py_None && !pos) || !is_float(*x) || x->dim() != 4 || x->stride(3) != 1 || f->scalar_type() != at::kDouble || f->dim() != 1 || !f->is_contiguous() ||
+        f->device() != x->device() || !on_current_device(*x))
+        return none();
+    const int64_t B = x->size(0), T = x->size(1), H = x->size(2), D = x->size(3);
+    int bits = 32;
+    int64_t apart = 0;
+    if (pos) {
+        if ((pos->scalar_type() != at::kInt && pos->scalar_type() != at::kLong) || pos->device() != x->device() || !pos->is_contiguous()) return none();
+        if (pos->dim() == 2 ? pos->size(0) != B || pos->size(1) != T : pos->dim() != 1 || pos->size(0) != T) return none();
+        bits = pos->scalar_type() == at::kLong ? 64 : 32;
+        apart = pos->dim() == 2 ? T : 0;
+    }
+    const int interleaved = PyObject_IsTrue(a[3]), inverse = PyObject_IsTrue(a[5]);
+    const double scale = PyFloat_AsDouble(a[4]);
+    void *st;
+    if (PyErr_Occurred() || interleaved < 0 || inverse < 0 || !stream(*x, st)) return nullptr;
+    at::Tensor y = empty(x->sizes(), x->scalar_type(), *x);
+    const nm_heads from = heads_of(*x), to = heads_of(y);
+    const double *pf = (const double *)f->data_ptr();
+    const void *pp = pos ? pos->data_ptr() : nullptr;
+    const int64_t part = 2 * f->numel();
+    const int dt = code_of(x->scalar_type());
+    int rc;
+    {
+        NoGil free;
+        rc = p_rotary(&from, &to, dt, B, T, H, D, part, pf, pp, bits, apart, interleaved, (float)scale, inverse, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+// a tensor of heads as attention reads it, of q's type and device
+bool heads_tensor(const at::Tensor *t, const at::Tensor *like)
+{
+    if (!t || t->dim() != 4 || !is_float(*t) || t->scalar_type() != like->scalar_type() || t->device() != like->device() || t->stride(3) != 1 || (uintptr_t)t->data_ptr() % 16) return false;
+    const int64_t unit = 16 / (int64_t)t->element_size();
+    for (int i = 0; i < 3; ++i)
+        if (t->size(i) > 1 && t->stride(i) % unit) return false;
+    return true;
+}
+bool lengths_tensor(PyObject *o, const at::Tensor &q, const int32_t *&out)
+{
+    out = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *t = gpu_tensor(o);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != q.size(0) || !t->is_contiguous() || t->device() != q.device()) return false;
+    out = (const int32_t *)t->data_ptr();
+    return true;
+}
+
+// attention(q, k, v, causal, scale, q_lens or None, k_lens or None, lse) -> o, or (o, lse)
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 8) return none();
+    const at::Tensor *q = gpu_tensor(a[0]), *k = gpu_tensor(a[1]), *v = gpu_tensor(a[2]);
+    const int32_t *ql, *kl;
+    if (!q || !heads_tensor(q, q) || !heads_tensor(k, q) || !heads_tensor(v, q) || k->sizes() != v->sizes() || k->size(0) != q->size(0) || k->size(3) != q->size(3) ||
+        !lengths_tensor(a[5], *q, ql) || !lengths_tensor(a[6], *q, kl) || !on_current_device(*q))
+        return none();
+    const int causal = PyObject_IsTrue(a[3]), want = PyObject_IsTrue(a[7]);
+    const double scale = PyFloat_AsDouble(a[4]);
+    void *st;
+    if (PyErr_Occurred() || causal < 0 || want < 0 || !stream(*q, st)) return nullptr;
+    const int64_t B = q->size(0), Tq = q->size(1), Hq = q->size(2), D = q->size(3), Tk = k->size(1), Hk = k->size(2);
+    const int dt = code_of(q->scalar_type());
+    const size_t need = p_attention_workspace(B, Tq, Tk, Hq, Hk, D, dt);
+    at::Tensor o = empty(q->sizes(), q->scalar_type(), *q), lse, ws;
+    if (want) lse = empty({B, Hq, Tq}, at::kFloat, *q);
+    if (need) ws = empty({(int64_t)need}, at::kByte, *q);
+    const nm_heads hq = heads_of(*q), hk = heads_of(*k), hv = heads_of(*v), ho = heads_of(o);
+    float *pl = want ? (float *)lse.data_ptr() : nullptr;
+    void *pw = need ? ws.data_ptr() : nullptr;
+    int rc;
+    {
+        NoGil free;
+        rc = p_attention(&hq, &hk, &hv, &ho, pl, B, Tq, Tk, Hq, Hk, D, dt, causal, (float)scale, ql, kl, pw, need, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    if (!want) return THPVariable_Wrap(std::move(o));
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(o)), THPVariable_Wrap(std::move(lse)));
+    END_HANDLE_TH_ERRORS
+}
+
+// attention_grad(g, q, k, v, o, lse, causal, scale, q_lens or None, k_lens or None) -> (dq, dk, dv)
+PyObject *attention_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 10) return none();
+    const at::Tensor *g = gpu_tensor(a[0]), *q = gpu_tensor(a[1]), *k = gpu_tensor(a[2]), *v = gpu_tensor(a[3]), *o = gpu_tensor(a[4]), *lse = gpu_tensor(a[5]);
+    const int32_t *ql, *kl;
+    if (!q || !heads_tensor(q, q) || !heads_tensor(k, q) || !heads_tensor(v, q) || !heads_tensor(g, q) || !heads_tensor(o, q) || k->sizes() != v->sizes() ||
+        k->size(0) != q->size(0) || k->size(3) != q->size(3) || g->sizes() != q->sizes() || o->sizes() != q->sizes() || !lse || lse->scalar_type() != at::kFloat ||
+        lse->dim() != 3 || lse->size(0) != q->size(0) || lse->size(1) != q->size(2) || lse->size(2) != q->size(1) || !lse->is_contiguous() || lse->device() != q->device() ||
+        !lengths_tensor(a[8], *q, ql) || !lengths_tensor(a[9], *q, kl) || !on_current_device(*q))
+        return none();
+    const int causal = PyObject_IsTrue(a[6]);
+    const double scale = PyFloat_AsDouble(a[7]);
+    void *st;
+    if (PyErr_Occurred() || causal < 0 || !stream(*q, st)) return nullptr;
+    const int64_t B = q->size(0), Tq = q->size(1), Hq = q->size(2), D = q->size(3), Tk = k->size(1), Hk = k->size(2);
+    const int dt = code_of(q->scalar_type());
+    const size_t need = p_attention_grad_workspace(B, Tq, Tk, Hq, Hk, D, dt);
+    at::Tensor dq = empty(q->sizes(), q->scalar_type(), *q), dk = empty(k->sizes(), q->scalar_type(), *q), dv = empty(k->sizes(), q->scalar_type(), *q), ws = empty({(int64_t)need}, at::kByte, *q);
+    const nm_heads hg = heads_of(*g), hq = heads_of(*q), hk = heads_of(*k), hv = heads_of(*v), ho = heads_of(*o), gq = heads_of(dq), gk = heads_of(dk), gv = heads_of(dv);
+    const float *pl = (const float *)lse->data_ptr();
+    void *pw = ws.data_ptr();
+    int rc;
+    {
+        NoGil free;
+        rc = p_attention_grad(&hg, &hq, &hk, &hv, &ho, pl, B, Tq, Tk, Hq, Hk, D, dt, causal, (float)scale, ql, kl, &gq, &gk, &gv, pw, need, st);
+    }
+    if (rc) return PyLong_FromLong(rc);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(dq)), THPVariable_Wrap(std::move(dk)), THPVariable_Wrap(std::move(dv)));
+    END_HANDLE_TH_ERRORS
+}
+
 // ---- adamw(params, grads, ms, vs, masters or None, numbers or None, step, lr, beta1, beta2, eps, weight_decay, grad_scale, grad_scale tensor or None, seed) -> True:
 // the step has been taken.  Lists of one length; one type of parameters, gradients and states, all on one device, a tensor's arrays with one dense layout.
 // A state is a binary32 tensor, or a pair of e4m3 codes and binary32 scales.
@@ -524,7 +737,10 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         {"nm_linear_input_grad", (void **)&p_linear_input_grad}, {"nm_adamw", (void **)&p_adamw}, {"nm_embed", (void **)&p_embed},
         {"nm_embed_grad", (void **)&p_embed_grad}, {"nm_embed_grad_workspace", (void **)&p_embed_grad_workspace},
         {"nm_quant_i8", (void **)&p_quant_i8}, {"nm_quant_i8_t", (void **)&p_quant_i8_t}, {"nm_quant_i8_t_workspace", (void **)&p_quant_i8_t_workspace},
-        {"nm_linear_i8", (void **)&p_linear_i8}, {"nm_linear_i8_workspace", (void **)&p_linear_i8_workspace}};
+        {"nm_linear_i8", (void **)&p_linear_i8}, {"nm_linear_i8_workspace", (void **)&p_linear_i8_workspace},
+        {"nm_layer_norm", (void **)&p_layer_norm}, {"nm_layer_norm_grad", (void **)&p_layer_norm_grad}, {"nm_layer_norm_grad_workspace", (void **)&p_layer_norm_grad_workspace},
+        {"nm_rotary", (void **)&p_rotary}, {"nm_attention", (void **)&p_attention}, {"nm_attention_workspace", (void **)&p_attention_workspace},
+        {"nm_attention_grad", (void **)&p_attention_grad}, {"nm_attention_grad_workspace", (void **)&p_attention_grad_workspace}};
     for (auto &f : all) {
         PyObject *address = PyDict_GetItemString(a[0], f.name);
         if (!address) { PyErr_Format(PyExc_KeyError, "%s", f.name); return nullptr; }
@@ -539,6 +755,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 #define NM_METHOD(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {NM_METHOD(bind), NM_METHOD(prune), NM_METHOD(update_gemm), NM_METHOD(linear_update), NM_METHOD(linear_forward), NM_METHOD(linear_input_grad), NM_METHOD(adamw), NM_METHOD(embed), NM_METHOD(embed_grad), NM_METHOD(quant_i8), NM_METHOD(linear_i8),
+                         NM_METHOD(layer_norm), NM_METHOD(layer_norm_grad), NM_METHOD(rotary), NM_METHOD(attention), NM_METHOD(attention_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_nm_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
