@@ -1,4 +1,4 @@
-"""Linear and Conv2d layers whose UPDATE phase runs through libnm_mvue.
+"""Linear and Conv2d layers whose UPDATE phase runs through libnm_mvue, and what stands around them in a language model: embedding, layer norm, rotary positions, attention.
 
 Only the weight-gradient GEMM dW = g^T h (eq. (3)) sees the pruned gradient; the forward GEMM (eq. (1)) and the
 backward GEMM that propagates g (eq. (2)) are dense, as in the paper (Table 1: the neural-gradient
@@ -372,3 +372,138 @@ class NMEmbedding(torch.nn.Embedding):
 
     def forward(self, ids):
         return _NMEmbeddingFn.apply(self.weight, ids, self.scale, self.padding_idx)
+
+
+class _NMLayerNormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = api.nm_layer_norm(x, weight, bias, eps, want_stats=True)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dx, dw, db = api.nm_layer_norm_grad(gy, x, weight, mean, rstd, want_weight=ctx.needs_input_grad[1], want_bias=ctx.needs_input_grad[2])
+        return dx if ctx.needs_input_grad[0] else None, dw, db, None
+
+
+class NMLayerNorm(torch.nn.LayerNorm):
+    """torch.nn.LayerNorm over the last dimension (1 to 32768) on the library's kernels: a row is read once in each direction, and the sums of the weight's and bias's
+    gradients run in a fixed order."""
+
+    def __init__(self, normalized_shape, eps: float = 1e-5, elementwise_affine: bool = True, bias: bool = True, device=None, dtype=None):
+        super().__init__(normalized_shape, eps=eps, elementwise_affine=elementwise_affine, bias=bias, device=device, dtype=dtype)
+        if len(self.normalized_shape) != 1:
+            raise ValueError("NMLayerNorm is over the last dimension")
+
+    def forward(self, x):
+        if x.shape[-1:] != self.normalized_shape:
+            raise ValueError(f"rows of {self.normalized_shape[0]} expected, got {tuple(x.shape)}")
+        return _NMLayerNormFn.apply(x, self.weight, self.bias, self.eps)
+
+
+class _NMRotaryFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, freqs, positions, interleaved, scale):
+        ctx.save_for_backward(freqs, positions)
+        ctx.how = interleaved, scale
+        return api.nm_rotary(x, freqs, positions, interleaved, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gy):
+        freqs, positions = ctx.saved_tensors
+        return api.nm_rotary(gy, freqs, positions, *ctx.how, inverse=True), None, None, None, None
+
+
+def rotary(x: torch.Tensor, freqs: torch.Tensor, positions: Optional[torch.Tensor] = None, interleaved: bool = False, scale: float = 1.0) -> torch.Tensor:
+    """nm_rotary with a gradient for x."""
+    return _NMRotaryFn.apply(x, freqs, positions, interleaved, scale)
+
+
+class _NMAttentionFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, causal, scale, q_lens, k_lens):
+        o, lse = api.nm_attention(q, k, v, causal, scale, q_lens, k_lens, want_lse=True)
+        ctx.save_for_backward(q, k, v, o, lse, q_lens, k_lens)
+        ctx.how = causal, scale
+        return o
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        q, k, v, o, lse, q_lens, k_lens = ctx.saved_tensors
+        return *api.nm_attention_grad(g, q, k, v, o, lse, *ctx.how, q_lens, k_lens), None, None, None, None
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None, q_lens: Optional[torch.Tensor] = None,
+              k_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nm_attention with gradients for q, k and v, which compute the probabilities again."""
+    return _NMAttentionFn.apply(q, k, v, causal, scale, q_lens, k_lens)
+
+
+class _NMSelfAttentionFn(torch.autograd.Function):
+    """o [B x T x H x D] of the joined projections qkv [B x T x (H + 2 K) x D]: the heads of q and k turned, v and all gradients where they lie in the one tensor."""
+
+    @staticmethod
+    def forward(ctx, qkv, heads, kv_heads, freqs, positions, interleaved, causal, lens):
+        turned = qkv[:, :, :heads + kv_heads]
+        if freqs is not None:
+            turned = api.nm_rotary(turned, freqs, positions, interleaved)
+        o, lse = api.nm_attention(turned[:, :, :heads], turned[:, :, heads:], qkv[:, :, heads + kv_heads:], causal, None, lens, lens, want_lse=True)
+        ctx.save_for_backward(turned, qkv, o, lse, freqs, positions, lens)
+        ctx.how = heads, kv_heads, interleaved, causal
+        return o
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        turned, qkv, o, lse, freqs, positions, lens = ctx.saved_tensors
+        heads, kv_heads, interleaved, causal = ctx.how
+        d = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
+        both = d[:, :, :heads + kv_heads]
+        api.nm_attention_grad(g, turned[:, :, :heads], turned[:, :, heads:], qkv[:, :, heads + kv_heads:], o, lse, causal, None, lens, lens,
+                              out=(both[:, :, :heads], both[:, :, heads:], d[:, :, heads + kv_heads:]))
+        if freqs is not None:
+            api.nm_rotary(both, freqs, positions, interleaved, inverse=True, out=both)
+        return d, None, None, None, None, None, None, None
+
+
+class NMSelfAttention(torch.nn.Module):
+    """Self-attention of a transformer block: one NMLinear for queries, keys and values, rotary positions, attention, one NMLinear behind it.
+
+    heads query heads of width / heads elements (a multiple of 8 up to 128) share kv_heads heads of keys and values.  rotary: elements of a head that are turned
+    (all by default, 0: none), with the frequencies of api.rotary_freqs; further arguments of that function in rotary_options.
+    forward(x, positions, lens): x [batch x length x width]; positions [length] or [batch x length], 0 .. by default; lens (int32 [batch]): tokens of each sequence, from
+    the front; what lies behind them is not looked at and gives the output projection's bias."""
+
+    def __init__(self, width: int, heads: int, kv_heads: Optional[int] = None, causal: bool = True, bias: bool = True, rotary: Optional[int] = None, interleaved: bool = False,
+                 rotary_options: Optional[dict] = None, cfg: Optional[NMConfig] = None, device=None, dtype=None):
+        super().__init__()
+        kv_heads = heads if kv_heads is None else kv_heads
+        if heads < 1 or kv_heads < 1 or width % heads or heads % kv_heads or width // heads % 8 or width // heads > 128:
+            raise ValueError(f"{heads} heads of {width} elements over {kv_heads} heads of keys: a head has a multiple of 8 elements up to 128, and heads are a multiple of kv_heads")
+        self.heads, self.kv_heads, self.head, self.causal, self.interleaved = heads, kv_heads, width // heads, causal, interleaved
+        rotary = self.head if rotary is None else rotary
+        if rotary < 0 or rotary > self.head or rotary % 2:
+            raise ValueError(f"an even number of a head's {self.head} elements is turned, got {rotary}")
+        kw = dict(bias=bias, cfg=cfg, device=device, dtype=dtype)
+        self.qkv, self.proj = NMLinear(width, (heads + 2 * kv_heads) * self.head, **kw), NMLinear(width, width, **kw)
+        # (a plain attribute: a module's .to(dtype) would round a buffer's binary64)
+        self._freqs = api.rotary_freqs(rotary, **(rotary_options or {})) if rotary else None
+        self._freqs_on = {}
+
+    def _frequencies(self, device):
+        if self._freqs is None:
+            return None
+        if device not in self._freqs_on:
+            self._freqs_on[device] = self._freqs.to(device)
+        return self._freqs_on[device]
+
+    def forward(self, x, positions: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None):
+        B, T, width = x.shape
+        qkv = self.qkv(x).view(B, T, self.heads + 2 * self.kv_heads, self.head)
+        o = _NMSelfAttentionFn.apply(qkv, self.heads, self.kv_heads, self._frequencies(x.device), positions, self.interleaved, self.causal, lens)
+        return self.proj(o.view(B, T, width))
