@@ -20,42 +20,58 @@ namespace attn {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// rows of D = 32 BLOCKS or fewer elements in LDS, each in a power of two of 16-byte chunks; chunk c of row r lies at c ^ turn(r): 16 rows' same chunk, and the four
-// rows x four chunks that a transposing read takes with 32 lanes, lie in 256 bytes of different banks
-template <int DT, int BLOCKS> struct Tile {
-    static constexpr int ES = DT == NM_DT_BF16 ? 2 : 4;
-    static constexpr int CHUNKS = (BLOCKS == 3 ? 4 : BLOCKS) * 32 * ES / 16;       // of a row
-    static constexpr int USED = BLOCKS * 32 * ES / 16;                             // that are read
+// Binary32 operands go through the bf16 instructions as three terms, x = x1 + x2 + x3 of 8 bits each, cut off one after another, which is exact; a product takes the six
+// products of terms down to 2^-16 of the first (what is left out is below 2^-23 of a product, half of it in the mean).  The binary32 instructions have a sixteenth of the bf16 ones'
+// rate, six products an eighth of work to sixteen.  An infinity becomes NaN.
+template <int DT> constexpr int TERMS = DT == NM_DT_BF16 ? 1 : 3;
+
+// rows of D = 32 BLOCKS or fewer elements in LDS as bf16 (binary32: three tiles of terms), each in a power of two of 16-byte chunks; chunk c of row r lies at c ^ turn(r):
+// 16 rows' same chunk, and the four rows x four chunks that a transposing read takes with 32 lanes, lie in 256 bytes of different banks
+template <int BLOCKS> struct Tile {
+    static constexpr int CHUNKS = (BLOCKS == 3 ? 4 : BLOCKS) * 4;                  // of a row
     static constexpr int ROW = CHUNKS * 16;
-    static constexpr int EC = 16 / ES;                                             // elements of a chunk
     static __device__ __forceinline__ int turn(int r)
     {
         const int low = r >> 2 & 3;
-        if constexpr (CHUNKS >= 16) return (r & 3) << 2 | low;
+        if constexpr (CHUNKS == 16) return (r & 3) << 2 | low;
         else if constexpr (CHUNKS == 8) return (r >> 1 & 1) << 2 | low;
         else return low;
     }
     static __device__ __forceinline__ int at(int r, int c) { return r * ROW + ((c ^ turn(r)) << 4); }
 };
 
-template <int DT> struct Frag;
-template <> struct Frag<NM_DT_BF16> { bf16x8 v; };
-template <> struct Frag<NM_DT_F32> { f32x8 v; };
+template <int DT> struct Frag { bf16x8 v[TERMS<DT>]; };
 
-__device__ __forceinline__ void mma(f32x16 &d, const Frag<NM_DT_BF16> &a, const Frag<NM_DT_BF16> &b) { d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, d, 0, 0, 0); }
-__device__ __forceinline__ void mma(f32x16 &d, const Frag<NM_DT_F32> &a, const Frag<NM_DT_F32> &b)
+__device__ __forceinline__ void mma(f32x16 &d, const bf16x8 &a, const bf16x8 &b) { d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, d, 0, 0, 0); }
+template <int DT> __device__ __forceinline__ void mma(f32x16 &d, const Frag<DT> &a, const Frag<DT> &b)
 {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], d, 0, 0, 0);
+    if constexpr (DT == NM_DT_F32) {
+        mma(d, a.v[2], b.v[0]);
+        mma(d, a.v[0], b.v[2]);
+        mma(d, a.v[1], b.v[1]);
+        mma(d, a.v[1], b.v[0]);
+        mma(d, a.v[0], b.v[1]);
+    }
+    mma(d, a.v[0], b.v[0]);
+}
+
+// the upper halves of two words in one
+__device__ __forceinline__ uint32_t upper(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
+// the terms of two values: word k holds term k of both
+__device__ __forceinline__ void terms_of(float x, float y, uint32_t (&w)[3])
+{
+    const float x1 = __uint_as_float(__float_as_uint(x) & 0xffff0000u), y1 = __uint_as_float(__float_as_uint(y) & 0xffff0000u), rx = x - x1, ry = y - y1;
+    const float x2 = __uint_as_float(__float_as_uint(rx) & 0xffff0000u), y2 = __uint_as_float(__float_as_uint(ry) & 0xffff0000u);
+    w[0] = upper(x, y);
+    w[1] = upper(rx, ry);
+    w[2] = upper(rx - x2, ry - y2);
 }
 
 // Where a lane's fragments lie in LDS: the turns of rows and chunks are exclusive-ors, so the address of row r + r', chunk c + c' is the lane's own (r, c) with
@@ -66,16 +82,17 @@ typedef __attribute__((address_space(3))) char lds_char;
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const lds_char *)p; }
 template <typename T> __device__ __forceinline__ T lds_read(uint32_t at) { return *(const __attribute__((address_space(3))) T *)(uintptr_t)at; }
 
-template <int DT, int BLOCKS> struct Lane {
-    typedef Tile<DT, BLOCKS> L;
+// ROWS: of a tile
+template <int DT, int BLOCKS, int ROWS> struct Lane {
+    typedef Tile<BLOCKS> L;
+    static constexpr uint32_t TERM = ROWS * L::ROW, BYTES = TERMS<DT> * TERM;      // from a term's tile to the next one's, and of all of them
     uint32_t row, col;               // relative to a tile
     __device__ __forceinline__ Lane(int lane)
     {
-        const int hi = lane >> 5, e = lane & 31;
-        row = (uint32_t)L::at(e, DT == NM_DT_BF16 ? hi : 2 * hi);
-        // bf16: 16 lanes bring 4 rows x 16 elements, 8 bytes each, and get an element's 4 rows each
-        if constexpr (DT == NM_DT_BF16) col = (uint32_t)(L::at(4 * hi + (lane >> 2 & 3), (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) + (lane & 1) * 8);
-        else col = (uint32_t)(L::at(4 * hi, e >> 2) + (e & 3) * 4);
+        const int hi = lane >> 5;
+        row = (uint32_t)L::at(lane & 31, hi);
+        // 16 lanes bring 4 rows x 16 elements, 8 bytes each, and get an element's 4 rows each
+        col = (uint32_t)(L::at(4 * hi + (lane >> 2 & 3), (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) + (lane & 1) * 8);
     }
     static __device__ __forceinline__ uint32_t moved(uint32_t at, int r, int c) { return (at ^ (uint32_t)((c ^ L::turn(r)) << 4)) + (uint32_t)(r * L::ROW); }
     // the addresses in a tile, as the compiler shall not know them from the last tile's
@@ -86,26 +103,20 @@ template <int DT, int BLOCKS> struct Lane {
     static __device__ __forceinline__ Frag<DT> rows(uint32_t from, int r0, int kk)
     {
         Frag<DT> f;
-        if constexpr (DT == NM_DT_BF16) f.v = lds_read<bf16x8>(moved(from, r0, 2 * kk));
-        else {
-            const f32x4 a = lds_read<f32x4>(moved(from, r0, 4 * kk)), b = lds_read<f32x4>(moved(from, r0, 4 * kk + 1));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { f.v[j] = a[j]; f.v[4 + j] = b[j]; }
-        }
+        for (int n = 0; n < TERMS<DT>; ++n) f.v[n] = lds_read<bf16x8>(moved(from, r0, 2 * kk) + n * TERM);
         return f;
     }
     // A fragment of the transposed tile: elements 32 b .. 32 b + 31 as its rows, the tile's rows r0 .. r0 + 15 (r0 a multiple of 16) as k in the slots' order
     static __device__ __forceinline__ Frag<DT> columns(uint32_t from, int r0, int b)
     {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         Frag<DT> f;
-        if constexpr (DT == NM_DT_BF16) {
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)moved(from, r0, 4 * b));
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)moved(from, r0 + 8, 4 * b));
-            f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f.v[j] = lds_read<float>(moved(from, r0 + 8 * (j >> 2) + (j & 3), 8 * b));
+        for (int n = 0; n < TERMS<DT>; ++n) {
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(moved(from, r0, 4 * b) + n * TERM));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(moved(from, r0 + 8, 4 * b) + n * TERM));
+            f.v[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         }
         return f;
     }
@@ -115,16 +126,20 @@ template <int DT, int BLOCKS> struct Lane {
 // probabilities take them before that
 template <int DT> __device__ __forceinline__ Frag<DT> as_fragment(const f32x16 &d, int first)
 {
-    Frag<DT> f;
-    if constexpr (DT == NM_DT_BF16) {
-        u32x4 w;
+    u32x4 w[TERMS<DT>];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack_bf16_rne(d[first + 2 * j], d[first + 2 * j + 1]);
-        f.v = __builtin_bit_cast(bf16x8, w);
-    } else {
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (DT == NM_DT_BF16) w[0][j] = pack_bf16_rne(d[first + 2 * j], d[first + 2 * j + 1]);
+        else {
+            uint32_t t[3];
+            terms_of(d[first + 2 * j], d[first + 2 * j + 1], t);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f.v[j] = d[first + j];
+            for (int n = 0; n < 3; ++n) w[n][j] = t[n];
+        }
     }
+    Frag<DT> f;
+#pragma unroll
+    for (int n = 0; n < TERMS<DT>; ++n) f.v[n] = __builtin_bit_cast(bf16x8, w[n]);
     return f;
 }
 
@@ -147,11 +162,16 @@ struct Sequence {
     // keys that query i sees; not below 0
     __device__ __forceinline__ int seen(const AttnArg &p, int i) const { return p.causal ? max(0, min(nk, i + 1 + nk - nq)) : nk; }
 };
-// Workgroups go round-robin to the XCDs; each XCD takes a run of the list, so that the workgroups that read the same keys and values share an L2.
-__device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t n)
+// Workgroups go round-robin to the XCDs; each XCD takes a run of the list, so that the workgroups that read the same keys and values share an L2.  A head's tiles stand in the list
+// by falling work.  Where a CU holds two workgroups at once, the second 32 of a run (an XCD's CUs) go in reverse, so that each CU starts with a long and a short one; where
+// heads have few tiles, every other 32, since 32 are then whole heads and a CU would get the same tile of each.  2 x 4096 tokens, 8 heads of 64 in binary32, causal, all
+// workgroups at once: forward 560 us without, 233 with; 32 x 512 tokens, 16 heads of 64: dk dv 95 and 81 us.  Where a CU holds one, the list as it is: whoever is
+// done takes the longest that is left (2 x 8192 tokens, 64 heads of 128 over 8: dk dv 4.6 ms, in reverse 6.5).
+__device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t n, int tiles, bool two)
 {
-    const uint32_t x = id % 8;
-    return x * (n / 8) + min(x, n % 8) + id / 8;
+    const uint32_t x = id % 8, size = n / 8 + (x < n % 8), i = id / 8, row = i & ~31u;
+    const bool reverse = tiles <= 16 ? row & 32 : two && row == 32;
+    return x * (n / 8) + min(x, n % 8) + (reverse && row + 32 <= size ? row + 31 - (i - row) : i);
 }
 
 // the first of part k of n parts of some tiles (2^26 at most)
@@ -167,44 +187,80 @@ template <int DT, int BLOCKS> __device__ __forceinline__ void load_fragments(Fra
     for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
         const int e = 16 * kk + 8 * hi;
         const bool ok = there && e < D;
-        const char *at = from + (ok ? e : 0) * Tile<DT, BLOCKS>::ES;
         if constexpr (DT == NM_DT_BF16) {
-            u32x4 w = *(const u32x4 *)at;
+            u32x4 w = *(const u32x4 *)(from + (ok ? e : 0) * 2);
             if (!ok) w = u32x4{0, 0, 0, 0};
-            f[kk].v = __builtin_bit_cast(bf16x8, w);
+            f[kk].v[0] = __builtin_bit_cast(bf16x8, w);
         } else {
+            const char *at = from + (ok ? e : 0) * 4;
             f32x4 a = *(const f32x4 *)at, b = *(const f32x4 *)(at + 16);
             if (!ok) a = b = f32x4{0, 0, 0, 0};
+            f32x16 x;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { f[kk].v[j] = a[j]; f[kk].v[4 + j] = b[j]; }
+            for (int j = 0; j < 4; ++j) { x[j] = a[j]; x[4 + j] = b[j]; }
+            f[kk] = as_fragment<DT>(x, 0);
         }
     }
 }
+// the product of two rows, element by element, added up over this lane's elements
+template <int DT, int BLOCKS> __device__ __forceinline__ float row_product(const char *x, const char *y, int D, int lane)
+{
+    const int hi = lane >> 5;
+    float sum = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+        const int e = 16 * kk + 8 * hi;
+        if (e >= D) continue;
+        if constexpr (DT == NM_DT_BF16) {
+            const bf16x8 a = *(const bf16x8 *)(x + e * 2), b = *(const bf16x8 *)(y + e * 2);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)a[j], (float)b[j], sum);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                const f32x4 a = *(const f32x4 *)(x + (e + h) * 4), b = *(const f32x4 *)(y + (e + h) * 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum = __builtin_fmaf(a[j], b[j], sum);
+            }
+        }
+    }
+    return sum;
+}
 
-// ROWS rows of a tile on their way from memory to LDS through the registers of THREADS threads.  Rows behind `rows` and chunks behind D become zeros (a masked key's
-// probability is zero, and zero times what a padded row may hold would not be).
+// ROWS rows of a tile on their way from memory to LDS through the registers of THREADS threads, 16 bytes at a time.  Rows behind `rows` and elements behind D become zeros (a
+// masked key's probability is zero, and zero times what a padded row may hold would not be).
 template <int DT, int BLOCKS, int ROWS, int THREADS> struct Stage {
-    typedef Tile<DT, BLOCKS> L;
-    static constexpr int PIECES = ROWS * L::USED, N = (PIECES + THREADS - 1) / THREADS;
+    typedef Tile<BLOCKS> L;
+    static constexpr int EC = DT == NM_DT_BF16 ? 8 : 4, USED = 32 * BLOCKS / EC;   // elements of a piece, pieces of a row
+    static constexpr int PIECES = ROWS * USED, N = (PIECES + THREADS - 1) / THREADS;
     u32x4 v[N];
-    // at(row): the row's address; rows `from` .. rows - 1 of the tile are there, rows > 0.  What is not there is read from a row that is, and left out by store: a choice
-    // made here would wait for the loads.
+    // at(row): the row's address; `rows` > 0 of the tile's are there.  What is not there is read from a row that is, and left out by store: a choice made here would
+    // wait for the loads.
     template <typename At> __device__ __forceinline__ void load(const At &at, int rows, int D)
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int piece = (int)threadIdx.x + n * THREADS, r = piece / L::USED, c = piece % L::USED;
-            v[n] = *(const u32x4 *)(at(min(r, rows - 1)) + (c * L::EC < D ? c : 0) * 16);
+            const int piece = (int)threadIdx.x + n * THREADS, r = piece / USED, c = piece % USED;
+            v[n] = *(const u32x4 *)(at(min(r, rows - 1)) + (c * EC < D ? c : 0) * 16);
         }
     }
+    // rows `from` .. rows - 1 are there
     __device__ __forceinline__ void store(char *tile, int rows, int D, int from = 0) const
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int piece = (int)threadIdx.x + n * THREADS, r = piece / L::USED, c = piece % L::USED;
-            const bool ok = r < rows && r >= from && c * L::EC < D;
+            const int piece = (int)threadIdx.x + n * THREADS, r = piece / USED, c = piece % USED;
+            const bool ok = r < rows && r >= from && c * EC < D;
             const u32x4 w = {ok ? v[n][0] : 0u, ok ? v[n][1] : 0u, ok ? v[n][2] : 0u, ok ? v[n][3] : 0u};
-            if (PIECES % THREADS == 0 || piece < PIECES) *(u32x4 *)(tile + L::at(r, c)) = w;
+            if (PIECES % THREADS != 0 && piece >= PIECES) continue;
+            if constexpr (DT == NM_DT_BF16) *(u32x4 *)(tile + L::at(r, c)) = w;
+            else {
+                uint32_t lo[3], hi[3];
+                terms_of(__uint_as_float(w[0]), __uint_as_float(w[1]), lo);
+                terms_of(__uint_as_float(w[2]), __uint_as_float(w[3]), hi);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *(u32x2 *)(tile + k * ROWS * L::ROW + L::at(r, c >> 1) + (c & 1) * 8) = u32x2{lo[k], hi[k]};
+            }
         }
     }
 };

@@ -21,12 +21,12 @@ constexpr float MOVE = 8.0f;     // a maximum moves when it is beaten by this po
 template <int DT, int BLOCKS, int WAVES, int KEYS>
 __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2) void attention_kernel(const AttnArg p, int row_tiles)
 {
-    typedef Tile<DT, BLOCKS> L;
-    constexpr int ES = L::ES, THREADS = 64 * WAVES, ROWS = 32 * WAVES, SB = KEYS / 32;
-    __shared__ __align__(16) char lds[2][2][KEYS * L::ROW];
+    typedef Lane<DT, BLOCKS, KEYS> F;
+    constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, THREADS = 64 * WAVES, ROWS = 32 * WAVES, SB = KEYS / 32;
+    __shared__ __align__(16) char lds[2][2][F::BYTES];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
     // the tiles of a head side by side, those with most keys first
-    const uint32_t place = place_of(blockIdx.x, gridDim.x), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)row_tiles;
+    const uint32_t place = place_of(blockIdx.x, gridDim.x, row_tiles, DT == NM_DT_BF16 || BLOCKS < 3), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)row_tiles;
     const int tile = row_tiles - 1 - (int)(whole - bh * row_tiles), split = (int)(place - whole * p.splits);
     const Sequence s(p, (int)bh);
     const int total = p.Tq * p.group, r0 = tile * ROWS;
@@ -62,8 +62,7 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
     for (int b = 0; b < BLOCKS; ++b) o[b] = f32x16{};
     float m = -INFINITY, sum = 0.0f;
     const float c = p.scale * LOG2E;
-    const Lane<DT, BLOCKS> at_lane(lane);
-    typedef Lane<DT, BLOCKS> F;
+    const F at_lane(lane);
     if (first_tile < end_tile) store(first_tile, 0);
     __syncthreads();
     for (int t = first_tile; t < end_tile; ++t) {

@@ -20,11 +20,11 @@ namespace attn {
 template <int DT, int BLOCKS, int KEYS>
 __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void attention_dq_kernel(const AttnArg p, int row_tiles)
 {
-    typedef Tile<DT, BLOCKS> L;
-    constexpr int ES = L::ES, ROWS = 128, SB = KEYS / 32;
-    __shared__ __align__(16) char lds[2][2][KEYS * L::ROW];
+    typedef Lane<DT, BLOCKS, KEYS> F;
+    constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, ROWS = 128, SB = KEYS / 32;
+    __shared__ __align__(16) char lds[2][2][F::BYTES];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
-    const uint32_t place = place_of(blockIdx.x, gridDim.x), bh = place / (uint32_t)row_tiles;
+    const uint32_t place = place_of(blockIdx.x, gridDim.x, row_tiles, DT == NM_DT_BF16 || BLOCKS < 3), bh = place / (uint32_t)row_tiles;
     const int tile = row_tiles - 1 - (int)(place - bh * row_tiles);
     const Sequence s(p, (int)bh);
     const int total = p.Tq * p.group, r0 = tile * ROWS;
@@ -52,16 +52,10 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     };
     if (tiles > 0) load(0);
     Frag<DT> q[2 * BLOCKS], g[2 * BLOCKS];
-    load_fragments<DT, BLOCKS>(g, row_at(p.o, p.so, s.b, query, head, ES), there, p.D, lane);
-    load_fragments<DT, BLOCKS>(q, row_at(p.g, p.sg, s.b, query, head, ES), there, p.D, lane);
-    float delta = 0.0f;
-#pragma unroll
-    for (int kk = 0; kk < 2 * BLOCKS; ++kk)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)q[kk].v[j], (float)g[kk].v[j], delta);
+    const char *g_row = row_at(p.g, p.sg, s.b, query, head, ES);
+    load_fragments<DT, BLOCKS>(g, g_row, there, p.D, lane);
+    float delta = there ? row_product<DT, BLOCKS>(g_row, row_at(p.o, p.so, s.b, query, head, ES), p.D, lane) : 0.0f;
     delta += other_half(delta);
-#pragma unroll
-    for (int kk = 0; kk < 2 * BLOCKS; ++kk) g[kk] = q[kk];
     if (hi == 0 && row < total) p.delta[at] = delta;
     load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
     // (a row that sees nothing has lse = -infinity: with +infinity in its place P is zero)
@@ -70,8 +64,7 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) dq[b] = f32x16{};
 
-    const Lane<DT, BLOCKS> at_lane(lane);
-    typedef Lane<DT, BLOCKS> F;
+    const F at_lane(lane);
     if (tiles > 0) store(0);
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
@@ -114,16 +107,16 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
 template <int DT, int BLOCKS, int ROWS, int WAVES, int PER_SIMD, bool VL>
 __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(const AttnArg p, int key_tiles)
 {
-    typedef Tile<DT, BLOCKS> L;
-    typedef Lane<DT, BLOCKS> F;
-    constexpr int ES = L::ES, KEYS = 32 * WAVES, SB = ROWS / 32, THREADS = 64 * WAVES;
-    constexpr uint32_t G = ROWS * L::ROW;                                // from q's tile to g's
-    __shared__ __align__(16) char lds[2][2][ROWS * L::ROW];
-    __shared__ __align__(16) char v_lds[VL ? KEYS * L::ROW : 16];
+    typedef Lane<DT, BLOCKS, ROWS> F;
+    typedef Lane<DT, BLOCKS, 32 * WAVES> FV;
+    constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, KEYS = 32 * WAVES, SB = ROWS / 32, THREADS = 64 * WAVES;
+    constexpr uint32_t G = F::BYTES;                                     // from q's tile to g's
+    __shared__ __align__(16) char lds[2][2][F::BYTES];
+    __shared__ __align__(16) char v_lds[VL ? FV::BYTES : 16];
     __shared__ float lse_of[2][ROWS], delta_of[2][ROWS];
     __shared__ int seen_of[2][ROWS];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
-    const uint32_t place = place_of(blockIdx.x, gridDim.x), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)key_tiles;
+    const uint32_t place = place_of(blockIdx.x, gridDim.x, key_tiles, PER_SIMD * 4 >= 2 * WAVES), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)key_tiles;
     const int tile = (int)(whole - bh * key_tiles), split = (int)(place - whole * p.splits);       // (the first keys have most rows)
     const Sequence s(p, (int)bh);
     const int key0 = tile * KEYS, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
@@ -185,7 +178,7 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
     for (int t = first_tile; t < end_tile; ++t) {
         const int buf = t - first_tile & 1;
         // (one register for the rows of both tiles and one for their columns: the second tile is a constant away)
-        [[maybe_unused]] const uint32_t v_rows = VL ? at_lane.rows_of(lds_address(v_lds) + (uint32_t)(wave * 32 * L::ROW)) : 0u;
+        [[maybe_unused]] const uint32_t v_rows = VL ? at_lane.rows_of(lds_address(v_lds) + (uint32_t)(wave * 32 * Tile<BLOCKS>::ROW)) : 0u;
         const uint32_t rows = at_lane.rows_of(lds_address(lds[buf][0])), columns = at_lane.columns_of(lds_address(lds[buf][0]));
         if (t + 1 < end_tile) load(t + 1);
         // the tile's last row sees most keys, its first one fewest
@@ -198,7 +191,7 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
 #pragma unroll
                 for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
                     mma(x, F::rows(rows, 32 * a, kk), k[kk]);
-                    if constexpr (VL) mma(dp, F::rows(rows + G, 32 * a, kk), F::rows(v_rows, 0, kk));
+                    if constexpr (VL) mma(dp, F::rows(rows + G, 32 * a, kk), FV::rows(v_rows, 0, kk));
                     else mma(dp, F::rows(rows + G, 32 * a, kk), v[kk]);
                 }
 #pragma unroll

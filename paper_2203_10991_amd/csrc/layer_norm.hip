@@ -68,6 +68,13 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(con
     float w[N][EW], b[N][EW];
     load_weights<WT, T>(w, p.w, t, C, 1.0f);
     load_weights<WT, T>(b, p.b, t, C, 0.0f);
+    int mine = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Piece q = piece_of<T>(n, t, C);
+        mine += max(0, q.left - q.skip);
+    }
+    const float count = WAVES > 1 ? wave_sum((float)mine) : (float)C, divisor = count > 0.0f ? count : 1.0f;
     int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     Raw<DT> next[N];
@@ -85,16 +92,14 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(con
 #pragma unroll
             for (int n = 0; n < N; ++n) next[n] = load_piece<DT>(row_from<DT>(p.x, row + step, p.ldx), piece_of<T>(n, t, C), C);
         float sum = 0.0f, sq = 0.0f;
-        int mine = 0;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const Piece q = piece_of<T>(n, t, C);
 #pragma unroll
             for (int i = 0; i < EW; ++i)
-                if (i >= q.skip && i < q.left) { sum += x[n][i]; ++mine; }
+                if (i >= q.skip && i < q.left) sum += x[n][i];
         }
-        const float count = WAVES > 1 ? wave_sum((float)mine) : (float)C;
-        float mean = wave_sum(sum) / (count > 0.0f ? count : 1.0f);
+        float mean = wave_sum(sum) / divisor;                              // (a quotient: the mean of equal elements is theirs)
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const Piece q = piece_of<T>(n, t, C);
@@ -270,7 +275,7 @@ hipError_t launch_layer_norm(const NormArg &a, hipStream_t st)
     if (a.R <= 0) return hipSuccess;
     return with_shape(a.C, [&](auto s) {
         typedef decltype(s) S;
-        const unsigned wgs = (unsigned)std::min<int64_t>((a.R + S::rows - 1) / S::rows, 8 * NM_CUS);
+        const unsigned wgs = (unsigned)std::min<int64_t>((a.R + S::rows - 1) / S::rows, 5 * NM_CUS);
         const dim3 threads(S::t < NORM_T ? NORM_T : S::t);
         if (a.x_dt == NM_DT_BF16) {
             if (a.w_dt == NM_DT_BF16) layer_norm_kernel<NM_DT_BF16, NM_DT_BF16, S::t, S::n><<<wgs, threads, 0, st>>>(a);
