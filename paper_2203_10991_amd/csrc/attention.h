@@ -162,16 +162,18 @@ struct Sequence {
     // keys that query i sees; not below 0
     __device__ __forceinline__ int seen(const AttnArg &p, int i) const { return p.causal ? max(0, min(nk, i + 1 + nk - nq)) : nk; }
 };
-// Workgroups go round-robin to the XCDs; each XCD takes a run of the list, so that the workgroups that read the same keys and values share an L2.  A head's tiles stand in the list
-// by falling work.  Where a CU holds two workgroups at once, the second 32 of a run (an XCD's CUs) go in reverse, so that each CU starts with a long and a short one; where
-// heads have few tiles, every other 32, since 32 are then whole heads and a CU would get the same tile of each.  2 x 4096 tokens, 8 heads of 64 in binary32, causal, all
+// Workgroups go round-robin to the XCDs; here each XCD takes 32 (its CUs) in a row of the list at a time, which mostly read the same keys and values and share its L2.  A
+// head's tiles stand in the list by falling work, and sequences differ in length, so runs of 32 go to the XCDs forth and back (one long run to each left XCDs with the short
+// sequences of a batch idle).  Where a CU holds two workgroups at once, its XCD's second 32 go in reverse, so that each CU starts with a long and a short one; where heads
+// have few tiles, every other 32, since 32 are then whole heads and a CU would get the same tile of each.  2 x 4096 tokens, 8 heads of 64 in binary32, causal, all
 // workgroups at once: forward 560 us without, 233 with; 32 x 512 tokens, 16 heads of 64: dk dv 95 and 81 us.  Where a CU holds one, the list as it is: whoever is
 // done takes the longest that is left (2 x 8192 tokens, 64 heads of 128 over 8: dk dv 4.6 ms, in reverse 6.5).
 __device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t n, int tiles, bool two)
 {
-    const uint32_t x = id % 8, size = n / 8 + (x < n % 8), i = id / 8, row = i & ~31u;
-    const bool reverse = tiles <= 16 ? row & 32 : two && row == 32;
-    return x * (n / 8) + min(x, n % 8) + (reverse && row + 32 <= size ? row + 31 - (i - row) : i);
+    const uint32_t x = id % 8, i = id / 8, round = i / 32, at = i % 32;
+    if (round >= n / 256) return id;
+    const bool reverse = tiles <= 16 ? round & 1 : two && round == 1;
+    return (round * 8 + (round & 1 ? 7 - x : x)) * 32 + (reverse ? 31 - at : at);
 }
 
 // the first of part k of n parts of some tiles (2^26 at most)

@@ -154,10 +154,12 @@ template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(c
     const int query = (int)(at - bh * p.Tq), b = (int)(bh / p.Hq), head = (int)(bh - (int64_t)b * p.Hq);
     const float *st = p.part + (int64_t)p.splits * rows * p.D;
     float m = -INFINITY;
+#pragma unroll 8
     for (int k = 0; k < p.splits; ++k) m = fmaxf(m, st[(k * rows + at) * 2]);
     const float base = m == -INFINITY ? 0.0f : m;
     float sum = 0.0f;
     f32x4 o = {0, 0, 0, 0};
+#pragma unroll 8
     for (int k = 0; k < p.splits; ++k) {
         const float w = exp2_of(st[(k * rows + at) * 2] - base);
         const f32x4 x = *(const f32x4 *)(p.part + (k * rows + at) * p.D + e);
@@ -182,7 +184,8 @@ inline Plan plan_of(const AttnArg &a)
     p.keys = p.waves == 1 ? 32 : a.dt == NM_DT_F32 ? 32 : 64;
     p.row_tiles = (total + 32 * p.waves - 1) / (32 * p.waves);
     const int64_t wgs = heads * p.row_tiles, want = (p.waves == 1 ? 8 : 2) * NM_CUS;
-    p.splits = wgs >= want / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, (a.Tk + 4 * p.keys - 1) / (4 * p.keys), 64}));
+    const int64_t least = p.waves == 1 ? 128 : 512;                     // keys to a part
+    p.splits = wgs >= want / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, (a.Tk + least - 1) / least, 64}));
     return p;
 }
 

@@ -104,6 +104,17 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     if (row < total) store_column<DT, BLOCKS>((char *)row_at(p.dq, p.sdq, s.b, query, head, ES), dq, p.scale, p.D, lane);
 }
 
+// the tiles of rows that see any key from key0 on: those of queries from a first one on
+struct RowTiles {
+    int first, count;
+    __device__ __forceinline__ RowTiles(const AttnArg &p, const Sequence &s, int key0, int rows)
+    {
+        const int total = s.nq * p.group, query = p.causal ? max(0, key0 - (s.nk - s.nq)) : 0;
+        first = (int)(min((int64_t)total, (int64_t)query * p.group) / rows);
+        count = key0 < s.nk ? max(0, (total + rows - 1) / rows - first) : 0;
+    }
+};
+
 template <int DT, int BLOCKS, int ROWS, int WAVES, int PER_SIMD, bool VL>
 __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(const AttnArg p, int key_tiles)
 {
@@ -120,10 +131,10 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
     const int tile = (int)(whole - bh * key_tiles), split = (int)(place - whole * p.splits);       // (the first keys have most rows)
     const Sequence s(p, (int)bh);
     const int key0 = tile * KEYS, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
-    // rows that see any of the keys: those of queries from first_query on
-    const int total = s.nq * p.group, first_query = p.causal ? max(0, key0 - (s.nk - s.nq)) : 0;
-    const int first = min((int64_t)total, (int64_t)first_query * p.group) / ROWS, tiles = key0 < s.nk ? max(0, (total + ROWS - 1) / ROWS - first) : 0;
-    const int first_tile = first + part_of(tiles, split, p.splits), end_tile = first + part_of(tiles, split + 1, p.splits);
+    const int total = s.nq * p.group;
+    const RowTiles tiles(p, s, key0, ROWS);
+    const int first_tile = tiles.first + min(tiles.count, split * p.chunk), end_tile = tiles.first + min(tiles.count, (split + 1) * p.chunk);
+    if (split > 0 && first_tile >= end_tile) return;
     const int blind = p.causal ? max(0, s.nq - s.nk) * p.group : 0;       // rows that see nothing: what their q and g hold does not count
 
     const char *q0 = row_at(p.q, p.sq, s.b, 0, s.h * p.group, ES), *g0 = row_at(p.g, p.sg, s.b, 0, s.h * p.group, ES);
@@ -237,82 +248,101 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
 }
 
 // the parts of dk and dv added up in their order: 4 elements to a thread; blockIdx.y: dk, dv
-template <int DT> __global__ __launch_bounds__(256) void attention_sum_kernel(const AttnArg p)
+template <int DT> __global__ __launch_bounds__(256) void attention_sum_kernel(const AttnArg p, int tile_keys, int tile_rows)
 {
     const int64_t keys = (int64_t)p.B * p.Hk * p.Tk, n4 = keys * p.D / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n4) return;
     const int which = (int)blockIdx.y;
+    const int64_t at = 4 * i / p.D, bh = at / p.Tk;
+    const int e = (int)(4 * i - at * p.D), b = (int)(bh / p.Hk), key = (int)(at - bh * p.Tk);
+    // (the parts that were made: one at least)
+    const RowTiles tiles(p, Sequence(p, (int)bh), key / tile_keys * tile_keys, tile_rows);
+    const int parts = min(p.splits, max(1, (tiles.count + p.chunk - 1) / p.chunk));
     f32x4 x = {0, 0, 0, 0};
-    for (int k = 0; k < p.splits; ++k) {
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
         const f32x4 y = *(const f32x4 *)(p.part + (int64_t)(2 * k + which) * keys * p.D + 4 * i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[j] += y[j];
     }
-    const int64_t at = 4 * i / p.D, bh = at / p.Tk;
-    const int e = (int)(4 * i - at * p.D), b = (int)(bh / p.Hk);
     const AttnStride st = which ? p.sdv : p.sdk;
-    char *to = (char *)row_at(which ? p.dv : p.dk, st, b, at - bh * p.Tk, bh - (int64_t)b * p.Hk, DT == NM_DT_BF16 ? 2 : 4);
+    char *to = (char *)row_at(which ? p.dv : p.dk, st, b, key, bh - (int64_t)b * p.Hk, DT == NM_DT_BF16 ? 2 : 4);
     if constexpr (DT == NM_DT_BF16) *(u32x2 *)(to + e * 2) = u32x2{pack_bf16_rne(x[0], x[1]), pack_bf16_rne(x[2], x[3])};
     else *(f32x4 *)(to + e * 4) = x;
 }
 
-// Waves of a workgroup of the dk dv kernel, waves to a SIMD, rows of a tile, and whether v's fragments come from LDS each time instead of staying in registers.
-// In bf16: 128 elements to a head have 128 registers of sums; with v in LDS the rest fits two waves to a SIMD (2 x 8192 tokens, 64 heads over 8: one wave with everything in
-// registers 8.1 ms, four waves 5.1, eight 4.6), with 64 three fit (32 x 512 tokens, 16 heads: 105 -> 94 us).
-template <int DT, int BLOCKS> struct KeyShape { static constexpr int waves = 4, per_simd = DT == NM_DT_F32 ? 1 : 2, rows = 32; static constexpr bool v_in_lds = false; };
-template <> struct KeyShape<NM_DT_BF16, 2> { static constexpr int waves = 4, per_simd = 3, rows = 32; static constexpr bool v_in_lds = true; };
-template <> struct KeyShape<NM_DT_BF16, 3> { static constexpr int waves = 8, per_simd = 2, rows = 32; static constexpr bool v_in_lds = true; };
-template <> struct KeyShape<NM_DT_BF16, 4> { static constexpr int waves = 8, per_simd = 2, rows = 32; static constexpr bool v_in_lds = true; };
-inline int keys_to_workgroup(const AttnArg &a)
+// Waves of a workgroup of the dk dv kernel, waves to a SIMD, and whether v's fragments come from LDS each time instead of staying in registers; tiles have 32 rows.
+// In bf16: 128 elements to a head have 128 registers of sums; with v in LDS the rest fits two waves to a SIMD, with 64 three.  WIDE: eight waves share a tile of rows instead of
+// four, for heads of more than 64 elements where keys and workgroups are many.  2 x 8192 tokens, 64 heads of 128 over 8: one wave to a SIMD with everything in registers 8.1 ms,
+// four waves 5.1, eight 4.6; 32 x 512 tokens, 16 heads of 64: 105 us with two to a SIMD, 94 with three.
+template <int DT, int BLOCKS, bool WIDE> struct KeyShape { static constexpr int waves = 4, per_simd = DT == NM_DT_F32 ? 1 : 2; static constexpr bool v_in_lds = false; };
+template <bool WIDE> struct KeyShape<NM_DT_BF16, 2, WIDE> { static constexpr int waves = 4, per_simd = 3; static constexpr bool v_in_lds = true; };
+template <bool WIDE> struct KeyShape<NM_DT_BF16, 3, WIDE> { static constexpr int waves = WIDE ? 8 : 4, per_simd = 2; static constexpr bool v_in_lds = true; };
+template <bool WIDE> struct KeyShape<NM_DT_BF16, 4, WIDE> { static constexpr int waves = WIDE ? 8 : 4, per_simd = 2; static constexpr bool v_in_lds = true; };
+constexpr int KEY_ROWS = 32;
+// 2 x 8192 tokens, 16 heads of 96, all gradients: eight waves 2986 us (causal 1677), four 3172 (1886); 4 x 2048 tokens, 16 heads of 96 over 4, causal: 333 and 304;
+// 32 x 512 tokens, 16 heads of 80, causal: 228 and 220
+inline bool wide_keys(const AttnArg &a) { return a.dt == NM_DT_BF16 && a.D > 64 && a.Tk >= 2048 && (int64_t)a.B * a.Hk * ((a.Tk + 255) / 256) >= NM_CUS; }
+
+template <int DT, int BLOCKS, bool WIDE> struct KeyPlan {
+    typedef KeyShape<DT, BLOCKS, WIDE> W;
+    static constexpr int dt = DT, blocks = BLOCKS;
+    // How many parts the rows go in where keys are few, and how long one is: rows divided evenly where every key is seen, so that a key's part is as long whether many
+    // rows see it or few (parts that nothing is left for end at once).  Twice as many workgroups as have room, since they are all as long: 6 x up to 1333 tokens, 12 heads of
+    // 80 over 1, causal: 125 us with as many as have room, 80 with twice, 79 with three and four times.
+    static void plan(AttnArg &a)
+    {
+        const int64_t keys = 32 * W::waves, wgs = (int64_t)a.B * a.Hk * ((a.Tk + keys - 1) / keys), tiles = ((int64_t)a.Tq * a.group + KEY_ROWS - 1) / KEY_ROWS;
+        const int64_t room = (int64_t)NM_CUS * W::per_simd * 4 / W::waves;
+        a.splits = wgs >= room || wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({room * (a.causal ? 4 : 2) / wgs, tiles / 8, 32}));
+        a.chunk = (int)std::max<int64_t>(1, (tiles + a.splits - 1) / a.splits);
+    }
+};
+template <typename F> auto with_plan(const AttnArg &a, F &&f)
 {
-    if (a.dt != NM_DT_BF16) return 32 * KeyShape<NM_DT_F32, 1>::waves;
-    return 32 * (a.D > 96 ? KeyShape<NM_DT_BF16, 4>::waves : a.D > 64 ? KeyShape<NM_DT_BF16, 3>::waves : KeyShape<NM_DT_BF16, 2>::waves);
-}
-inline int64_t key_tiles(const AttnArg &a) { return ((int64_t)a.Tk + keys_to_workgroup(a) - 1) / keys_to_workgroup(a); }
-inline int key_splits(const AttnArg &a)
-{
-    const int64_t wgs = (int64_t)a.B * a.Hk * key_tiles(a), rows = (int64_t)a.Tq * a.group;
-    return wgs >= NM_CUS || wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({2 * NM_CUS / wgs, rows / 256, 16}));
+    const int blocks = (a.D + 31) / 32;
+    if (a.dt == NM_DT_F32) return blocks == 1 ? f(KeyPlan<NM_DT_F32, 1, false>{}) : blocks == 2 ? f(KeyPlan<NM_DT_F32, 2, false>{}) : blocks == 3 ? f(KeyPlan<NM_DT_F32, 3, false>{}) : f(KeyPlan<NM_DT_F32, 4, false>{});
+    if (wide_keys(a)) return blocks == 3 ? f(KeyPlan<NM_DT_BF16, 3, true>{}) : f(KeyPlan<NM_DT_BF16, 4, true>{});
+    return blocks == 1 ? f(KeyPlan<NM_DT_BF16, 1, false>{}) : blocks == 2 ? f(KeyPlan<NM_DT_BF16, 2, false>{}) : blocks == 3 ? f(KeyPlan<NM_DT_BF16, 3, false>{}) : f(KeyPlan<NM_DT_BF16, 4, false>{});
 }
 
-template <int DT, int BLOCKS> hipError_t launch_grads(const AttnArg &a, hipStream_t st)
+template <typename P> hipError_t launch_grads(const AttnArg &a, P, hipStream_t st)
 {
-    constexpr int KEYS = DT == NM_DT_F32 ? 32 : 64;
-    typedef KeyShape<DT, BLOCKS> W;
-    const int64_t heads = (int64_t)a.B * a.Hk, row_tiles = ((int64_t)a.Tq * a.group + 127) / 128, kt = key_tiles(a);
-    const int64_t wq = heads * row_tiles, wk = heads * kt * a.splits;
-    if (std::max(wq, wk) > 0x7fffffff || !grid_holds(std::max(wq, wk), 256)) return hipErrorInvalidConfiguration;
+    constexpr int DT = P::dt, BLOCKS = P::blocks, KEYS = DT == NM_DT_F32 ? 32 : 64;
+    typedef typename P::W W;
+    const int64_t heads = (int64_t)a.B * a.Hk, row_tiles = ((int64_t)a.Tq * a.group + 127) / 128, kt = ((int64_t)a.Tk + 32 * W::waves - 1) / (32 * W::waves);
+    const int64_t wq = heads * row_tiles, wk = heads * kt * a.splits, ws = (heads * a.Tk * a.D / 4 + 255) / 256;
+    if (std::max(wq, wk) > 0x7fffffff || !grid_holds(std::max(wq, wk), 64 * W::waves) || !grid_holds(wq, 256) || !grid_holds(ws, 256)) return hipErrorInvalidConfiguration;
     if (wq > 0) attention_dq_kernel<DT, BLOCKS, KEYS><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || wk == 0) return e;
-    attention_dkdv_kernel<DT, BLOCKS, W::rows, W::waves, W::per_simd, W::v_in_lds><<<dim3((unsigned)wk), dim3(64 * W::waves), 0, st>>>(a, (int)kt);
+    attention_dkdv_kernel<DT, BLOCKS, KEY_ROWS, W::waves, W::per_simd, W::v_in_lds><<<dim3((unsigned)wk), dim3(64 * W::waves), 0, st>>>(a, (int)kt);
+    e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    attention_sum_kernel<DT><<<dim3((unsigned)ws, 2), dim3(256), 0, st>>>(a, 32 * W::waves, KEY_ROWS);
     return hipGetLastError();
 }
+inline size_t delta_bytes(const AttnArg &a) { return ((size_t)a.B * a.Hq * a.Tq * 4 + 15) / 16 * 16; }
 
 }  // namespace attn
 
+// (the number of parts follows from the sizes and from whether the call is causal; a workspace holds either)
 size_t attention_grad_workspace(const AttnArg &a)
 {
-    const int splits = attn::key_splits(a);
-    const size_t delta = ((size_t)a.B * a.Hq * a.Tq * 4 + 15) / 16 * 16;
-    return delta + (splits == 1 ? 0 : (size_t)splits * 2 * a.B * a.Hk * a.Tk * a.D * 4);
+    AttnArg b = a;
+    b.causal = 1;
+    attn::with_plan(b, [&](auto plan) { plan.plan(b); });
+    return attn::delta_bytes(a) + (b.splits == 1 ? 0 : (size_t)b.splits * 2 * a.B * a.Hk * a.Tk * a.D * 4);
 }
 
 hipError_t launch_attention_grad(AttnArg a, void *workspace, hipStream_t st)
 {
-    a.splits = attn::key_splits(a);
     a.delta = (float *)workspace;
-    a.part = (float *)((char *)workspace + ((size_t)a.B * a.Hq * a.Tq * 4 + 15) / 16 * 16);
-    hipError_t e;
-    const int blocks = (a.D + 31) / 32;
-    if (a.dt == NM_DT_BF16) e = blocks == 1 ? attn::launch_grads<NM_DT_BF16, 1>(a, st) : blocks == 2 ? attn::launch_grads<NM_DT_BF16, 2>(a, st) : blocks == 3 ? attn::launch_grads<NM_DT_BF16, 3>(a, st) : attn::launch_grads<NM_DT_BF16, 4>(a, st);
-    else e = blocks == 1 ? attn::launch_grads<NM_DT_F32, 1>(a, st) : blocks == 2 ? attn::launch_grads<NM_DT_F32, 2>(a, st) : blocks == 3 ? attn::launch_grads<NM_DT_F32, 3>(a, st) : attn::launch_grads<NM_DT_F32, 4>(a, st);
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t wgs = ((int64_t)a.B * a.Hk * a.Tk * a.D / 4 + 255) / 256;
-    if (!grid_holds(wgs, 256)) return hipErrorInvalidConfiguration;
-    if (a.dt == NM_DT_BF16) attn::attention_sum_kernel<NM_DT_BF16><<<dim3((unsigned)wgs, 2), dim3(256), 0, st>>>(a);
-    else attn::attention_sum_kernel<NM_DT_F32><<<dim3((unsigned)wgs, 2), dim3(256), 0, st>>>(a);
-    return hipGetLastError();
+    a.part = (float *)((char *)workspace + attn::delta_bytes(a));
+    return attn::with_plan(a, [&](auto plan) {
+        plan.plan(a);
+        return attn::launch_grads(a, plan, st);
+    });
 }
 
 }  // namespace nm

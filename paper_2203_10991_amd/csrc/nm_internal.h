@@ -262,6 +262,7 @@ struct AttnArg {
     int group_shift;
     float scale;
     int splits;                               // of the keys (forward) or of the rows (gradients of k and v)
+    int chunk;                                // gradients: tiles of rows to a part
     float *part;                              // their partial results
     // gradients
     const void *g;
