@@ -115,17 +115,17 @@ struct RowTiles {
     }
 };
 
-template <int DT, int BLOCKS, int ROWS, int WAVES, int PER_SIMD, bool VL>
+template <int DT, int BLOCKS, int ROWS, int WAVES, int PER_SIMD, bool VL, int BUFFERS>
 __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(const AttnArg p, int key_tiles)
 {
     typedef Lane<DT, BLOCKS, ROWS> F;
     typedef Lane<DT, BLOCKS, 32 * WAVES> FV;
     constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, KEYS = 32 * WAVES, SB = ROWS / 32, THREADS = 64 * WAVES;
     constexpr uint32_t G = F::BYTES;                                     // from q's tile to g's
-    __shared__ __align__(16) char lds[2][2][F::BYTES];
+    __shared__ __align__(16) char lds[BUFFERS][2][F::BYTES];
     __shared__ __align__(16) char v_lds[VL ? FV::BYTES : 16];
-    __shared__ float lse_of[2][ROWS], delta_of[2][ROWS];
-    __shared__ int seen_of[2][ROWS];
+    __shared__ float lse_of[BUFFERS][ROWS], delta_of[BUFFERS][ROWS];
+    __shared__ int seen_of[BUFFERS][ROWS];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
     const uint32_t place = place_of(blockIdx.x, gridDim.x, key_tiles, PER_SIMD * 4 >= 2 * WAVES), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)key_tiles;
     const int tile = (int)(whole - bh * key_tiles), split = (int)(place - whole * p.splits);       // (the first keys have most rows)
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
     const F at_lane(lane);
     __syncthreads();
     for (int t = first_tile; t < end_tile; ++t) {
-        const int buf = t - first_tile & 1;
+        const int buf = t - first_tile & (BUFFERS - 1);
         // (one register for the rows of both tiles and one for their columns: the second tile is a constant away)
         [[maybe_unused]] const uint32_t v_rows = VL ? at_lane.rows_of(lds_address(v_lds) + (uint32_t)(wave * 32 * Tile<BLOCKS>::ROW)) : 0u;
         const uint32_t rows = at_lane.rows_of(lds_address(lds[buf][0])), columns = at_lane.columns_of(lds_address(lds[buf][0]));
@@ -230,7 +230,8 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
                 }
             }
         }
-        if (t + 1 < end_tile) store(t + 1, buf ^ 1);
+        if constexpr (BUFFERS == 1) __syncthreads();
+        if (t + 1 < end_tile) store(t + 1, buf ^ (BUFFERS - 1));
         __syncthreads();
     }
     if (key >= p.Tk) return;
@@ -275,10 +276,11 @@ template <int DT> __global__ __launch_bounds__(256) void attention_sum_kernel(co
 // In bf16: 128 elements to a head have 128 registers of sums; with v in LDS the rest fits two waves to a SIMD, with 64 three.  WIDE: eight waves share a tile of rows instead of
 // four, for heads of more than 64 elements where keys and workgroups are many.  2 x 8192 tokens, 64 heads of 128 over 8: one wave to a SIMD with everything in registers 8.1 ms,
 // four waves 5.1, eight 4.6; 32 x 512 tokens, 16 heads of 64: 105 us with two to a SIMD, 94 with three.
-template <int DT, int BLOCKS, bool WIDE> struct KeyShape { static constexpr int waves = 4, per_simd = DT == NM_DT_F32 ? 1 : 2; static constexpr bool v_in_lds = false; };
-template <bool WIDE> struct KeyShape<NM_DT_BF16, 2, WIDE> { static constexpr int waves = 4, per_simd = 3; static constexpr bool v_in_lds = true; };
-template <bool WIDE> struct KeyShape<NM_DT_BF16, 3, WIDE> { static constexpr int waves = WIDE ? 8 : 4, per_simd = 2; static constexpr bool v_in_lds = true; };
-template <bool WIDE> struct KeyShape<NM_DT_BF16, 4, WIDE> { static constexpr int waves = WIDE ? 8 : 4, per_simd = 2; static constexpr bool v_in_lds = true; };
+template <int DT, int BLOCKS, bool WIDE> struct KeyShape { static constexpr int waves = 4, per_simd = DT == NM_DT_F32 ? 1 : 2; static constexpr bool v_in_lds = false; static constexpr int buffers = 2; };
+template <> struct KeyShape<NM_DT_F32, 4, false> { static constexpr int waves = 4, per_simd = 1; static constexpr bool v_in_lds = true; static constexpr int buffers = 1; };
+template <bool WIDE> struct KeyShape<NM_DT_BF16, 2, WIDE> { static constexpr int waves = 4, per_simd = 3; static constexpr bool v_in_lds = true; static constexpr int buffers = 2; };
+template <bool WIDE> struct KeyShape<NM_DT_BF16, 3, WIDE> { static constexpr int waves = WIDE ? 8 : 4, per_simd = 2; static constexpr bool v_in_lds = true; static constexpr int buffers = 2; };
+template <bool WIDE> struct KeyShape<NM_DT_BF16, 4, WIDE> { static constexpr int waves = WIDE ? 8 : 4, per_simd = 2; static constexpr bool v_in_lds = true; static constexpr int buffers = 2; };
 constexpr int KEY_ROWS = 32;
 // 2 x 8192 tokens, 16 heads of 96, all gradients: eight waves 2986 us (causal 1677), four 3172 (1886); 4 x 2048 tokens, 16 heads of 96 over 4, causal: 333 and 304;
 // 32 x 512 tokens, 16 heads of 80, causal: 228 and 220
@@ -316,7 +318,7 @@ template <typename P> hipError_t launch_grads(const AttnArg &a, P, hipStream_t s
     if (wq > 0) attention_dq_kernel<DT, BLOCKS, KEYS><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || wk == 0) return e;
-    attention_dkdv_kernel<DT, BLOCKS, KEY_ROWS, W::waves, W::per_simd, W::v_in_lds><<<dim3((unsigned)wk), dim3(64 * W::waves), 0, st>>>(a, (int)kt);
+    attention_dkdv_kernel<DT, BLOCKS, KEY_ROWS, W::waves, W::per_simd, W::v_in_lds, W::buffers><<<dim3((unsigned)wk), dim3(64 * W::waves), 0, st>>>(a, (int)kt);
     e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     attention_sum_kernel<DT><<<dim3((unsigned)ws, 2), dim3(256), 0, st>>>(a, 32 * W::waves, KEY_ROWS);

@@ -166,6 +166,27 @@ def test_many_rows_over_few_keys(dtype):
         _compare(*inputs(1, 700, 100, 4, 1, 64, dtype, seed=9), causal, 0.125)
 
 
+@pytest.mark.parametrize("B,Tq,Tk,H,K,D,kl", [(32, 40, 2048, 2, 1, 128, None), (32, 33, 2050, 1, 1, 96, "ragged"), (16, 9, 4100, 2, 1, 72, "ragged")])
+def test_many_keys_of_many_heads(B, Tq, Tk, H, K, D, kl):
+    """eight waves to a tile of rows: from 2048 keys on, where there are workgroups for every CU"""
+    import paper_2203_10991_amd as nm
+    lens = None if kl is None else [Tk - 97 * b for b in range(B)]
+    ins = inputs(B, Tq, Tk, H, K, D, BF16, seed=12)
+    for causal in (False, True):
+        _compare(*ins, causal, D ** -0.5, None, lens)
+    q, k, v, g = (t.to(DEV) for t in ins)
+    o, lse = nm.nm_attention(q, k, v, want_lse=True)
+    assert any("attention_dkdv_kernel<1, %d, 32, 8," % (-(-D // 32)) in n for n in kernels_of(lambda: nm.nm_attention_grad(g, q, k, v, o, lse)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,T,H,K,D", [(20, 130, 16, 16, 32), (9, 300, 16, 16, 64), (3, 600, 30, 15, 40)])
+def test_many_workgroups(B, T, H, K, D, dtype):
+    """more than the 256 that are dealt to the XCDs at a time, and what is left behind the last 256; lengths from all to none"""
+    lens = [T - (T * b) // max(1, B - 1) for b in range(B)]
+    _compare(*inputs(B, T, T, H, K, D, dtype, seed=13), True, D ** -0.5, lens, lens)
+
+
 def test_another_stream_and_two_graphs():
     """two captured calls with workspaces of their own, replayed in turn with eager calls between"""
     import paper_2203_10991_amd as nm
