@@ -2,7 +2,7 @@
 //     y = (x - mean) r w + b, r = 1 / sqrt(var + eps)
 //     with h = (x - mean) r and u = g w:  dx = r (u - mean(u) - h mean(u h))      dw = sum over the rows of g h      db = sum of g
 // A row is held in registers, 8 N elements to a thread, T threads to a row, so that it is read once; a workgroup goes through its rows with w, b and the next row's elements
-// in registers.  Mean and sum of squared deviations: in two steps within a wave, and between the waves of a row by the formula for joining two samples (one exchange).
+// in registers (LEAN, for rows beyond 16384: registers hold the row and half of the sums; w and b are read again, sums of dw wait in LDS).  Mean and sum of squared deviations: in two steps within a wave, and between the waves of a row by the formula for joining two samples (one exchange).
 // Sums of dw and db stay with the threads of a column; what a workgroup has goes to the workspace, and a second launch adds the workgroups' parts up in a fixed order.
 // Bound: HBM.
 #include <hip/hip_runtime.h>
@@ -43,31 +43,32 @@ template <int DT> __device__ __forceinline__ Raw<DT> load_piece(const void *row,
 {
     return C >= EW ? load_raw<DT>(row, p.at) : load_raw<DT, true>(row, p.at, p.left);
 }
-template <int WT, int T, int N> __device__ __forceinline__ void load_weights(float (&w)[N][EW], const void *from, int t, int C, float missing)
+template <int WT, int T> __device__ __forceinline__ void load_weights(float (&w)[EW], const void *from, int n, int t, int C, float missing)
 {
+    if (!from) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        if (!from) {
+        for (int i = 0; i < EW; ++i) w[i] = missing;
+    } else {
+        const Raw<WT> r = load_piece<WT>(from, piece_of<T>(n, t, C), C);
 #pragma unroll
-            for (int i = 0; i < EW; ++i) w[n][i] = missing;
-        } else {
-            const Raw<WT> r = load_piece<WT>(from, piece_of<T>(n, t, C), C);
-#pragma unroll
-            for (int i = 0; i < EW; ++i) w[n][i] = element(r, i);
-        }
+        for (int i = 0; i < EW; ++i) w[i] = element(r, i);
     }
 }
 template <int DT> __device__ __forceinline__ const void *row_from(const void *p, int64_t row, int64_t ld) { return (const char *)p + row * ld * (DT == NM_DT_BF16 ? 2 : 4); }
 
-template <int DT, int WT, int T, int N>
+template <int DT, int WT, int T, int N, bool LEAN>
 __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(const NormArg p)
 {
-    constexpr int THREADS = T < NORM_T ? NORM_T : T, ROWS = THREADS / T, WAVES = T / 64;
+    constexpr int THREADS = T < NORM_T ? NORM_T : T, ROWS = THREADS / T, WAVES = T > 64 ? T / 64 : 1, LANES = T < 64 ? T : 64;
     __shared__ float join[2][WAVES > 1 ? WAVES : 1][3];
     const int t = (int)threadIdx.x % T, C = (int)p.C;
-    float w[N][EW], b[N][EW];
-    load_weights<WT, T>(w, p.w, t, C, 1.0f);
-    load_weights<WT, T>(b, p.b, t, C, 0.0f);
+    float w[LEAN ? 1 : N][EW], b[LEAN ? 1 : N][EW];
+    if constexpr (!LEAN)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            load_weights<WT, T>(w[n], p.w, n, t, C, 1.0f);
+            load_weights<WT, T>(b[n], p.b, n, t, C, 0.0f);
+        }
     int mine = 0;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -78,17 +79,20 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(con
     int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     Raw<DT> next[N];
-    if (row < p.R)
+    if (!LEAN && row < p.R)
 #pragma unroll
         for (int n = 0; n < N; ++n) next[n] = load_piece<DT>(row_from<DT>(p.x, row, p.ldx), piece_of<T>(n, t, C), C);
     // (rows of a workgroup with several waves to a row end together)
     for (int odd = 0; row < p.R; row += step, odd ^= 1) {
+        if constexpr (LEAN)
+#pragma unroll
+            for (int n = 0; n < N; ++n) next[n] = load_piece<DT>(row_from<DT>(p.x, row, p.ldx), piece_of<T>(n, t, C), C);
         float x[N][EW];
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int i = 0; i < EW; ++i) x[n][i] = element(next[n], i);
-        if (row + step < p.R)
+        if (!LEAN && row + step < p.R)
 #pragma unroll
             for (int n = 0; n < N; ++n) next[n] = load_piece<DT>(row_from<DT>(p.x, row + step, p.ldx), piece_of<T>(n, t, C), C);
         float sum = 0.0f, sq = 0.0f;
@@ -99,7 +103,7 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(con
             for (int i = 0; i < EW; ++i)
                 if (i >= q.skip && i < q.left) sum += x[n][i];
         }
-        float mean = wave_sum(sum) / divisor;                              // (a quotient: the mean of equal elements is theirs)
+        float mean = wave_sum<LANES>(sum) / divisor;                              // (a quotient: the mean of equal elements is theirs)
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const Piece q = piece_of<T>(n, t, C);
@@ -107,7 +111,7 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(con
             for (int i = 0; i < EW; ++i)
                 if (i >= q.skip && i < q.left) { const float d = x[n][i] - mean; sq += d * d; }
         }
-        sq = wave_sum(sq);
+        sq = wave_sum<LANES>(sq);
         if constexpr (WAVES > 1) {
             if ((t & 63) == 0) { join[odd][t >> 6][0] = count; join[odd][t >> 6][1] = mean; join[odd][t >> 6][2] = sq; }
             __syncthreads();
@@ -124,9 +128,13 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(con
         for (int n = 0; n < N; ++n) {
             const Piece q = piece_of<T>(n, t, C);
             if (q.skip >= EW) continue;
+            if constexpr (LEAN) {
+                load_weights<WT, T>(w[0], p.w, n, t, C, 1.0f);
+                load_weights<WT, T>(b[0], p.b, n, t, C, 0.0f);
+            }
             float y[EW];
 #pragma unroll
-            for (int i = 0; i < EW; ++i) y[i] = __builtin_fmaf((x[n][i] - mean) * r, w[n][i], b[n][i]);
+            for (int i = 0; i < EW; ++i) y[i] = __builtin_fmaf((x[n][i] - mean) * r, w[LEAN ? 0 : n][i], b[LEAN ? 0 : n][i]);
             store_row<DT>((void *)row_from<DT>(p.y, row, p.ldy), q.at, q.skip, q.left, y);
         }
         if (t == 0) {
@@ -136,19 +144,25 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_kernel(con
     }
 }
 
-template <int DT, int WT, int T, int N>
+template <int DT, int WT, int T, int N, bool LEAN>
 __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_grad_kernel(const NormGradArg p)
 {
-    constexpr int THREADS = T < NORM_T ? NORM_T : T, ROWS = THREADS / T, WAVES = T / 64;
+    constexpr int THREADS = T < NORM_T ? NORM_T : T, ROWS = THREADS / T, WAVES = T > 64 ? T / 64 : 1, LANES = T < 64 ? T : 64;
     __shared__ float join[2][WAVES > 1 ? WAVES : 1][2];
     __shared__ float sums[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? T * EW : 1];
+    __shared__ float dw_lds[LEAN ? N * EW * T : 1];
     const int t = (int)threadIdx.x % T, group = (int)threadIdx.x / T, C = (int)p.C;
-    float w[N][EW], dw[N][EW], db[N][EW];
-    load_weights<WT, T>(w, p.w, t, C, 1.0f);
+    float w[LEAN ? 1 : N][EW], dw[LEAN ? 1 : N][EW], db[N][EW];
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+    for (int n = 0; n < N; ++n) {
+        if constexpr (!LEAN) load_weights<WT, T>(w[n], p.w, n, t, C, 1.0f);
 #pragma unroll
-        for (int i = 0; i < EW; ++i) dw[n][i] = db[n][i] = 0.0f;
+        for (int i = 0; i < EW; ++i) {
+            db[n][i] = 0.0f;
+            if constexpr (LEAN) dw_lds[(n * EW + i) * T + t] = 0.0f;
+            else dw[n][i] = 0.0f;
+        }
+    }
     int64_t row = (int64_t)blockIdx.x * ROWS + group;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     Raw<DT> nx[N], ng[N];
@@ -162,30 +176,32 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_grad_kerne
             ng[n] = load_piece<DT>(row_from<DT>(p.g, at, p.ldg), piece_of<T>(n, t, C), C);
         }
     };
-    if (row < p.R) load(row);
+    if (!LEAN && row < p.R) load(row);
     for (int odd = 0; row < p.R; row += step, odd ^= 1) {
+        if constexpr (LEAN) load(row);
         const float mean = nmean, r = nr;
-        float h[N][EW], g[N][EW], su = 0.0f, suh = 0.0f;
+        Raw<DT> x[N], g[N];
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int i = 0; i < EW; ++i) { h[n][i] = (element(nx[n], i) - mean) * r; g[n][i] = element(ng[n], i); }
-        if (row + step < p.R) load(row + step);
+        for (int n = 0; n < N; ++n) { x[n] = nx[n]; g[n] = ng[n]; }
+        if (!LEAN && row + step < p.R) load(row + step);
+        float su = 0.0f, suh = 0.0f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const Piece q = piece_of<T>(n, t, C);
+            if constexpr (LEAN) load_weights<WT, T>(w[0], p.w, n, t, C, 1.0f);
 #pragma unroll
             for (int i = 0; i < EW; ++i)
                 if (i >= q.skip && i < q.left) {
-                    dw[n][i] += g[n][i] * h[n][i];
-                    db[n][i] += g[n][i];
-                    const float u = g[n][i] * w[n][i];
+                    const float h = (element(x[n], i) - mean) * r, gi = element(g[n], i), u = gi * w[LEAN ? 0 : n][i];
+                    if constexpr (LEAN) dw_lds[(n * EW + i) * T + t] += gi * h;
+                    else dw[n][i] += gi * h;
+                    db[n][i] += gi;
                     su += u;
-                    suh += u * h[n][i];
+                    suh += u * h;
                 }
         }
-        su = wave_sum(su);
-        suh = wave_sum(suh);
+        su = wave_sum<LANES>(su);
+        suh = wave_sum<LANES>(suh);
         if constexpr (WAVES > 1) {
             if ((t & 63) == 0) { join[odd][t >> 6][0] = su; join[odd][t >> 6][1] = suh; }
             __syncthreads();
@@ -199,9 +215,10 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_grad_kerne
         for (int n = 0; n < N; ++n) {
             const Piece q = piece_of<T>(n, t, C);
             if (q.skip >= EW) continue;
+            if constexpr (LEAN) load_weights<WT, T>(w[0], p.w, n, t, C, 1.0f);
             float y[EW];
 #pragma unroll
-            for (int i = 0; i < EW; ++i) y[i] = (g[n][i] * w[n][i] - su - h[n][i] * suh) * r;
+            for (int i = 0; i < EW; ++i) y[i] = (element(g[n], i) * w[LEAN ? 0 : n][i] - su - (element(x[n], i) - mean) * r * suh) * r;
             store_row<DT>((void *)row_from<DT>(p.dx, row, p.lddx), q.at, q.skip, q.left, y);
         }
     }
@@ -211,7 +228,13 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_grad_kerne
     for (int which = 0; which < 2; ++which)
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            float (&d)[EW] = which ? db[n] : dw[n];
+            float d[EW];
+#pragma unroll
+            for (int i = 0; i < EW; ++i) {
+                if (which) d[i] = db[n][i];
+                else if constexpr (LEAN) d[i] = dw_lds[(n * EW + i) * T + t];
+                else d[i] = dw[n][i];
+            }
             if constexpr (ROWS > 1) {
                 __syncthreads();
                 if (group > 0)
@@ -219,7 +242,6 @@ __global__ __launch_bounds__(T < NORM_T ? NORM_T : T) void layer_norm_grad_kerne
                     for (int i = 0; i < EW; ++i) sums[group - 1][i * T + t] = d[i];
                 __syncthreads();
                 if (group > 0) continue;
-#pragma unroll
                 for (int k = 0; k < ROWS - 1; ++k)
 #pragma unroll
                     for (int i = 0; i < EW; ++i) d[i] += sums[k][i * T + t];
@@ -249,23 +271,27 @@ template <int WT> __global__ __launch_bounds__(1024) void layer_norm_sum_kernel(
     else ((uint16_t *)to)[at] = (uint16_t)pack_bf16_rne(s, s);
 }
 
-template <int T, int N> struct Shape { static constexpr int t = T, n = N, rows = (T < NORM_T ? NORM_T : T) / T; };
-// threads to a row and pieces to a thread: a wave up to 1024 elements
-template <typename F> hipError_t with_shape(int64_t C, F &&f)
+template <int T, int N, bool LEAN = false> struct Shape { static constexpr int t = T, n = N, threads = T < NORM_T ? NORM_T : T, rows = threads / T; static constexpr bool lean = LEAN; };
+// Threads to a row and pieces to a thread: part of a wave up to 256 elements, a wave up to 1024.  200000 rows of 64 in bf16: 60 us with a wave to a row, 12 with 8 threads.  lean: the
+// gradients of binary32 rows of 8193 to 16384 elements (4096 x 16384: 251 us with 512 threads and 94 spills, 196 lean; in bf16 101 and 128).
+template <typename F> auto with_shape(int64_t C, bool lean, F &&f)
 {
+    if (C <= 64) return f(Shape<8, 1>{});
+    if (C <= 128) return f(Shape<16, 1>{});
+    if (C <= 256) return f(Shape<32, 1>{});
     if (C <= 512) return f(Shape<64, 1>{});
     if (C <= 1024) return f(Shape<64, 2>{});
     if (C <= 2048) return f(Shape<256, 1>{});
     if (C <= 4096) return f(Shape<256, 2>{});
     if (C <= 8192) return f(Shape<256, 4>{});
-    if (C <= 16384) return f(Shape<512, 4>{});
-    return f(Shape<1024, 4>{});
+    if (C <= 16384) return lean ? f(Shape<1024, 2, true>{}) : f(Shape<512, 4>{});
+    return f(Shape<1024, 4, true>{});
 }
-inline int rows_to_workgroup(int64_t C) { return C <= 1024 ? 4 : 1; }
+// (a workgroup's sums are 8 C bytes out and in again: 512 rows of 16384 in 512 workgroups take 37 us, in 256 25)
 inline int64_t grad_workgroups(int64_t R, int64_t C)
 {
-    const int64_t wgs = (R + rows_to_workgroup(C) - 1) / rows_to_workgroup(C);
-    return std::min<int64_t>(wgs, 2 * NM_CUS);
+    const int64_t rows = with_shape(C, false, [](auto s) { return (int64_t)decltype(s)::rows; }), wgs = (R + rows - 1) / rows;
+    return std::min<int64_t>(wgs, (C > 16384 || wgs < 4 * NM_CUS ? 1 : 2) * NM_CUS);
 }
 
 }  // namespace
@@ -273,15 +299,15 @@ inline int64_t grad_workgroups(int64_t R, int64_t C)
 hipError_t launch_layer_norm(const NormArg &a, hipStream_t st)
 {
     if (a.R <= 0) return hipSuccess;
-    return with_shape(a.C, [&](auto s) {
+    return with_shape(a.C, false, [&](auto s) {
         typedef decltype(s) S;
         const unsigned wgs = (unsigned)std::min<int64_t>((a.R + S::rows - 1) / S::rows, 5 * NM_CUS);
-        const dim3 threads(S::t < NORM_T ? NORM_T : S::t);
+        const dim3 threads(S::threads);
         if (a.x_dt == NM_DT_BF16) {
-            if (a.w_dt == NM_DT_BF16) layer_norm_kernel<NM_DT_BF16, NM_DT_BF16, S::t, S::n><<<wgs, threads, 0, st>>>(a);
-            else layer_norm_kernel<NM_DT_BF16, NM_DT_F32, S::t, S::n><<<wgs, threads, 0, st>>>(a);
-        } else if (a.w_dt == NM_DT_BF16) layer_norm_kernel<NM_DT_F32, NM_DT_BF16, S::t, S::n><<<wgs, threads, 0, st>>>(a);
-        else layer_norm_kernel<NM_DT_F32, NM_DT_F32, S::t, S::n><<<wgs, threads, 0, st>>>(a);
+            if (a.w_dt == NM_DT_BF16) layer_norm_kernel<NM_DT_BF16, NM_DT_BF16, S::t, S::n, S::lean><<<wgs, threads, 0, st>>>(a);
+            else layer_norm_kernel<NM_DT_BF16, NM_DT_F32, S::t, S::n, S::lean><<<wgs, threads, 0, st>>>(a);
+        } else if (a.w_dt == NM_DT_BF16) layer_norm_kernel<NM_DT_F32, NM_DT_BF16, S::t, S::n, S::lean><<<wgs, threads, 0, st>>>(a);
+        else layer_norm_kernel<NM_DT_F32, NM_DT_F32, S::t, S::n, S::lean><<<wgs, threads, 0, st>>>(a);
         return hipGetLastError();
     });
 }
@@ -293,14 +319,14 @@ hipError_t launch_layer_norm_grad(const NormGradArg &a, hipStream_t st)
     const int64_t wgs = grad_workgroups(a.R, a.C);
     hipError_t e = hipSuccess;
     if (wgs > 0)
-        e = with_shape(a.C, [&](auto s) {
+        e = with_shape(a.C, a.x_dt == NM_DT_F32, [&](auto s) {
             typedef decltype(s) S;
-            const dim3 threads(S::t < NORM_T ? NORM_T : S::t);
+            const dim3 threads(S::threads);
             if (a.x_dt == NM_DT_BF16) {
-                if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_BF16, NM_DT_BF16, S::t, S::n><<<(unsigned)wgs, threads, 0, st>>>(a);
-                else layer_norm_grad_kernel<NM_DT_BF16, NM_DT_F32, S::t, S::n><<<(unsigned)wgs, threads, 0, st>>>(a);
-            } else if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_F32, NM_DT_BF16, S::t, S::n><<<(unsigned)wgs, threads, 0, st>>>(a);
-            else layer_norm_grad_kernel<NM_DT_F32, NM_DT_F32, S::t, S::n><<<(unsigned)wgs, threads, 0, st>>>(a);
+                if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_BF16, NM_DT_BF16, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
+                else layer_norm_grad_kernel<NM_DT_BF16, NM_DT_F32, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
+            } else if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_F32, NM_DT_BF16, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
+            else layer_norm_grad_kernel<NM_DT_F32, NM_DT_F32, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
             return hipGetLastError();
         });
     if (e != hipSuccess || !a.part) return e;
