@@ -35,7 +35,6 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     const int wave_first = query_of(min(r0 + wave * 32, total - 1), p), wave_last = query_of(min(r0 + wave * 32 + 31, total - 1), p);
     const int wave_most = r0 + wave * 32 >= total || wave_first >= s.nq ? 0 : s.seen(p, min(wave_last, s.nq - 1)), wave_least = s.seen(p, wave_first);
     const int seen = s.seen(p, query), tiles = (most + KEYS - 1) / KEYS;
-    const int64_t at = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
 
     const char *k0 = row_at(p.k, p.sk, s.b, 0, s.h, ES), *v0 = row_at(p.v, p.sv, s.b, 0, s.h, ES);
     Stage<DT, BLOCKS, KEYS, 256> ks, vs;
@@ -56,10 +55,10 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     load_fragments<DT, BLOCKS>(g, g_row, there, p.D, lane);
     float delta = there ? row_product<DT, BLOCKS>(g_row, row_at(p.o, p.so, s.b, query, head, ES), p.D, lane) : 0.0f;
     delta += other_half(delta);
-    if (hi == 0 && row < total) p.delta[at] = delta;
     load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
     // (a row that sees nothing has lse = -infinity: with +infinity in its place P is zero)
-    const float l = there ? p.lse[at] : -INFINITY, lse = l == -INFINITY ? INFINITY : l * LOG2E, c = p.scale * LOG2E;
+    const float l = there ? p.lse[((int64_t)s.b * p.Hq + head) * p.Tq + query] : -INFINITY, lse = l == -INFINITY ? INFINITY : l * LOG2E, c = p.scale * LOG2E;
+    if (hi == 0 && row < total) p.rows[(int64_t)bh * total + row] = make_float2(lse, delta);
     f32x16 dq[BLOCKS];
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) dq[b] = f32x16{};
@@ -139,7 +138,8 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
 
     const char *q0 = row_at(p.q, p.sq, s.b, 0, s.h * p.group, ES), *g0 = row_at(p.g, p.sg, s.b, 0, s.h * p.group, ES);
     Stage<DT, BLOCKS, ROWS, THREADS> qs, gs;
-    float lse_next = 0.0f, delta_next = 0.0f;
+    float2 row_next = make_float2(0.0f, 0.0f);
+    const float2 *rows_of_head = p.rows + (int64_t)bh * p.Tq * p.group;
     auto load = [&](int t) {
         const int r0 = t * ROWS, rows = min(ROWS, total - r0);
         auto at = [&](const char *from, const AttnStride &st, int r) {
@@ -148,12 +148,7 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
         };
         qs.load([&](int r) { return at(q0, p.sq, r); }, rows, p.D);
         gs.load([&](int r) { return at(g0, p.sg, r); }, rows, p.D);
-        if ((int)threadIdx.x < ROWS) {
-            const int r = r0 + min((int)threadIdx.x, rows - 1), query = query_of(r, p), head = s.h * p.group + r - query * p.group;
-            const int64_t where = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
-            lse_next = p.lse[where];
-            delta_next = p.delta[where];
-        }
+        if ((int)threadIdx.x < ROWS) row_next = rows_of_head[r0 + min((int)threadIdx.x, rows - 1)];
     };
     auto store = [&](int t, int to) {
         const int r0 = t * ROWS, rows = min(ROWS, total - r0);
@@ -161,8 +156,8 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
         gs.store(lds[to][1], rows, p.D, blind - r0);
         if ((int)threadIdx.x < ROWS) {
             const bool ok = (int)threadIdx.x < rows;
-            lse_of[to][threadIdx.x] = ok && lse_next != -INFINITY ? lse_next * LOG2E : INFINITY;        // (P = 0)
-            delta_of[to][threadIdx.x] = ok ? delta_next : 0.0f;
+            lse_of[to][threadIdx.x] = ok ? row_next.x : INFINITY;        // (P = 0)
+            delta_of[to][threadIdx.x] = ok ? row_next.y : 0.0f;
             seen_of[to][threadIdx.x] = ok ? s.seen(p, query_of(r0 + (int)threadIdx.x, p)) : 0;
         }
     };
@@ -324,7 +319,7 @@ template <typename P> hipError_t launch_grads(const AttnArg &a, P, hipStream_t s
     attention_sum_kernel<DT><<<dim3((unsigned)ws, 2), dim3(256), 0, st>>>(a, 32 * W::waves, KEY_ROWS);
     return hipGetLastError();
 }
-inline size_t delta_bytes(const AttnArg &a) { return ((size_t)a.B * a.Hq * a.Tq * 4 + 15) / 16 * 16; }
+inline size_t row_bytes(const AttnArg &a) { return ((size_t)a.B * a.Hq * a.Tq * 8 + 15) / 16 * 16; }
 
 }  // namespace attn
 
@@ -334,13 +329,13 @@ size_t attention_grad_workspace(const AttnArg &a)
     AttnArg b = a;
     b.causal = 1;
     attn::with_plan(b, [&](auto plan) { plan.plan(b); });
-    return attn::delta_bytes(a) + (b.splits == 1 ? 0 : (size_t)b.splits * 2 * a.B * a.Hk * a.Tk * a.D * 4);
+    return attn::row_bytes(a) + (b.splits == 1 ? 0 : (size_t)b.splits * 2 * a.B * a.Hk * a.Tk * a.D * 4);
 }
 
 hipError_t launch_attention_grad(AttnArg a, void *workspace, hipStream_t st)
 {
-    a.delta = (float *)workspace;
-    a.part = (float *)((char *)workspace + attn::delta_bytes(a));
+    a.rows = (float2 *)workspace;
+    a.part = (float *)((char *)workspace + attn::row_bytes(a));
     return attn::with_plan(a, [&](auto plan) {
         plan.plan(a);
         return attn::launch_grads(a, plan, st);

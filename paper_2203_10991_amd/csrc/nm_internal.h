@@ -268,7 +268,7 @@ struct AttnArg {
     const void *g;
     AttnStride sg, sdq, sdk, sdv;
     void *dq, *dk, *dv;
-    float *delta;                             // [B][Hq][Tq]
+    float2 *rows;                             // [B][Hk][Tq group]: lse in powers of two (infinity where a row sees nothing) and delta of each row
 };
 size_t attention_workspace(const AttnArg &a);
 hipError_t launch_attention(AttnArg a, void *workspace, hipStream_t st);
