@@ -494,14 +494,16 @@ int nm_rotary(const nm_heads *x, const nm_heads *y, int dtype, int64_t B, int64_
  * holds, and o, dq, dk and dv are zeros there.  (Lengths beyond the tensors count as the tensors'.)  causal: query i of n sees the keys j <= i + m - n of m, so that the last query
  * sees the last key.  A query that sees no key: o = 0, lse = -infinity, and it adds nothing to any gradient.  What a query does not see of its own sequence has to be finite.
  * lse: binary32 [B][Hq][Tq], the logarithm of the sum of the exponentials; NULL: not wanted; the gradients need it, and o as the forward pass left it.
+ * rest: bf16 [B][Tq][Hq][D], contiguous, on a 4-byte boundary: what rounding took from a bf16 o.  With it the gradients of queries that look at few keys are as exact as others';
+ * NULL: not wanted, or not at hand.  Binary32 tensors have none.
  * scale > 0.  Scores, probabilities and all sums are binary32; with bf16 tensors probabilities (not those of the sum) and their gradients are rounded to bf16 for the
  * products that follow.  The gradients recompute the probabilities; no sum's order depends on anything but the sizes.
  * workspaces: nm_attention_workspace(...) and nm_attention_grad_workspace(...) bytes.
  */
-int nm_attention(const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, float *lse, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype,
+int nm_attention(const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, float *lse, void *rest, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype,
                  int causal, float scale, const int32_t *q_lens, const int32_t *k_lens, void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t nm_attention_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype);
-int nm_attention_grad(const nm_heads *g, const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, const float *lse, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq,
+int nm_attention_grad(const nm_heads *g, const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, const float *lse, const void *rest, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq,
                       int64_t Hk, int64_t D, int dtype, int causal, float scale, const int32_t *q_lens, const int32_t *k_lens, const nm_heads *dq, const nm_heads *dk, const nm_heads *dv,
                       void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t nm_attention_grad_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype);

@@ -131,9 +131,9 @@ def load():
     lib.nm_rotary.argtypes = [heads, heads, i32, i64, i64, i64, i64, i64, vp, vp, i32, i64, i32, f32, i32, vp]
     lib.nm_rotary.restype = i32
     sizes = [i64] * 6 + [i32]                                                # B, Tq, Tk, Hq, Hk, D, dtype
-    lib.nm_attention.argtypes = [heads] * 4 + [vp, *sizes, i32, f32, vp, vp, vp, sz, vp]
+    lib.nm_attention.argtypes = [heads] * 4 + [vp, vp, *sizes, i32, f32, vp, vp, vp, sz, vp]
     lib.nm_attention.restype = i32
-    lib.nm_attention_grad.argtypes = [heads] * 5 + [vp, *sizes, i32, f32, vp, vp, heads, heads, heads, vp, sz, vp]
+    lib.nm_attention_grad.argtypes = [heads] * 5 + [vp, vp, *sizes, i32, f32, vp, vp, heads, heads, heads, vp, sz, vp]
     lib.nm_attention_grad.restype = i32
     for f in (lib.nm_attention_workspace, lib.nm_attention_grad_workspace):
         f.argtypes, f.restype = sizes, sz
@@ -1071,6 +1071,15 @@ def _attention_sizes(q, k, v):
     return B, Tq, k.shape[1], Hq, k.shape[2], D
 
 
+def _lse_planes(q: torch.Tensor) -> int:
+    return 1 + q.shape[-1] // 2 if q.dtype == torch.bfloat16 else 1
+
+
+def _rest(lse: Optional[torch.Tensor]):
+    """the address of what rounding took from o, behind lse's first plane"""
+    return lse.data_ptr() + 4 * lse[0].numel() if lse is not None and lse.shape[0] > 1 else None
+
+
 def _scale_of(scale: Optional[float], q: torch.Tensor) -> float:
     return float(scale) if scale is not None else q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
 
@@ -1089,7 +1098,8 @@ def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool
     8 up to 128; heads / kv_heads heads of q in a row share one of k and v.  scale: D ** -0.5 by default.  causal: query i of n sees the keys up to i + m - n of m, the last
     query the last key, so that one query over a cache of keys sees all of them.  q_lens, k_lens (int32 or int64 [batch], on the GPU): the tokens of each sequence, from
     the front; what lies behind counts for nothing, and the result is zero there, as for a query that sees no key.
-    want_lse: (o, lse), lse float32 [batch x heads x queries], the logarithm of the sum of exponentials, which nm_attention_grad reads."""
+    want_lse: (o, lse).  lse[0] is float32 [batch x heads x queries], the logarithm of the sum of exponentials; for bfloat16 lse has D / 2 planes more, whose bits are
+    what rounding took from o (bfloat16 [batch x queries x heads x D]).  nm_attention_grad reads all of it."""
     lib = load()
     scale = _scale_of(scale, q)
     r = _native_result(_native.attention(q, k, v, causal, scale, q_lens, k_lens, want_lse))
@@ -1101,11 +1111,11 @@ def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool
     sizes = B, Tq, Tk, Hq, Hk, D = _attention_sizes(q, k, v)
     ql, kl = _lengths_of(q_lens, B, q.device), _lengths_of(k_lens, B, q.device)
     o = torch.empty((B, Tq, Hq, D), dtype=q.dtype, device=q.device)
-    lse = torch.empty((B, Hq, Tq), dtype=torch.float32, device=q.device) if want_lse else None
+    lse = torch.empty((_lse_planes(q), B, Hq, Tq), dtype=torch.float32, device=q.device) if want_lse else None
     need = int(lib.nm_attention_workspace(*sizes, dt))
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     with torch.cuda.device(q.device):
-        _check(lib.nm_attention(_heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), scale, _ptr(ql), _ptr(kl),
+        _check(lib.nm_attention(_heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), _rest(lse), *sizes, dt, int(causal), scale, _ptr(ql), _ptr(kl),
                                 _ptr(ws), need, _stream(q)))
     return (o, lse) if want_lse else o
 
@@ -1113,7 +1123,7 @@ def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool
 def nm_attention_grad(g: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor, causal: bool = False,
                       scale: Optional[float] = None, q_lens: Optional[torch.Tensor] = None, k_lens: Optional[torch.Tensor] = None, out=None):
     """(dq, dk, dv) of nm_attention from the gradient g of its result o; the other arguments as they were given to it, and the lse that it left.  The probabilities
-    are computed again.  The same call gives the same bits.  out: three tensors for the results, of q's, k's and v's shapes, parts of one tensor among them."""
+    are computed again.  lse[:1] alone will do; gradients of queries that look at few keys are then less exact in bfloat16.  The same call gives the same bits.  out: three tensors for the results, of q's, k's and v's shapes, parts of one tensor among them."""
     lib = load()
     scale = _scale_of(scale, q)
     if out is None:
@@ -1126,8 +1136,8 @@ def nm_attention_grad(g: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torc
     sizes = B, Tq, Tk, Hq, Hk, D = _attention_sizes(q, k, v)
     if g.shape != q.shape or o.shape != q.shape:
         raise ValueError("g and o have q's shape")
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, Tq) or lse.device != q.device:
-        raise ValueError(f"lse is float32 [{B}, {Hq}, {Tq}] on the tensors' device")
+    if lse.dtype != torch.float32 or lse.dim() != 4 or lse.shape[0] not in (1, _lse_planes(q)) or tuple(lse.shape[1:]) != (B, Hq, Tq) or lse.device != q.device:
+        raise ValueError(f"lse is float32 [{_lse_planes(q)}, {B}, {Hq}, {Tq}] on the tensors' device, as nm_attention left it")
     lse = lse.contiguous()
     ql, kl = _lengths_of(q_lens, B, q.device), _lengths_of(k_lens, B, q.device)
     if out is None:
@@ -1140,7 +1150,7 @@ def nm_attention_grad(g: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torc
     need = int(lib.nm_attention_grad_workspace(*sizes, dt))
     ws = torch.empty(need, dtype=torch.uint8, device=q.device)
     with torch.cuda.device(q.device):
-        _check(lib.nm_attention_grad(_heads(g), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), *sizes, dt, int(causal), scale,
+        _check(lib.nm_attention_grad(_heads(g), _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), _rest(lse), *sizes, dt, int(causal), scale,
                                      _ptr(ql), _ptr(kl), _heads(dq), _heads(dk), _heads(dv), _ptr(ws), need, _stream(q)))
     if out is not None:
         torch.autograd.graph.increment_version([t for t in out if not t.is_inference()])

@@ -204,8 +204,8 @@ template <int DT, int BLOCKS> __device__ __forceinline__ void load_fragments(Fra
         }
     }
 }
-// the product of two rows, element by element, added up over this lane's elements
-template <int DT, int BLOCKS> __device__ __forceinline__ float row_product(const char *x, const char *y, int D, int lane)
+// the product of row x with y + rest (null: none), element by element, added up over this lane's elements
+template <int DT, int BLOCKS> __device__ __forceinline__ float row_product(const char *x, const char *y, const char *rest, int D, int lane)
 {
     const int hi = lane >> 5;
     float sum = 0.0f;
@@ -217,6 +217,12 @@ template <int DT, int BLOCKS> __device__ __forceinline__ float row_product(const
             const bf16x8 a = *(const bf16x8 *)(x + e * 2), b = *(const bf16x8 *)(y + e * 2);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)a[j], (float)b[j], sum);
+            if (rest) {
+                typedef bf16x8 any __attribute__((aligned(4)));
+                const bf16x8 d = *(const any *)(rest + e * 2);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)a[j], (float)d[j], sum);
+            }
         } else {
 #pragma unroll
             for (int h = 0; h < 8; h += 4) {
@@ -267,8 +273,23 @@ template <int DT, int BLOCKS, int ROWS, int THREADS> struct Stage {
     }
 };
 
+__device__ __forceinline__ const char *rest_at(const AttnArg &p, int b, int t, int h) { return p.rest ? (const char *)p.rest + (((int64_t)b * p.Tq + t) * p.Hq + h) * p.D * 2 : nullptr; }
+
+// four elements of a row, and (bf16, rest not null) what rounding took from them
+template <int DT> __device__ __forceinline__ void store_four(char *to, char *rest, int e, const f32x4 &x)
+{
+    if constexpr (DT == NM_DT_BF16) {
+        const u32x2 w = {pack_bf16_rne(x[0], x[1]), pack_bf16_rne(x[2], x[3])};
+        *(u32x2 *)(to + e * 2) = w;
+        if (rest) {
+            typedef u32x2 any __attribute__((aligned(4)));
+            *(any *)(rest + e * 2) = u32x2{pack_bf16_rne(x[0] - __uint_as_float(w[0] << 16), x[1] - __uint_as_float(w[0] & 0xffff0000u)),
+                                           pack_bf16_rne(x[2] - __uint_as_float(w[1] << 16), x[3] - __uint_as_float(w[1] & 0xffff0000u))};
+        }
+    } else *(f32x4 *)(to + e * 4) = x;
+}
 // a column of D blocks (an output row of D elements) times `by`, to memory
-template <int DT, int BLOCKS> __device__ __forceinline__ void store_column(char *to, const f32x16 (&d)[BLOCKS], float by, int D, int lane)
+template <int DT, int BLOCKS> __device__ __forceinline__ void store_column(char *to, const f32x16 (&d)[BLOCKS], float by, int D, int lane, char *rest = nullptr)
 {
     const int hi = lane >> 5;
 #pragma unroll
@@ -276,10 +297,19 @@ template <int DT, int BLOCKS> __device__ __forceinline__ void store_column(char 
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const int e = 32 * b + 8 * (i >> 2) + 4 * hi;
-            if (e >= D) continue;
-            if constexpr (DT == NM_DT_BF16) *(u32x2 *)(to + e * 2) = u32x2{pack_bf16_rne(d[b][i] * by, d[b][i + 1] * by), pack_bf16_rne(d[b][i + 2] * by, d[b][i + 3] * by)};
-            else *(f32x4 *)(to + e * 4) = f32x4{d[b][i] * by, d[b][i + 1] * by, d[b][i + 2] * by, d[b][i + 3] * by};
+            if (e < D) store_four<DT>(to, rest, e, f32x4{d[b][i] * by, d[b][i + 1] * by, d[b][i + 2] * by, d[b][i + 3] * by});
         }
+}
+
+// the sum of a fragment's values as they are rounded
+__device__ __forceinline__ float sum_of(const Frag<NM_DT_BF16> &f, float sum)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+    const bf16x2 *p = (const bf16x2 *)&f.v[0];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_fdot2_f32_bf16(p[j], one, sum, false);
+    return sum;
 }
 
 }  // namespace attn

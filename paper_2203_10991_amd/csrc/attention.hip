@@ -2,7 +2,8 @@
 //
 // One pass over the keys with the running maximum and sum.  A wave keeps 32 rows (attention.h) as columns: S^T = K Q^T from rows of K in LDS, P^T = 2^(c S^T - m) where it
 // lies, O^T += V^T P^T from columns of V in LDS.  The maximum m of a column moves only when a score is 2^8 times beyond it (P then stays below 2^8, sums and products in
-// binary32 are as near), so that the sums O are scaled only a few times.  Tiles of keys go through the registers of the workgroup into one of two LDS buffers while the
+// binary32 are as near), so that the sums O are scaled only a few times.  In bf16 O is divided by the sum of the probabilities as they were rounded for the second product, so
+// that they add up to one: what rounding moves is then a difference between keys.  lse takes their sum unrounded.  Tiles of keys go through the registers of the workgroup into one of two LDS buffers while the
 // other is read; one barrier a tile.  A row that sees no key: o = 0, lse = -infinity.  Rows behind their sequence's queries: the same.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
     f32x16 o[BLOCKS];
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) o[b] = f32x16{};
-    float m = -INFINITY, sum = 0.0f;
+    float m = -INFINITY, sum = 0.0f, rounded = 0.0f;                     // the sums of P, and of P as rounded
     const float c = p.scale * LOG2E;
     const F at_lane(lane);
     if (first_tile < end_tile) store(first_tile, 0);
@@ -94,6 +95,7 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
                 const float by = move ? exp2_of(m - top) : 1.0f;
                 if (move) m = top;
                 sum *= by;
+                rounded *= by;
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
@@ -103,15 +105,18 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
 #pragma unroll
             for (int a = 0; a < SB; ++a)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    x[a][i] = exp2_of(__builtin_fmaf(x[a][i], c, -base));
-                    sum += x[a][i];
-                }
+                for (int i = 0; i < 16; ++i) x[a][i] = exp2_of(__builtin_fmaf(x[a][i], c, -base));
+            if (DT == NM_DT_F32 || p.lse)
+#pragma unroll
+                for (int a = 0; a < SB; ++a)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum += x[a][i];
 #pragma unroll
             for (int a = 0; a < SB; ++a)
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const Frag<DT> w = as_fragment<DT>(x[a], 8 * g);
+                    if constexpr (DT == NM_DT_BF16) rounded = sum_of(w, rounded);
 #pragma unroll
                     for (int b = 0; b < BLOCKS; ++b) mma(o[b], F::columns(vt, 32 * a + 16 * g, b), w);
                 }
@@ -120,26 +125,26 @@ __global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2)
         __syncthreads();
     }
     sum += other_half(sum);
+    rounded = DT == NM_DT_BF16 ? rounded + other_half(rounded) : sum;
     if (row >= total) return;
     if (!there) {                                                        // (a column that was not there has taken part with zeros)
         m = -INFINITY;
-        sum = 0.0f;
+        sum = rounded = 0.0f;
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) o[b] = f32x16{};
     }
     const int64_t at = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
     if (p.splits == 1) {
-        store_column<DT, BLOCKS>((char *)row_at(p.o, p.so, s.b, query, head, ES), o, sum != 0.0f ? 1.0f / sum : 0.0f, p.D, lane);
+        store_column<DT, BLOCKS>((char *)row_at(p.o, p.so, s.b, query, head, ES), o, rounded != 0.0f ? 1.0f / rounded : 0.0f, p.D, lane, (char *)rest_at(p, s.b, query, head));
         if (p.lse && hi == 0) p.lse[at] = (m + __builtin_amdgcn_logf(sum)) * LN2;             // (log2; -infinity of a sum of zero)
     } else {
-        // O, m and the sum of this part of the keys
+        // O, m and the sums of this part of the keys
         const int64_t rows = (int64_t)p.B * p.Hq * p.Tq;
         float *to = p.part + ((int64_t)split * rows + at) * p.D;
         store_column<NM_DT_F32, BLOCKS>((char *)to, o, 1.0f, p.D, lane);
         if (hi == 0) {
-            float *st = p.part + (int64_t)p.splits * rows * p.D + ((int64_t)split * rows + at) * 2;
-            st[0] = m;
-            st[1] = sum;
+            float4 *st = (float4 *)(p.part + (int64_t)p.splits * rows * p.D) + (int64_t)split * rows + at;
+            *st = make_float4(m, sum, rounded, 0.0f);
         }
     }
 }
@@ -152,25 +157,26 @@ template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(c
     if (at >= rows || e >= p.D) return;
     const int64_t bh = at / p.Tq;
     const int query = (int)(at - bh * p.Tq), b = (int)(bh / p.Hq), head = (int)(bh - (int64_t)b * p.Hq);
-    const float *st = p.part + (int64_t)p.splits * rows * p.D;
+    const float4 *st = (const float4 *)(p.part + (int64_t)p.splits * rows * p.D) + at;
     float m = -INFINITY;
 #pragma unroll 8
-    for (int k = 0; k < p.splits; ++k) m = fmaxf(m, st[(k * rows + at) * 2]);
+    for (int k = 0; k < p.splits; ++k) m = fmaxf(m, st[k * rows].x);
     const float base = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f;
+    float sum = 0.0f, rounded = 0.0f;
     f32x4 o = {0, 0, 0, 0};
 #pragma unroll 8
     for (int k = 0; k < p.splits; ++k) {
-        const float w = exp2_of(st[(k * rows + at) * 2] - base);
+        const float4 part = st[k * rows];
+        const float w = exp2_of(part.x - base);
         const f32x4 x = *(const f32x4 *)(p.part + (k * rows + at) * p.D + e);
-        sum += w * st[(k * rows + at) * 2 + 1];
+        sum += w * part.y;
+        rounded += w * part.z;
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] += w * x[i];
     }
-    const float by = sum != 0.0f ? 1.0f / sum : 0.0f;
+    const float by = rounded != 0.0f ? 1.0f / rounded : 0.0f;
     char *to = (char *)row_at(p.o, p.so, b, query, head, DT == NM_DT_BF16 ? 2 : 4);
-    if constexpr (DT == NM_DT_BF16) *(u32x2 *)(to + e * 2) = u32x2{pack_bf16_rne(o[0] * by, o[1] * by), pack_bf16_rne(o[2] * by, o[3] * by)};
-    else *(f32x4 *)(to + e * 4) = f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by};
+    store_four<DT>(to, (char *)rest_at(p, b, query, head), e, f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by});
     if (p.lse && e == 0) p.lse[at] = (base + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
@@ -212,7 +218,7 @@ template <int DT> hipError_t launch(const AttnArg &a, const Plan &p, hipStream_t
 size_t attention_workspace(const AttnArg &a)
 {
     const attn::Plan p = attn::plan_of(a);
-    return p.splits == 1 ? 0 : (size_t)p.splits * a.B * a.Hq * a.Tq * (a.D + 2) * 4;
+    return p.splits == 1 ? 0 : (size_t)p.splits * a.B * a.Hq * a.Tq * (a.D + 4) * 4;
 }
 
 hipError_t launch_attention(AttnArg a, void *workspace, hipStream_t st)

@@ -1,5 +1,7 @@
 // Attention, gradients.  With P = 2^(c S - lse) recomputed from q, k and the forward pass's lse, delta = sum over the head of g o, dP = g v^T:
 //     dS = P (dP - delta)      dq = scale dS k      dk = scale dS^T q      dv = P^T g
+// Where a row looks at few keys, dP and delta nearly cancel, and a bf16 o makes delta too coarse; `rest` holds what its rounding took.  16 heads of 512 tokens, scores of a deviation
+// of 0.4 to 2.7: 2-norm of dq's and dk's errors 0.27 and 0.29 % without it, 0.24 % with it and with an exact delta alike (0.17 % is the rounding of the results).
 // Two kernels, each with its results in registers from beginning to end, so that no sum crosses workgroups and the same call gives the same bits:
 //   dq      a wave keeps 32 rows (attention.h) of q and g as columns: S^T = K Q^T, dP^T = V G^T, dQ^T += K^T dS^T over tiles of keys; delta comes from its own rows first
 //   dk dv   a wave keeps 32 keys as columns: S = Q K^T, dP = G V^T, dV^T += G^T P, dK^T += Q^T dS over tiles of the rows of all heads that share the keys
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     Frag<DT> q[2 * BLOCKS], g[2 * BLOCKS];
     const char *g_row = row_at(p.g, p.sg, s.b, query, head, ES);
     load_fragments<DT, BLOCKS>(g, g_row, there, p.D, lane);
-    float delta = there ? row_product<DT, BLOCKS>(g_row, row_at(p.o, p.so, s.b, query, head, ES), p.D, lane) : 0.0f;
+    float delta = there ? row_product<DT, BLOCKS>(g_row, row_at(p.o, p.so, s.b, query, head, ES), rest_at(p, s.b, query, head), p.D, lane) : 0.0f;
     delta += other_half(delta);
     load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
     // (a row that sees nothing has lse = -infinity: with +infinity in its place P is zero)

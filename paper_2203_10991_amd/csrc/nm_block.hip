@@ -232,25 +232,27 @@ size_t nm_attention_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int
     return a.group ? nm::attention_workspace(a) : 0;
 }
 
-int nm_attention(const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, float *lse, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype,
+int nm_attention(const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, float *lse, void *rest, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int dtype,
                  int causal, float scale, const int32_t *q_lens, const int32_t *k_lens, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     const char *fn = "nm_attention";
     nm::AttnArg a;
     if (int rc = check_attention(fn, a, q, k, v, B, Tq, Tk, Hq, Hk, D, dtype, causal, scale, q_lens, k_lens)) return rc;
     if (int rc = check_heads(fn, "o", o, B, Tq, Hq, D, dtype, 16, true)) return rc;
-    if (!aligned(lse, 4)) return fail(NM_ERR_ALIGN, "%s: lse is not on a 4-byte boundary", fn);
+    if (!aligned(lse, 4) || !aligned(rest, 4)) return fail(NM_ERR_ALIGN, "%s: lse or rest is not on a 4-byte boundary", fn);
     if (B == 0 || Tq == 0 || Hq == 0) { nm::abi_clear(); return NM_OK; }
     const size_t need = nm::attention_workspace(a);
     if (int rc = check_sizes(fn, a, need, workspace, workspace_bytes)) return rc;
-    const Range out[3] = {heads_range(o, B, Tq, Hq, D, dtype), range_of(lse, B * Hq * Tq * 4), range_of(workspace, (int64_t)need)};
+    if (dtype == NM_F32) rest = nullptr;
+    const Range out[4] = {heads_range(o, B, Tq, Hq, D, dtype), range_of(lse, B * Hq * Tq * 4), range_of(workspace, (int64_t)need), range_of(rest, B * Hq * Tq * D * 2)};
     const Range in[5] = {heads_range(q, B, Tq, Hq, D, dtype), heads_range(k, B, Tk, Hk, D, dtype), heads_range(v, B, Tk, Hk, D, dtype), range_of(q_lens, B * 4), range_of(k_lens, B * 4)};
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < 4; ++i)
         for (int j = 0; j < 5; ++j)
             if (overlap(out[i], in[j]) || (j < i && overlap(out[i], out[j]))) return fail(NM_ERR_ALIAS, "%s: outputs and the workspace must not overlap inputs or each other", fn);
     a.o = o->data;
     a.so = strides_of(o, B, Tq, Hq);
     a.lse = lse;
+    a.rest = rest;
     return launched(fn, nm::launch_attention(a, workspace, (hipStream_t)hip_stream));
 }
 
@@ -261,7 +263,7 @@ size_t nm_attention_grad_workspace(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq
     return a.group ? nm::attention_grad_workspace(a) : 0;
 }
 
-int nm_attention_grad(const nm_heads *g, const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, const float *lse, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq,
+int nm_attention_grad(const nm_heads *g, const nm_heads *q, const nm_heads *k, const nm_heads *v, const nm_heads *o, const float *lse, const void *rest, int64_t B, int64_t Tq, int64_t Tk, int64_t Hq,
                       int64_t Hk, int64_t D, int dtype, int causal, float scale, const int32_t *q_lens, const int32_t *k_lens, const nm_heads *dq, const nm_heads *dk, const nm_heads *dv,
                       void *workspace, size_t workspace_bytes, void *hip_stream)
 {
@@ -275,18 +277,20 @@ int nm_attention_grad(const nm_heads *g, const nm_heads *q, const nm_heads *k, c
     if (int rc = check_heads(fn, "dv", dv, B, Tk, Hk, D, dtype, 16, true)) return rc;
     if (B == 0 || Hq == 0) { nm::abi_clear(); return NM_OK; }
     if (Tq > 0 && !lse) return fail(NM_ERR_NULL, "%s: lse is NULL", fn);
-    if (!aligned(lse, 4)) return fail(NM_ERR_ALIGN, "%s: lse is not on a 4-byte boundary", fn);
+    if (!aligned(lse, 4) || !aligned(rest, 4)) return fail(NM_ERR_ALIGN, "%s: lse or rest is not on a 4-byte boundary", fn);
+    if (dtype == NM_F32) rest = nullptr;
     const size_t need = Tq > 0 ? nm::attention_grad_workspace(a) : 0;
     if (int rc = check_sizes(fn, a, need, workspace, workspace_bytes)) return rc;
     const Range out[4] = {heads_range(dq, B, Tq, Hq, D, dtype), heads_range(dk, B, Tk, Hk, D, dtype), heads_range(dv, B, Tk, Hk, D, dtype), range_of(workspace, (int64_t)need)};
-    const Range in[8] = {heads_range(q, B, Tq, Hq, D, dtype), heads_range(k, B, Tk, Hk, D, dtype), heads_range(v, B, Tk, Hk, D, dtype), heads_range(g, B, Tq, Hq, D, dtype),
-                         heads_range(o, B, Tq, Hq, D, dtype), range_of(lse, B * Hq * Tq * 4), range_of(q_lens, B * 4), range_of(k_lens, B * 4)};
+    const Range in[9] = {heads_range(q, B, Tq, Hq, D, dtype), heads_range(k, B, Tk, Hk, D, dtype), heads_range(v, B, Tk, Hk, D, dtype), heads_range(g, B, Tq, Hq, D, dtype),
+                         heads_range(o, B, Tq, Hq, D, dtype), range_of(lse, B * Hq * Tq * 4), range_of(q_lens, B * 4), range_of(k_lens, B * 4), range_of(rest, B * Hq * Tq * D * 2)};
     for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 9; ++j)
             if (overlap(out[i], in[j]) || (j < i && overlap(out[i], out[j]))) return fail(NM_ERR_ALIAS, "%s: outputs and the workspace must not overlap inputs or each other", fn);
     a.g = g->data; a.o = o->data; a.dq = dq->data; a.dk = dk->data; a.dv = dv->data;
     a.sg = strides_of(g, B, Tq, Hq); a.so = strides_of(o, B, Tq, Hq); a.sdq = strides_of(dq, B, Tq, Hq); a.sdk = strides_of(dk, B, Tk, Hk); a.sdv = strides_of(dv, B, Tk, Hk);
     a.lse = (float *)lse;
+    a.rest = (void *)rest;
     return launched(fn, nm::launch_attention_grad(a, workspace, (hipStream_t)hip_stream));
 }
 

@@ -590,7 +590,8 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int dt = code_of(q->scalar_type());
     const size_t need = p_attention_workspace(B, Tq, Tk, Hq, Hk, D, dt);
     at::Tensor o = empty(q->sizes(), q->scalar_type(), *q), lse, ws;
-    if (want) lse = empty({B, Hq, Tq}, at::kFloat, *q);
+    const bool rest = want && dt == NM_BF16;
+    if (want) lse = empty({rest ? 1 + D / 2 : 1, B, Hq, Tq}, at::kFloat, *q);
     if (need) ws = empty({(int64_t)need}, at::kByte, *q);
     const nm_heads hq = heads_of(*q), hk = heads_of(*k), hv = heads_of(*v), ho = heads_of(o);
     float *pl = want ? (float *)lse.data_ptr() : nullptr;
@@ -598,7 +599,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     int rc;
     {
         NoGil free;
-        rc = p_attention(&hq, &hk, &hv, &ho, pl, B, Tq, Tk, Hq, Hk, D, dt, causal, (float)scale, ql, kl, pw, need, st);
+        rc = p_attention(&hq, &hk, &hv, &ho, pl, rest ? pl + B * Hq * Tq : nullptr, B, Tq, Tk, Hq, Hk, D, dt, causal, (float)scale, ql, kl, pw, need, st);
     }
     if (rc) return PyLong_FromLong(rc);
     if (!want) return THPVariable_Wrap(std::move(o));
@@ -615,7 +616,7 @@ PyObject *attention_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int32_t *ql, *kl;
     if (!q || !heads_tensor(q, q) || !heads_tensor(k, q) || !heads_tensor(v, q) || !heads_tensor(g, q) || !heads_tensor(o, q) || k->sizes() != v->sizes() ||
         k->size(0) != q->size(0) || k->size(3) != q->size(3) || g->sizes() != q->sizes() || o->sizes() != q->sizes() || !lse || lse->scalar_type() != at::kFloat ||
-        lse->dim() != 3 || lse->size(0) != q->size(0) || lse->size(1) != q->size(2) || lse->size(2) != q->size(1) || !lse->is_contiguous() || lse->device() != q->device() ||
+        lse->dim() != 4 || (lse->size(0) != 1 && (q->scalar_type() == at::kFloat || lse->size(0) != 1 + q->size(3) / 2)) || lse->size(1) != q->size(0) || lse->size(2) != q->size(2) || lse->size(3) != q->size(1) || !lse->is_contiguous() || lse->device() != q->device() ||
         !lengths_tensor(a[8], *q, ql) || !lengths_tensor(a[9], *q, kl) || !on_current_device(*q))
         return none();
     const int causal = PyObject_IsTrue(a[6]);
@@ -632,7 +633,7 @@ PyObject *attention_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     int rc;
     {
         NoGil free;
-        rc = p_attention_grad(&hg, &hq, &hk, &hv, &ho, pl, B, Tq, Tk, Hq, Hk, D, dt, causal, (float)scale, ql, kl, &gq, &gk, &gv, pw, need, st);
+        rc = p_attention_grad(&hg, &hq, &hk, &hv, &ho, pl, lse->size(0) > 1 ? pl + B * Hq * Tq : nullptr, B, Tq, Tk, Hq, Hk, D, dt, causal, (float)scale, ql, kl, &gq, &gk, &gv, pw, need, st);
     }
     if (rc) return PyLong_FromLong(rc);
     return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(dq)), THPVariable_Wrap(std::move(dk)), THPVariable_Wrap(std::move(dv)));

@@ -55,7 +55,8 @@ def reference(q, k, v, g, causal, scale, q_lens=None, k_lens=None):
             # one in 8 binary orders: 40 are more than the scores here go through)
             eP = es + top + (m + 4 + 4 * 40) * E32
             o = P @ V
-            eo = (P * (eP + ut)) @ V.abs() + (m + 4) * E32 * (P @ V.abs()) + u * o.abs()
+            # (P as rounded in the product, and in the sum that it is divided by)
+            eo = (P * (eP + 2 * ut * (1 + 2 * ut))) @ V.abs() + (m + 4) * E32 * (P @ V.abs()) + u * o.abs()
             elr = top[:, 0] + (m + 4 + 4 * 40) * E32 + 4 * E32 * (base.abs() + 64)    # (lse = (m + log2 of the sum) ln 2: m and the logarithm are below 64 + |lse|)
             dP = GG @ V.t()
             delta = (GG * o).sum(1, keepdim=True)

@@ -54,9 +54,9 @@ int main()
                         const nm_heads x{at[0], ld, a, b}, y{at[1], ld, a, b}, z{at[2], ld, a, b}, o{at[3], ld, a, b}, w{at[4], INT64_MAX, ld, other};
                         nm_rotary(&x, &y, dt, a, b, other, 64, 32, (double *)at[3], at[4], 64, ld, 0, 1.f, 0, nullptr);
                         nm_rotary(&w, &x, dt, other, a, b, ld, 32, (double *)at[3], at[5], 32, ld, 1, 1.f, 1, nullptr);
-                        nm_attention(&x, &y, &z, &o, (float *)at[4], a, b, other, 8, 2, 64, dt, 1, 0.5f, (int *)at[5], (int *)at[6], at[7], SIZE_MAX / 2, nullptr);
-                        nm_attention(&x, &w, &z, &o, (float *)at[5], other, a, b, ld, other, 64, dt, 0, 0.5f, nullptr, nullptr, at[7], SIZE_MAX / 2, nullptr);
-                        nm_attention_grad(&x, &y, &z, &o, &w, (float *)at[5], other, a, b, ld, ld, 8, dt, 1, 0.5f, nullptr, nullptr, &x, &y, &z, at[7], SIZE_MAX / 2, nullptr);
+                        nm_attention(&x, &y, &z, &o, (float *)at[4], nullptr, a, b, other, 8, 2, 64, dt, 1, 0.5f, (int *)at[5], (int *)at[6], at[7], SIZE_MAX / 2, nullptr);
+                        nm_attention(&x, &w, &z, &o, (float *)at[5], nullptr, other, a, b, ld, other, 64, dt, 0, 0.5f, nullptr, nullptr, at[7], SIZE_MAX / 2, nullptr);
+                        nm_attention_grad(&x, &y, &z, &o, &w, (float *)at[5], at[8], other, a, b, ld, ld, 8, dt, 1, 0.5f, nullptr, nullptr, &x, &y, &z, at[7], SIZE_MAX / 2, nullptr);
                         nm_attention_workspace(a, b, ld, other, other, 64, dt);
                         nm_attention_grad_workspace(other, a, b, ld, other, 64, dt);
                         calls += 7;
@@ -67,13 +67,13 @@ int main()
     for (int64_t g = 1; g <= 300; ++g) {
         const int64_t Tq = (0x7fffffff - 256) / g;
         const nm_heads q{at[0], 0, 64, 64}, k{at[1], 0, 64, 0}, v{at[2], 0, 64, 0}, o{at[3], 0, 64 * g, 64};
-        expect("groups", nm_attention(&q, &k, &v, &o, nullptr, 1, Tq, 10, g, 1, 64, 1, 0, 1.f, nullptr, nullptr, nullptr, 0, nullptr), NM_OK);
+        expect("groups", nm_attention(&q, &k, &v, &o, nullptr, nullptr, 1, Tq, 10, g, 1, 64, 1, 0, 1.f, nullptr, nullptr, nullptr, 0, nullptr), NM_OK);
     }
     expect("calls that arrive", launches, 300);
     // outputs that are parts of one tensor, side by side and shifted
     const nm_heads in{at[0], 384 * 1000, 384, 64}, dq{at[1], 384 * 1000, 384, 64}, dk{(char *)at[1] + 256, 384 * 1000, 384, 64}, dv{(char *)at[1] + 512, 384 * 1000, 384, 64}, off{(char *)at[1] + 496, 384 * 1000, 384, 64};
-    expect("parts", nm_attention_grad(&in, &in, &in, &in, &in, (float *)at[5], 3, 100, 100, 2, 2, 64, 1, 1, 1.f, nullptr, nullptr, &dq, &dk, &dv, at[7], 1 << 20, nullptr), NM_OK);
-    expect("shifted parts", nm_attention_grad(&in, &in, &in, &in, &in, (float *)at[5], 3, 100, 100, 2, 2, 64, 1, 1, 1.f, nullptr, nullptr, &dq, &dk, &off, at[7], 1 << 20, nullptr), NM_ERR_ALIAS);
+    expect("parts", nm_attention_grad(&in, &in, &in, &in, &in, (float *)at[5], at[8], 3, 100, 100, 2, 2, 64, 1, 1, 1.f, nullptr, nullptr, &dq, &dk, &dv, at[7], 1 << 20, nullptr), NM_OK);
+    expect("shifted parts", nm_attention_grad(&in, &in, &in, &in, &in, (float *)at[5], at[8], 3, 100, 100, 2, 2, 64, 1, 1, 1.f, nullptr, nullptr, &dq, &dk, &off, at[7], 1 << 20, nullptr), NM_ERR_ALIAS);
     // arrays at the end of the address space
     expect("norm at the end", nm_layer_norm((void *)(UINTPTR_MAX - 127), 8, 0, nullptr, nullptr, 0, 4, 8, 0.f, at[0], 8, nullptr, nullptr, nullptr), NM_OK);
     if (errors) return 1;

@@ -69,15 +69,15 @@ def test_attention(lib):
     def sizes(B=2, Tq=8, Tk=8, Hq=2, Hk=2, D=32, dt=BF16):
         return B, Tq, Tk, Hq, Hk, D, dt
 
-    def fwd(q=tensor(0), k=tensor(1), v=tensor(2), o=tensor(3), lse=P + 0x400000, scale=0.5, ql=None, kl=None, ws=None, n=0, **kw):
-        return lib.nm_attention(q, k, v, o, lse, *sizes(**kw), 0, scale, ql, kl, ws, n, None)
+    def fwd(q=tensor(0), k=tensor(1), v=tensor(2), o=tensor(3), lse=P + 0x400000, rest=None, scale=0.5, ql=None, kl=None, ws=None, n=0, **kw):
+        return lib.nm_attention(q, k, v, o, lse, rest, *sizes(**kw), 0, scale, ql, kl, ws, n, None)
     assert fwd(dt=2) == DTYPE
     for bad in (dict(B=-1), dict(Tq=-1), dict(D=4), dict(D=12), dict(D=136), dict(Hq=3), dict(Hq=0), dict(Hk=0), dict(Hq=1), dict(Tk=1 << 31), dict(Tq=1 << 30, Hq=4), dict(B=1 << 40)):
         assert fwd(**bad) == SHAPE, bad
     assert fwd(q=tensor(0, token=-64)) == SHAPE and fwd(o=tensor(3, head=0)) == SHAPE and fwd(o=tensor(3, token=32)) == SHAPE
     assert fwd(q=None) == NULL and fwd(q=_heads(None)) == NULL and fwd(o=_heads(None)) == NULL
     assert fwd(q=_heads(P + 8)) == ALIGN and fwd(k=tensor(1, token=65)) == ALIGN and fwd(k=tensor(1, token=66), dt=F32) == ALIGN and fwd(o=tensor(3, head=36)) == ALIGN
-    assert fwd(lse=P + 0x400002) == ALIGN and fwd(ql=P + 2) == ALIGN and fwd(kl=P + 1) == ALIGN
+    assert fwd(lse=P + 0x400002) == ALIGN and fwd(rest=P + 0x480002) == ALIGN and fwd(rest=P) == ALIAS and fwd(rest=P + 0x400000) == ALIAS and fwd(ql=P + 2) == ALIGN and fwd(kl=P + 1) == ALIGN
     assert fwd(o=tensor(0)) == ALIAS and fwd(o=tensor(2)) == ALIAS and fwd(lse=P) == ALIAS and fwd(lse=P + 0x300000) == ALIAS and fwd(kl=P + 0x300000) == ALIAS
     for scale in (0.0, -1.0, float("inf"), float("nan")):
         assert fwd(scale=scale) == UNSUPPORTED
@@ -90,9 +90,9 @@ def test_attention(lib):
     need = lib.nm_attention_grad_workspace(*sizes())
     assert need >= 2 * 2 * 8 * 4 and lib.nm_attention_grad_workspace(*sizes(Tq=0)) == 0
 
-    def grad(g=tensor(0), q=tensor(1), k=tensor(2), v=tensor(3), o=tensor(4), lse=P + 0x500000, dq=tensor(6), dk=tensor(7), dv=tensor(8), ws=P + 0x900000, n=need, **kw):
-        return lib.nm_attention_grad(g, q, k, v, o, lse, *sizes(**kw), 0, 0.5, None, None, dq, dk, dv, ws, n, None)
-    assert grad(lse=None) == NULL and grad(dk=None) == NULL and grad(dv=_heads(None)) == NULL and grad(g=_heads(None)) == NULL
+    def grad(g=tensor(0), q=tensor(1), k=tensor(2), v=tensor(3), o=tensor(4), lse=P + 0x500000, rest=P + 0x580000, dq=tensor(6), dk=tensor(7), dv=tensor(8), ws=P + 0x900000, n=need, **kw):
+        return lib.nm_attention_grad(g, q, k, v, o, lse, rest, *sizes(**kw), 0, 0.5, None, None, dq, dk, dv, ws, n, None)
+    assert grad(lse=None) == NULL and grad(rest=P + 0x580001) == ALIGN and grad(rest=P + 0x600000) == ALIAS and grad(dk=None) == NULL and grad(dv=_heads(None)) == NULL and grad(g=_heads(None)) == NULL
     assert grad(ws=None) == WORKSPACE and grad(n=need - 1) == WORKSPACE and grad(ws=P + 0x900008) == ALIGN
     assert grad(dq=tensor(0)) == ALIAS and grad(dk=tensor(6)) == ALIAS and grad(dv=tensor(4)) == ALIAS and grad(ws=P + 0x600000) == ALIAS and grad(ws=P + 0x500000) == ALIAS
     assert grad(dq=tensor(6, head=0)) == SHAPE and grad(Hq=3) == SHAPE

@@ -18,7 +18,7 @@ def _all(q, k, v, g, causal, scale, ql=None, kl=None):
     mask = dict(causal=causal, scale=scale, q_lens=lens[0], k_lens=lens[1])
     o, lse = nm.nm_attention(*dev[:3], want_lse=True, **mask)
     dq, dk, dv = nm.nm_attention_grad(dev[3], *dev[:3], o, lse, **mask)
-    return dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv)
+    return dict(o=o, lse=lse[0], dq=dq, dk=dk, dv=dv)
 
 
 def _compare(q, k, v, g, causal, scale, ql=None, kl=None):
@@ -101,6 +101,26 @@ def test_gradients_against_differences(dtype):
         assert abs((got[name].cpu().double() * d).sum() - slope) <= bound
 
 
+def test_queries_that_look_at_few_keys():
+    """scores of a deviation of ten: dP and delta nearly cancel.  With what rounding took from o the errors' 2-norm stays near that of rounding dS and the result (two roundings of
+    at most 2^-8, 0.58 of that in the mean: 0.32 %); without it they are at least half as large again"""
+    import paper_2203_10991_amd as nm
+    q, k, v, g = inputs(1, 256, 256, 4, 4, 64, BF16, seed=14, spread=10.0)
+    want = reference(q, k, v, g, True, 0.125)
+    dev = [t.to(DEV) for t in (q, k, v, g)]
+    o, lse = nm.nm_attention(*dev[:3], causal=True, scale=0.125, want_lse=True)
+    assert lse.shape == (33, 1, 4, 256)
+    error = []
+    for stats in (lse, lse[:1]):
+        got = nm.nm_attention_grad(dev[3], *dev[:3], o, stats, causal=True, scale=0.125)
+        error.append([float((a.cpu().double() - want[name][0]).norm() / want[name][0].norm()) for name, a in zip(("dq", "dk"), got)])
+        for name, a in zip(("dq", "dk", "dv"), got):
+            check(name, a, want[name])
+    assert max(error[0]) < 0.0032 and all(b > 1.5 * a for a, b in zip(*error)), error
+    plain = nm.nm_attention(*dev[:3], causal=True, scale=0.125)
+    assert torch.equal(plain, o)
+
+
 def test_views():
     """parts of one tensor, heads before tokens, an expanded batch, elements apart, rows off a 16-byte boundary"""
     import paper_2203_10991_amd as nm
@@ -134,7 +154,7 @@ def test_nothing_to_do():
     for B, Tq, Tk in ((0, 4, 4), (2, 0, 4), (2, 4, 0)):
         q, k, v, g = (t.to(DEV) for t in inputs(B, Tq, Tk, 4, 2, 32, BF16))
         o, lse = nm.nm_attention(q, k, v, want_lse=True)
-        assert o.shape == q.shape and not bool(o.any()) and bool((lse == -float("inf")).all())
+        assert o.shape == q.shape and not bool(o.any()) and bool((lse[0] == -float("inf")).all())
         for d, t in zip(nm.nm_attention_grad(g, q, k, v, o, lse), (q, k, v)):
             assert d.shape == t.shape and not bool(d.any())
 
@@ -247,7 +267,7 @@ def test_refusals():
     o, lse = nm.nm_attention(q, k, v, want_lse=True)
     bad = [lambda: nm.nm_attention(q, k[:1], v[:1]), lambda: nm.nm_attention(q, k, v[:, :5]), lambda: nm.nm_attention(q.cpu(), k, v), lambda: nm.nm_attention(q[0], k, v),
            lambda: nm.nm_attention(q, k, v, k_lens=torch.ones(3, dtype=torch.int32, device=DEV)), lambda: nm.nm_attention(q, k, v, k_lens=torch.ones(2, dtype=torch.int32)),
-           lambda: nm.nm_attention_grad(g, q, k, v, o, lse[:, :, :3]), lambda: nm.nm_attention_grad(g[:, :3], q, k, v, o, lse),
+           lambda: nm.nm_attention_grad(g, q, k, v, o, lse[..., :3]), lambda: nm.nm_attention_grad(g, q, k, v, o, lse[0]), lambda: nm.nm_attention_grad(g, q, k, v, o, lse[:5]), lambda: nm.nm_attention_grad(g[:, :3], q, k, v, o, lse),
            lambda: nm.nm_attention_grad(g, q, k, v, o, lse, out=(q[:, :3], k, v))]
     for call in bad:
         with pytest.raises(ValueError):
