@@ -288,17 +288,51 @@ template <int DT> __device__ __forceinline__ void store_four(char *to, char *res
         }
     } else *(f32x4 *)(to + e * 4) = x;
 }
-// a column of D blocks (an output row of D elements) times `by`, to memory
+// Two words of both halves of a wave: the lower half keeps its first and gets the other's first behind it, the upper half keeps its second and gets the other's second in front
+__device__ __forceinline__ void join_halves(uint32_t &first, uint32_t &second)
+{
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(first, second, false, false));
+    first = r[0];
+    second = r[1];
+}
+// a column of D blocks (an output row of D elements) times `by`, to memory.  A lane holds 4 of every 8 elements of its row and lane + 32 the others; in bf16 they exchange
+// every other 4, so that each writes 16 bytes.
 template <int DT, int BLOCKS> __device__ __forceinline__ void store_column(char *to, const f32x16 (&d)[BLOCKS], float by, int D, int lane, char *rest = nullptr)
 {
     const int hi = lane >> 5;
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b)
+    for (int b = 0; b < BLOCKS; ++b) {
+        if constexpr (DT == NM_DT_BF16) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int e = 32 * b + 8 * (i >> 2) + 4 * hi;
-            if (e < D) store_four<DT>(to, rest, e, f32x4{d[b][i] * by, d[b][i + 1] * by, d[b][i + 2] * by, d[b][i + 3] * by});
+            for (int i = 0; i < 16; i += 8) {
+                const int e = 32 * b + 2 * i + 8 * hi;
+                float x[8];
+                uint32_t w[4], r[4];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = d[b][i + j] * by;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j] = pack_bf16_rne(x[2 * j], x[2 * j + 1]);
+                    r[j] = pack_bf16_rne(x[2 * j] - __uint_as_float(w[j] << 16), x[2 * j + 1] - __uint_as_float(w[j] & 0xffff0000u));
+                }
+                join_halves(w[0], w[2]);
+                join_halves(w[1], w[3]);
+                if (e < D) *(u32x4 *)(to + e * 2) = u32x4{w[0], w[1], w[2], w[3]};
+                if (rest) {
+                    typedef u32x4 any __attribute__((aligned(4)));
+                    join_halves(r[0], r[2]);
+                    join_halves(r[1], r[3]);
+                    if (e < D) *(any *)(rest + e * 2) = u32x4{r[0], r[1], r[2], r[3]};
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int e = 32 * b + 8 * (i >> 2) + 4 * hi;
+                if (e < D) *(f32x4 *)(to + e * 4) = f32x4{d[b][i] * by, d[b][i + 1] * by, d[b][i + 2] * by, d[b][i + 3] * by};
+            }
         }
+    }
 }
 
 // the sum of a fragment's values as they are rounded

@@ -20,7 +20,7 @@ namespace attn {
 constexpr float MOVE = 8.0f;     // a maximum moves when it is beaten by this power of two
 
 template <int DT, int BLOCKS, int WAVES, int KEYS>
-__global__ __launch_bounds__(64 * WAVES, BLOCKS == 4 && DT == NM_DT_F32 ? 1 : 2) void attention_kernel(const AttnArg p, int row_tiles)
+__global__ __launch_bounds__(64 * WAVES, DT == NM_DT_F32 && BLOCKS + (WAVES == 1) > 2 ? 1 : 2) void attention_kernel(const AttnArg p, int row_tiles)
 {
     typedef Lane<DT, BLOCKS, KEYS> F;
     constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, THREADS = 64 * WAVES, ROWS = 32 * WAVES, SB = KEYS / 32;
