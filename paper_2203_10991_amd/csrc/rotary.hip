@@ -19,66 +19,69 @@ namespace {
 constexpr int V = EW;            // elements of a vector
 
 // the first `left` of V elements at an element's boundary
-template <int DT> __device__ __forceinline__ void load_v(float (&v)[V], const void *p, int64_t at, int left)
-{
-    const Raw<DT> r = left >= V ? load_raw<DT>(p, at) : load_raw<DT, true>(p, at, left);
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = element(r, i);
-}
+template <int DT> __device__ __forceinline__ Raw<DT> load_v(const void *p, int64_t at, int left) { return left >= V ? load_raw<DT>(p, at) : load_raw<DT, true>(p, at, left); }
 
-// 2^lane_bits threads to a head, 2^head_bits heads, and what is left of 256 threads as tokens of a workgroup; `turned` vectors (or pairs of them), `copied` vectors behind the part
+// 2^lane_bits threads to a head, 2^head_bits heads, and what is left of 256 threads as tokens of a workgroup; `turned` vectors (or pairs of them), `copied` vectors behind the part.
+// A thread's first vectors are on their way while the angles are made.
 template <int DT, bool INTERLEAVED> __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArg p, int lane_bits, int head_bits, int turned, int copied)
 {
     extern __shared__ float2 turns[];
     const int tokens = 256 >> (lane_bits + head_bits), pairs = p.part / 2;
     const int64_t first = (int64_t)grid_place(blockIdx.x, blockIdx.y) * tokens, n = p.B * p.T;
+    if (first >= n) return;
+    const int lane = (int)threadIdx.x & ((1 << lane_bits) - 1), head0 = (int)threadIdx.x >> lane_bits & ((1 << head_bits) - 1), token = (int)threadIdx.x >> (lane_bits + head_bits);
+    const bool there = first + token < n;
+    const uint32_t at_token = (uint32_t)(there ? first + token : first), b = at_token / (uint32_t)p.T, t = at_token - b * (uint32_t)p.T;
+    const int64_t x0 = b * p.sx.b + t * p.sx.t, y0 = b * p.sy.b + t * p.sy.t;
+    // elements of a head that chunk c has, and where they begin
+    auto begin = [&](int c) { return c < turned ? c * V : p.part + (c - turned) * V; };
+    auto left_of = [&](int c) { return c >= turned ? p.D - begin(c) : INTERLEAVED ? p.part - begin(c) : pairs - begin(c); };
+    Raw<DT> v, w;
+    auto load = [&](int head, int c) {
+        v = load_v<DT>(p.x, x0 + head * p.sx.h + begin(c), left_of(c));
+        if (!INTERLEAVED && c < turned) w = load_v<DT>(p.x, x0 + head * p.sx.h + begin(c) + pairs, left_of(c));
+    };
+    if (there && head0 < p.H && lane < turned + copied) load(head0, lane);
     for (int i = threadIdx.x; i < tokens * pairs; i += 256) {
         const int k = i / pairs, j = i - k * pairs;
         if (first + k >= n) break;
-        const int64_t b = (first + k) / p.T, t = first + k - b * p.T;
-        const int64_t pos = !p.positions ? t : p.wide ? ((const int64_t *)p.positions)[b * p.pos_b + t] : ((const int32_t *)p.positions)[b * p.pos_b + t];
+        const uint32_t at = (uint32_t)(first + k), kb = at / (uint32_t)p.T, kt = at - kb * (uint32_t)p.T;
+        const int64_t pos = !p.positions ? (int64_t)kt : p.wide ? ((const int64_t *)p.positions)[kb * p.pos_b + kt] : ((const int32_t *)p.positions)[kb * p.pos_b + kt];
         const double turn = (double)pos * (p.freqs[j] * 0.15915494309189533577);
         float sn, cs;
         sincospif(2.0f * (float)(turn - rint(turn)), &sn, &cs);
         turns[i] = make_float2(cs * p.scale, sn * p.scale * p.sign);
     }
     __syncthreads();
-    const int lane = (int)threadIdx.x & ((1 << lane_bits) - 1), head0 = (int)threadIdx.x >> lane_bits & ((1 << head_bits) - 1), token = (int)threadIdx.x >> (lane_bits + head_bits);
-    if (first + token >= n) return;
-    const int64_t b = (first + token) / p.T, t = first + token - b * p.T;
+    if (!there) return;
     const float2 *cs = turns + token * pairs;
     for (int head = head0; head < p.H; head += 1 << head_bits) {
-        const int64_t x0 = b * p.sx.b + t * p.sx.t + head * p.sx.h, y0 = b * p.sy.b + t * p.sy.t + head * p.sy.h;
+        const int64_t to = y0 + head * p.sy.h;
         for (int c = lane; c < turned + copied; c += 1 << lane_bits) {
-            float v[V], y[V];
+            if (head != head0 || c != lane) load(head, c);
+            const int at = begin(c), left = left_of(c);
+            float y[V];
             if (c >= turned) {
-                const int at = p.part + (c - turned) * V, left = p.D - at;
-                load_v<DT>(v, p.x, x0 + at, left);
-                store_row<DT>(p.y, y0 + at, 0, left, v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = element(v, i);
             } else if constexpr (INTERLEAVED) {
-                const int at = c * V, left = p.part - at;
-                load_v<DT>(v, p.x, x0 + at, left);
 #pragma unroll
                 for (int i = 0; i < V; i += 2) {
                     const float2 k = cs[min(at / 2 + i / 2, pairs - 1)];
-                    y[i] = v[i] * k.x - v[i + 1] * k.y;
-                    y[i + 1] = v[i] * k.y + v[i + 1] * k.x;
+                    y[i] = element(v, i) * k.x - element(v, i + 1) * k.y;
+                    y[i + 1] = element(v, i) * k.y + element(v, i + 1) * k.x;
                 }
-                store_row<DT>(p.y, y0 + at, 0, left, y);
             } else {
-                const int at = c * V, left = pairs - at;
-                float w[V], z[V];
-                load_v<DT>(v, p.x, x0 + at, left);
-                load_v<DT>(w, p.x, x0 + pairs + at, left);
+                float z[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float2 k = cs[min(at + i, pairs - 1)];
-                    y[i] = v[i] * k.x - w[i] * k.y;
-                    z[i] = v[i] * k.y + w[i] * k.x;
+                    y[i] = element(v, i) * k.x - element(w, i) * k.y;
+                    z[i] = element(v, i) * k.y + element(w, i) * k.x;
                 }
-                store_row<DT>(p.y, y0 + at, 0, left, y);
-                store_row<DT>(p.y, y0 + pairs + at, 0, left, z);
+                store_row<DT>(p.y, to + pairs + at, 0, left, z);
             }
+            store_row<DT>(p.y, to + at, 0, left, y);
         }
     }
 }
