@@ -19,13 +19,14 @@ namespace attn {
 
 constexpr float MOVE = 8.0f;     // a maximum moves when it is beaten by this power of two
 
-template <int DT, int BLOCKS, int WAVES, int KEYS>
-__global__ __launch_bounds__(64 * WAVES, DT == NM_DT_F32 && BLOCKS + (WAVES == 1) > 2 ? 1 : 2) void attention_kernel(const AttnArg p, int row_tiles)
+// WAVES blocks of 32 rows; PARTS: two waves to a block, each with one half of a tile's keys, whose results are joined at the end
+template <int DT, int BLOCKS, int WAVES, int KEYS, int PARTS>
+__global__ __launch_bounds__(64 * WAVES * PARTS, DT == NM_DT_F32 && BLOCKS + (WAVES == 1) > 2 ? 1 : 2) void attention_kernel(const AttnArg p, int row_tiles)
 {
     typedef Lane<DT, BLOCKS, KEYS> F;
-    constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, THREADS = 64 * WAVES, ROWS = 32 * WAVES, SB = KEYS / 32;
+    constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, THREADS = 64 * WAVES * PARTS, ROWS = 32 * WAVES, SB = KEYS / 32 / PARTS;
     __shared__ __align__(16) char lds[2][2][F::BYTES];
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
+    const int lane = (int)threadIdx.x & 63, wave = ((int)threadIdx.x >> 6) % WAVES, part = ((int)threadIdx.x >> 6) / WAVES, hi = lane >> 5;
     // the tiles of a head side by side, those with most keys first
     const uint32_t place = place_of(blockIdx.x, gridDim.x, row_tiles, DT == NM_DT_BF16 || BLOCKS < 3), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)row_tiles;
     const int tile = row_tiles - 1 - (int)(whole - bh * row_tiles), split = (int)(place - whole * p.splits);
@@ -67,9 +68,11 @@ __global__ __launch_bounds__(64 * WAVES, DT == NM_DT_F32 && BLOCKS + (WAVES == 1
     if (first_tile < end_tile) store(first_tile, 0);
     __syncthreads();
     for (int t = first_tile; t < end_tile; ++t) {
-        const uint32_t kt = at_lane.rows_of(lds_address(lds[t - first_tile & 1][0])), vt = at_lane.columns_of(lds_address(lds[t - first_tile & 1][1]));
+        const uint32_t mine = (uint32_t)(part * 32 * SB * Tile<BLOCKS>::ROW);
+        const uint32_t kt = at_lane.rows_of(lds_address(lds[t - first_tile & 1][0]) + mine), vt = at_lane.columns_of(lds_address(lds[t - first_tile & 1][1]) + mine);
+        const int key0 = t * KEYS + part * 32 * SB;
         if (t + 1 < end_tile) load(t + 1);
-        if (t * KEYS < wave_most) {
+        if (key0 < wave_most) {
             f32x16 x[SB];
 #pragma unroll
             for (int a = 0; a < SB; ++a) {
@@ -77,12 +80,12 @@ __global__ __launch_bounds__(64 * WAVES, DT == NM_DT_F32 && BLOCKS + (WAVES == 1
 #pragma unroll
                 for (int kk = 0; kk < 2 * BLOCKS; ++kk) mma(x[a], F::rows(kt, 32 * a, kk), q[kk]);
             }
-            if ((t + 1) * KEYS > wave_least) {
+            if (key0 + 32 * SB > wave_least) {
 #pragma unroll
                 for (int a = 0; a < SB; ++a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (t * KEYS + 32 * a + row_of(i, hi) >= seen) x[a][i] = -INFINITY;
+                        if (key0 + 32 * a + row_of(i, hi) >= seen) x[a][i] = -INFINITY;
             }
             float top = x[0][0];
 #pragma unroll
@@ -123,6 +126,30 @@ __global__ __launch_bounds__(64 * WAVES, DT == NM_DT_F32 && BLOCKS + (WAVES == 1
         }
         if (t + 1 < end_tile) store(t + 1, (t - first_tile & 1) ^ 1);
         __syncthreads();
+    }
+    if constexpr (PARTS == 2) {
+        float *other = (float *)&lds[0][0][0] + (wave * BLOCKS * 16) * 64 + lane;
+        static_assert(sizeof lds >= (size_t)WAVES * BLOCKS * 16 * 64 * 4, "a block's sums go through the tiles' place");
+        __shared__ float stats[3][64 * WAVES];
+        if (part) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) other[(16 * b + i) * 64] = o[b][i];
+            stats[0][wave * 64 + lane] = m;
+            stats[1][wave * 64 + lane] = sum;
+            stats[2][wave * 64 + lane] = rounded;
+        }
+        __syncthreads();
+        if (part) return;
+        const float m2 = stats[0][wave * 64 + lane], top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top, w1 = exp2_of(m - base), w2 = exp2_of(m2 - base);
+        m = top;
+        sum = sum * w1 + stats[1][wave * 64 + lane] * w2;
+        rounded = rounded * w1 + stats[2][wave * 64 + lane] * w2;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] = o[b][i] * w1 + other[(16 * b + i) * 64] * w2;
     }
     sum += other_half(sum);
     rounded = DT == NM_DT_BF16 ? rounded + other_half(rounded) : sum;
@@ -181,7 +208,7 @@ template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(c
 }
 
 // how many rows a workgroup takes, and in how many parts the keys go
-struct Plan { int waves, keys, splits; int64_t row_tiles; };
+struct Plan { int waves, keys, splits, parts; int64_t row_tiles; };
 inline Plan plan_of(const AttnArg &a)
 {
     Plan p;
@@ -192,15 +219,20 @@ inline Plan plan_of(const AttnArg &a)
     const int64_t wgs = heads * p.row_tiles, want = (p.waves == 1 ? 8 : 2) * NM_CUS;
     const int64_t least = p.waves == 1 ? 128 : 512;                     // keys to a part
     p.splits = wgs >= want / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, (a.Tk + least - 1) / least, 64}));
+    // two waves to a block of rows where a CU has one workgroup at most, in binary32 (full attention, one wave and two, in us: 8 x 197 tokens of 12 heads of 64 17.6 and 15.4,
+    // 2 x 1000 of 4 heads on one 37.7 and 29.9; with two workgroups to a CU, 2 x 1333 of 12 on one of 48, 74 and 77).  In bf16, where a tile is a third of the work, there is nothing
+    // in it (8 x 197: 9.5 and 9.5, 6 x 256 of 16 of 128: 14.5 and 15.3)
+    p.parts = a.dt == NM_DT_F32 && a.D <= 64 && a.Tk > 64 && p.waves == 4 && wgs * p.splits < NM_CUS ? 2 : 1;
     return p;
 }
 
 template <int DT, int BLOCKS> hipError_t launch(const AttnArg &a, const Plan &p, hipStream_t st)
 {
     const int64_t wgs = (int64_t)a.B * a.Hk * p.row_tiles * p.splits;
-    if (!grid_holds(wgs, 64 * p.waves) || wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
-    if (p.waves == 1) attention_kernel<DT, BLOCKS, 1, 32><<<dim3((unsigned)wgs), dim3(64), 0, st>>>(a, (int)p.row_tiles);
-    else attention_kernel<DT, BLOCKS, 4, DT == NM_DT_F32 ? 32 : 64><<<dim3((unsigned)wgs), dim3(256), 0, st>>>(a, (int)p.row_tiles);
+    if (!grid_holds(wgs, 64 * p.waves * p.parts) || wgs > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (p.waves == 1) attention_kernel<DT, BLOCKS, 1, 32, 1><<<dim3((unsigned)wgs), dim3(64), 0, st>>>(a, (int)p.row_tiles);
+    else if (p.parts == 1) attention_kernel<DT, BLOCKS, 4, DT == NM_DT_F32 ? 32 : 64, 1><<<dim3((unsigned)wgs), dim3(256), 0, st>>>(a, (int)p.row_tiles);
+    else if constexpr (DT == NM_DT_F32 && BLOCKS <= 2) attention_kernel<DT, BLOCKS, 4, 64, 2><<<dim3((unsigned)wgs), dim3(512), 0, st>>>(a, (int)p.row_tiles);
     return hipGetLastError();
 }
 template <int DT> hipError_t launch(const AttnArg &a, const Plan &p, hipStream_t st)

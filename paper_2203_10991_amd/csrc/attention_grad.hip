@@ -19,13 +19,14 @@ namespace nm {
 
 namespace attn {
 
-template <int DT, int BLOCKS, int KEYS>
-__global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void attention_dq_kernel(const AttnArg p, int row_tiles)
+// PARTS: two waves to a block of rows, each with one half of a tile's keys, whose sums are added up at the end
+template <int DT, int BLOCKS, int KEYS, int PARTS>
+__global__ __launch_bounds__(256 * PARTS, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void attention_dq_kernel(const AttnArg p, int row_tiles)
 {
     typedef Lane<DT, BLOCKS, KEYS> F;
-    constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, ROWS = 128, SB = KEYS / 32;
+    constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, ROWS = 128, SB = KEYS / 32 / PARTS;
     __shared__ __align__(16) char lds[2][2][F::BYTES];
-    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
+    const int lane = (int)threadIdx.x & 63, wave = ((int)threadIdx.x >> 6) % 4, part = ((int)threadIdx.x >> 6) / 4, hi = lane >> 5;
     const uint32_t place = place_of(blockIdx.x, gridDim.x, row_tiles, DT == NM_DT_BF16 || BLOCKS < 3), bh = place / (uint32_t)row_tiles;
     const int tile = row_tiles - 1 - (int)(place - bh * row_tiles);
     const Sequence s(p, (int)bh);
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     const int seen = s.seen(p, query), tiles = (most + KEYS - 1) / KEYS;
 
     const char *k0 = row_at(p.k, p.sk, s.b, 0, s.h, ES), *v0 = row_at(p.v, p.sv, s.b, 0, s.h, ES);
-    Stage<DT, BLOCKS, KEYS, 256> ks, vs;
+    Stage<DT, BLOCKS, KEYS, 256 * PARTS> ks, vs;
     auto load = [&](int t) {
         const int64_t key0 = (int64_t)t * KEYS;
         const int rows = min(KEYS, s.nk - t * KEYS);
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     load_fragments<DT, BLOCKS>(q, row_at(p.q, p.sq, s.b, query, head, ES), there, p.D, lane);
     // (a row that sees nothing has lse = -infinity: with +infinity in its place P is zero)
     const float l = there ? p.lse[((int64_t)s.b * p.Hq + head) * p.Tq + query] : -INFINITY, lse = l == -INFINITY ? INFINITY : l * LOG2E, c = p.scale * LOG2E;
-    if (hi == 0 && row < total) p.rows[(int64_t)bh * total + row] = make_float2(lse, delta);
+    if (hi == 0 && part == 0 && row < total) p.rows[(int64_t)bh * total + row] = make_float2(lse, delta);
     f32x16 dq[BLOCKS];
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) dq[b] = f32x16{};
@@ -69,10 +70,12 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
     if (tiles > 0) store(0);
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
-        const uint32_t kt = at_lane.rows_of(lds_address(lds[t & 1][0])), vt = at_lane.rows_of(lds_address(lds[t & 1][1])), kc = at_lane.columns_of(lds_address(lds[t & 1][0]));
+        const uint32_t mine = (uint32_t)(part * 32 * SB * Tile<BLOCKS>::ROW), k_at = lds_address(lds[t & 1][0]) + mine;
+        const uint32_t kt = at_lane.rows_of(k_at), vt = at_lane.rows_of(lds_address(lds[t & 1][1]) + mine), kc = at_lane.columns_of(k_at);
+        const int key0 = t * KEYS + part * 32 * SB;
         if (t + 1 < tiles) load(t + 1);
-        if (t * KEYS < wave_most) {
-            const bool edge = (t + 1) * KEYS > wave_least;
+        if (key0 < wave_most) {
+            const bool edge = key0 + 32 * SB > wave_least;
 #pragma unroll
             for (int a = 0; a < SB; ++a) {
                 f32x16 x = f32x16{}, dp = f32x16{};
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
                 if (edge) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (t * KEYS + 32 * a + row_of(i, hi) >= seen) x[i] = 0.0f;
+                        if (key0 + 32 * a + row_of(i, hi) >= seen) x[i] = 0.0f;
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -99,11 +102,31 @@ __global__ __launch_bounds__(256, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2) void at
         if (t + 1 < tiles) store(t + 1);
         __syncthreads();
     }
+    if constexpr (PARTS == 2) {
+        float *other = (float *)&lds[0][0][0] + (wave * BLOCKS * 16) * 64 + lane;
+        static_assert(sizeof lds >= (size_t)4 * BLOCKS * 16 * 64 * 4, "a block's sums go through the tiles' place");
+        if (part) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) other[(16 * b + i) * 64] = dq[b][i];
+        }
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dq[b][i] += other[(16 * b + i) * 64];
+    }
     if (!there)
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) dq[b] = f32x16{};
     if (row < total) store_column<DT, BLOCKS>((char *)row_at(p.dq, p.sdq, s.b, query, head, ES), dq, p.scale, p.D, lane);
 }
+
+// Whether two waves share a block of rows in attention_dq_kernel: where CUs stay without a workgroup and the keys are many.  All gradients, one wave and two, in us: 1 x 2000 tokens of 8 heads
+// of 64 95 and 87 (binary32 275 and 254), 2 x 1333 of 12 heads on one of 48 74 and 69, 500 of 16 on four of 128 57 and 55; but 2 x 300 of 8 of 64 26.3 and 26.8, 4 x 256 of 16 23.2 and 24.3
+inline bool two_parts(const AttnArg &a, int64_t wgs) { return wgs < NM_CUS && a.Tk >= 512 && (a.dt == NM_DT_BF16 || a.D <= 64); }
 
 // the tiles of rows that see any key from key0 on: those of queries from a first one on
 struct RowTiles {
@@ -311,8 +334,13 @@ template <typename P> hipError_t launch_grads(const AttnArg &a, P, hipStream_t s
     typedef typename P::W W;
     const int64_t heads = (int64_t)a.B * a.Hk, row_tiles = ((int64_t)a.Tq * a.group + 127) / 128, kt = ((int64_t)a.Tk + 32 * W::waves - 1) / (32 * W::waves);
     const int64_t wq = heads * row_tiles, wk = heads * kt * a.splits, ws = (heads * a.Tk * a.D / 4 + 255) / 256;
-    if (std::max(wq, wk) > 0x7fffffff || !grid_holds(std::max(wq, wk), 64 * W::waves) || !grid_holds(wq, 256) || !grid_holds(ws, 256)) return hipErrorInvalidConfiguration;
-    if (wq > 0) attention_dq_kernel<DT, BLOCKS, KEYS><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
+    if (std::max(wq, wk) > 0x7fffffff || !grid_holds(std::max(wq, wk), 64 * W::waves) || !grid_holds(wq, 512) || !grid_holds(ws, 256)) return hipErrorInvalidConfiguration;
+    if (wq > 0) {
+        if constexpr (DT == NM_DT_BF16 || BLOCKS <= 2) {
+            if (two_parts(a, wq)) attention_dq_kernel<DT, BLOCKS, 64, 2><<<dim3((unsigned)wq), dim3(512), 0, st>>>(a, (int)row_tiles);
+            else attention_dq_kernel<DT, BLOCKS, KEYS, 1><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
+        } else attention_dq_kernel<DT, BLOCKS, KEYS, 1><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || wk == 0) return e;
     attention_dkdv_kernel<DT, BLOCKS, KEY_ROWS, W::waves, W::per_simd, W::v_in_lds, W::buffers><<<dim3((unsigned)wk), dim3(64 * W::waves), 0, st>>>(a, (int)kt);

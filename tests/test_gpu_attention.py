@@ -41,6 +41,15 @@ def test_against_binary64(B, Tq, Tk, H, K, D, causal, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,Tq,Tk,H,K,D,ql,kl", [(3, 150, 600, 2, 1, 24, [150, 33, 0], [600, 31, 555]), (2, 129, 513, 2, 2, 64, [129, 128], [513, 480]), (2, 520, 520, 2, 1, 48, [520, 400], [520, 33]),
+                                                 (2, 140, 530, 3, 1, 80, [140, 1], [530, 1]), (1, 200, 1100, 2, 2, 128, [200], [1030]), (2, 100, 100, 2, 2, 64, [100, 97], [96, 65])])
+def test_few_workgroups(B, Tq, Tk, H, K, D, ql, kl, causal, dtype):
+    """two waves to a block of rows: halves of a tile that hold no key, or none that a row sees"""
+    _compare(*inputs(B, Tq, Tk, H, K, D, dtype, seed=13), causal, D ** -0.5, ql, kl)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("Tq,Tk,ql,kl", [(70, 70, [70, 1, 0, 33, 69, 32], [70, 1, 0, 33, 69, 32]), (40, 90, [40, 40, 3, 0, 40, 7], [90, 20, 0, 64, 1, 65]),
                                          (1, 130, [1, 1, 1, 0, 1, 1], [130, 0, 1, 64, 129, 33])])
 def test_lengths_and_what_lies_behind(Tq, Tk, ql, kl, causal, dtype):
