@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "gemm_plan.h"           // NM_CUS
 #include "nm_internal.h"
 #include "prune_common.h"        // pack_bf16_rne
 
@@ -168,12 +169,36 @@ struct Sequence {
 // have few tiles, every other 32, since 32 are then whole heads and a CU would get the same tile of each.  2 x 4096 tokens, 8 heads of 64 in binary32, causal, all
 // workgroups at once: forward 560 us without, 233 with; 32 x 512 tokens, 16 heads of 64: dk dv 95 and 81 us.  Where a CU holds one, the list as it is: whoever is
 // done takes the longest that is left (2 x 8192 tokens, 64 heads of 128 over 8: dk dv 4.6 ms, in reverse 6.5).
-__device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t n, int tiles, bool two)
+__device__ __forceinline__ uint32_t place_of(uint32_t id, uint32_t n, bool every_other, bool two)
 {
     const uint32_t x = id % 8, i = id / 8, round = i / 32, at = i % 32;
     if (round >= n / 256) return id;
-    const bool reverse = tiles <= 16 ? round & 1 : two && round == 1;
+    const bool reverse = every_other ? round & 1 : two && round == 1;
     return (round * 8 + (round & 1 ? 7 - x : x)) * 32 + (reverse ? 31 - at : at);
+}
+// a workgroup's head of keys, its tile in the order of falling work, and its part of it; the tiles of `mix` heads stand in the list together
+struct Place {
+    uint32_t bh;
+    int tile, split;
+    __device__ __forceinline__ Place(const AttnArg &p, int tiles, int splits, bool two)
+    {
+        const uint32_t at = place_of(blockIdx.x, gridDim.x, p.mix > 1 || tiles <= 16, two), whole = splits == 1 ? at : at / (uint32_t)splits;
+        split = (int)(at - whole * splits);
+        const uint32_t set = whole / (uint32_t)(tiles * p.mix), in = whole - set * tiles * p.mix, heads = min((uint32_t)p.mix, (uint32_t)(p.B * p.Hk) - set * p.mix);
+        tile = (int)(in / heads);
+        bh = set * p.mix + in - tile * heads;
+    }
+};
+// How many heads that is.  Where the list is a few rounds long, all of them, so that the longest tiles of every head start first: forward / gradients, 6 x up to 1333 tokens, 12 heads of 80 over
+// 1: 47 / 147 us a head at a time, 36 / 129 so; 4 x 2048, 16 heads of 64: 73 / 221 and 63 / 175; 12 x 1200, 12 heads of 40: 60 / 165 and 51 / 137; 8 x 1000, 16 heads of 64 over 4, lengths from
+// half: 28.2 / 101 and 29.9 / 102.  Where it is longer, a head at a time (all: 2 x 8192, 64 heads of 128 over 8 2764 and 2865 us), but with lengths and many tiles to a head eight: empty tiles of short
+// sequences come at the same place of every head's, which is the same XCD's (8 x up to 8192, 32 heads of 128 over 8 4900 / 13000 and 3490 / 11200; 4 x up to 4096 583 / 1840 and 522 / 1570;
+// with 32 tiles to a head, 16 x up to 4096, 16 heads of 64, eight heads at a time are 674 / 1695 against 533 / 1490: runs of 32 no longer share keys).
+inline int mix_of(const AttnArg &a, int64_t heads, int64_t tiles)
+{
+    if (!a.causal || tiles <= 8) return 1;
+    if (heads * tiles <= 6 * NM_CUS) return (int)heads;
+    return (a.q_lens || a.k_lens) && tiles >= 64 ? 8 : 1;
 }
 
 // the first of part k of n parts of some tiles (2^26 at most)

@@ -28,9 +28,9 @@ __global__ __launch_bounds__(64 * WAVES * PARTS, DT == NM_DT_F32 && BLOCKS + (WA
     __shared__ __align__(16) char lds[2][2][F::BYTES];
     const int lane = (int)threadIdx.x & 63, wave = ((int)threadIdx.x >> 6) % WAVES, part = ((int)threadIdx.x >> 6) / WAVES, hi = lane >> 5;
     // the tiles of a head side by side, those with most keys first
-    const uint32_t place = place_of(blockIdx.x, gridDim.x, row_tiles, DT == NM_DT_BF16 || BLOCKS < 3), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)row_tiles;
-    const int tile = row_tiles - 1 - (int)(whole - bh * row_tiles), split = (int)(place - whole * p.splits);
-    const Sequence s(p, (int)bh);
+    const Place place(p, row_tiles, p.splits, DT == NM_DT_BF16 || BLOCKS < 3);
+    const int tile = row_tiles - 1 - place.tile, split = place.split;
+    const Sequence s(p, (int)place.bh);
     const int total = p.Tq * p.group, r0 = tile * ROWS;
     const int row = r0 + wave * 32 + (lane & 31), query = query_of(min(row, total - 1), p), head = s.h * p.group + min(row, total - 1) - query * p.group;
     const bool there = row < total && query < s.nq;
@@ -258,6 +258,7 @@ hipError_t launch_attention(AttnArg a, void *workspace, hipStream_t st)
     const attn::Plan p = attn::plan_of(a);
     a.splits = p.splits;
     a.part = (float *)workspace;
+    a.mix = attn::mix_of(a, (int64_t)a.B * a.Hk, p.row_tiles);
     hipError_t e = a.dt == NM_DT_BF16 ? attn::launch<NM_DT_BF16>(a, p, st) : attn::launch<NM_DT_F32>(a, p, st);
     if (e != hipSuccess || p.splits == 1) return e;
     const int shift = a.D <= 32 ? 3 : a.D <= 64 ? 4 : 5;

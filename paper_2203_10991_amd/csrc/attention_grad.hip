@@ -27,8 +27,9 @@ __global__ __launch_bounds__(256 * PARTS, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2)
     constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, ROWS = 128, SB = KEYS / 32 / PARTS;
     __shared__ __align__(16) char lds[2][2][F::BYTES];
     const int lane = (int)threadIdx.x & 63, wave = ((int)threadIdx.x >> 6) % 4, part = ((int)threadIdx.x >> 6) / 4, hi = lane >> 5;
-    const uint32_t place = place_of(blockIdx.x, gridDim.x, row_tiles, DT == NM_DT_BF16 || BLOCKS < 3), bh = place / (uint32_t)row_tiles;
-    const int tile = row_tiles - 1 - (int)(place - bh * row_tiles);
+    const Place place(p, row_tiles, 1, DT == NM_DT_BF16 || BLOCKS < 3);
+    const uint32_t bh = place.bh;
+    const int tile = row_tiles - 1 - place.tile;
     const Sequence s(p, (int)bh);
     const int total = p.Tq * p.group, r0 = tile * ROWS;
     const int row = r0 + wave * 32 + (lane & 31), query = query_of(min(row, total - 1), p), head = s.h * p.group + min(row, total - 1) - query * p.group;
@@ -151,8 +152,9 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
     __shared__ float lse_of[BUFFERS][ROWS], delta_of[BUFFERS][ROWS];
     __shared__ int seen_of[BUFFERS][ROWS];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
-    const uint32_t place = place_of(blockIdx.x, gridDim.x, key_tiles, PER_SIMD * 4 >= 2 * WAVES), whole = p.splits == 1 ? place : place / (uint32_t)p.splits, bh = whole / (uint32_t)key_tiles;
-    const int tile = (int)(whole - bh * key_tiles), split = (int)(place - whole * p.splits);       // (the first keys have most rows)
+    const Place place(p, key_tiles, p.splits, PER_SIMD * 4 >= 2 * WAVES);
+    const uint32_t bh = place.bh;
+    const int tile = place.tile, split = place.split;                    // (the first keys have most rows)
     const Sequence s(p, (int)bh);
     const int key0 = tile * KEYS, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
     const int total = s.nq * p.group;
@@ -328,7 +330,7 @@ template <typename F> auto with_plan(const AttnArg &a, F &&f)
     return blocks == 1 ? f(KeyPlan<NM_DT_BF16, 1, false>{}) : blocks == 2 ? f(KeyPlan<NM_DT_BF16, 2, false>{}) : blocks == 3 ? f(KeyPlan<NM_DT_BF16, 3, false>{}) : f(KeyPlan<NM_DT_BF16, 4, false>{});
 }
 
-template <typename P> hipError_t launch_grads(const AttnArg &a, P, hipStream_t st)
+template <typename P> hipError_t launch_grads(AttnArg a, P, hipStream_t st)
 {
     constexpr int DT = P::dt, BLOCKS = P::blocks, KEYS = DT == NM_DT_F32 ? 32 : 64;
     typedef typename P::W W;
@@ -336,6 +338,7 @@ template <typename P> hipError_t launch_grads(const AttnArg &a, P, hipStream_t s
     const int64_t wq = heads * row_tiles, wk = heads * kt * a.splits, ws = (heads * a.Tk * a.D / 4 + 255) / 256;
     if (std::max(wq, wk) > 0x7fffffff || !grid_holds(std::max(wq, wk), 64 * W::waves) || !grid_holds(wq, 512) || !grid_holds(ws, 256)) return hipErrorInvalidConfiguration;
     if (wq > 0) {
+        a.mix = mix_of(a, heads, row_tiles);
         if constexpr (DT == NM_DT_BF16 || BLOCKS <= 2) {
             if (two_parts(a, wq)) attention_dq_kernel<DT, BLOCKS, 64, 2><<<dim3((unsigned)wq), dim3(512), 0, st>>>(a, (int)row_tiles);
             else attention_dq_kernel<DT, BLOCKS, KEYS, 1><<<dim3((unsigned)wq), dim3(256), 0, st>>>(a, (int)row_tiles);
@@ -343,6 +346,7 @@ template <typename P> hipError_t launch_grads(const AttnArg &a, P, hipStream_t s
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || wk == 0) return e;
+    a.mix = a.splits == 1 ? mix_of(a, heads, kt) : 1;
     attention_dkdv_kernel<DT, BLOCKS, KEY_ROWS, W::waves, W::per_simd, W::v_in_lds, W::buffers><<<dim3((unsigned)wk), dim3(64 * W::waves), 0, st>>>(a, (int)kt);
     e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

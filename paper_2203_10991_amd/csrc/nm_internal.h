@@ -262,6 +262,7 @@ struct AttnArg {
     uint32_t group_mul;
     int group_shift;
     float scale;
+    int mix;                                  // heads whose tiles stand in the list together
     int splits;                               // of the keys (forward) or of the rows (gradients of k and v)
     int chunk;                                // gradients: tiles of rows to a part
     float *part;                              // their partial results

@@ -216,6 +216,14 @@ def test_many_workgroups(B, T, H, K, D, dtype):
     _compare(*inputs(B, T, T, H, K, D, dtype, seed=13), True, D ** -0.5, lens, lens)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,T,H,K,D", [(3, 300, 48, 6, 16), (4, 1100, 15, 15, 72), (3, 130, 576, 9, 8)])
+def test_tiles_of_many_heads_together(B, T, H, K, D, dtype):
+    """all heads' tiles in one list, of rows and of keys, and eight heads' at a time with three heads left over"""
+    lens = [T - (T * b) // (2 * B) for b in range(B)]
+    _compare(*inputs(B, T, T, H, K, D, dtype, seed=14), True, D ** -0.5, lens, lens)
+
+
 def test_another_stream_and_two_graphs():
     """two captured calls with workspaces of their own, replayed in turn with eager calls between"""
     import paper_2203_10991_amd as nm
