@@ -144,6 +144,17 @@ template <int DT> __device__ __forceinline__ Frag<DT> as_fragment(const f32x16 &
     return f;
 }
 
+// eight values less what that rounding made of them
+template <int DT> __device__ __forceinline__ void take_rounded(f32x16 &d, int first, const Frag<DT> &f)
+{
+    const u32x4 w = __builtin_bit_cast(u32x4, f.v[0]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        d[first + 2 * j] -= __builtin_bit_cast(float, w[j] << 16);
+        d[first + 2 * j + 1] -= __builtin_bit_cast(float, w[j] & 0xffff0000u);
+    }
+}
+
 __device__ __forceinline__ int row_of(int i, int hi) { return 8 * (i >> 2) + 4 * hi + (i & 3); }        // of a D block
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }

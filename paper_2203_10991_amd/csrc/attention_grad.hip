@@ -1,7 +1,7 @@
 // Attention, gradients.  With P = 2^(c S - lse) recomputed from q, k and the forward pass's lse, delta = sum over the head of g o, dP = g v^T:
 //     dS = P (dP - delta)      dq = scale dS k      dk = scale dS^T q      dv = P^T g
 // Where a row looks at few keys, dP and delta nearly cancel, and a bf16 o makes delta too coarse; `rest` holds what its rounding took.  16 heads of 512 tokens, scores of a deviation
-// of 0.4 to 2.7: 2-norm of dq's and dk's errors 0.27 and 0.29 % without it, 0.24 % with it and with an exact delta alike (0.17 % is the rounding of the results).
+// of 0.4 to 2.7: 2-norm of dq's and dk's errors 0.27 and 0.29 % without it, 0.24 % with it and with an exact delta alike, before LARGE below (0.17 % is the rounding of the results).
 // Two kernels, each with its results in registers from beginning to end, so that no sum crosses workgroups and the same call gives the same bits:
 //   dq      a wave keeps 32 rows (attention.h) of q and g as columns: S^T = K Q^T, dP^T = V G^T, dQ^T += K^T dS^T over tiles of keys; delta comes from its own rows first
 //   dk dv   a wave keeps 32 keys as columns: S = Q K^T, dP = G V^T, dV^T += G^T P, dK^T += Q^T dS over tiles of the rows of all heads that share the keys
@@ -18,6 +18,12 @@
 namespace nm {
 
 namespace attn {
+
+// In bf16 dS is rounded for the products with k and q.  Where a probability is large, few keys make up a row's sums, rounding does not average out, and dS nearly cancels: blocks that hold one
+// above 1/8 (LARGE, as a power of two) take what rounding took from their dS in a further product, one of seven.  3 heads of 32, 3332 tokens, scores of a deviation of 6: 2-norm of dq's and dk's
+// errors 0.272 and 0.249 % without, 0.20 and 0.19 with; scores of a deviation of 2 over 2898 keys 0.25 and 0.243.  It costs 71 + 76 -> 74 + 81 us at 32 x 512 tokens, 16 heads of 64 (a fifth of the blocks),
+// 3.40 + 4.45 -> 3.48 + 4.65 ms at 2 x 8192, 64 heads of 128 over 8 (one in 500); from 1/16 on 78 + 84 us, and 0.236 %.  The column fragments are read again there: held, they spill.
+constexpr float LARGE = -3.0f;
 
 // PARTS: two waves to a block of rows, each with one half of a tile's keys, whose sums are added up at the end
 template <int DT, int BLOCKS, int KEYS, int PARTS>
@@ -80,13 +86,18 @@ __global__ __launch_bounds__(256 * PARTS, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2)
 #pragma unroll
             for (int a = 0; a < SB; ++a) {
                 f32x16 x = f32x16{}, dp = f32x16{};
+                float top = -INFINITY;
 #pragma unroll
                 for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
                     mma(x, F::rows(kt, 32 * a, kk), q[kk]);
                     mma(dp, F::rows(vt, 32 * a, kk), g[kk]);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = exp2_of(__builtin_fmaf(x[i], c, -lse)) * (dp[i] - delta);
+                for (int i = 0; i < 16; ++i) {
+                    const float e = __builtin_fmaf(x[i], c, -lse);
+                    top = fmaxf(top, e);
+                    x[i] = exp2_of(e) * (dp[i] - delta);
+                }
                 if (edge) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
@@ -97,6 +108,17 @@ __global__ __launch_bounds__(256 * PARTS, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : 2)
                     const Frag<DT> w = as_fragment<DT>(x, 8 * h);
 #pragma unroll
                     for (int b = 0; b < BLOCKS; ++b) mma(dq[b], F::columns(kc, 32 * a + 16 * h, b), w);
+                }
+                if (DT == NM_DT_BF16 && __any(top > LARGE)) {
+                    uint32_t again = kc;                                 // (read again, not held)
+                    asm volatile("" : "+v"(again));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        take_rounded<DT>(x, 8 * h, as_fragment<DT>(x, 8 * h));
+                        const Frag<DT> w = as_fragment<DT>(x, 8 * h);
+#pragma unroll
+                        for (int b = 0; b < BLOCKS; ++b) mma(dq[b], F::columns(again, 32 * a + 16 * h, b), w);
+                    }
                 }
             }
         }
@@ -221,6 +243,7 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
 #pragma unroll
             for (int a = 0; a < SB; ++a) {
                 f32x16 x = f32x16{}, dp = f32x16{};
+                float top = -INFINITY;
 #pragma unroll
                 for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
                     mma(x, F::rows(rows, 32 * a, kk), k[kk]);
@@ -232,7 +255,9 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
                     const f32x4 l = *(const f32x4 *)&lse_of[buf][32 * a + row_of(i, hi)], d = *(const f32x4 *)&delta_of[buf][32 * a + row_of(i, hi)];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        x[i + j] = exp2_of(__builtin_fmaf(x[i + j], c, -l[j]));
+                        const float e = __builtin_fmaf(x[i + j], c, -l[j]);
+                        top = fmaxf(top, e);
+                        x[i + j] = exp2_of(e);
                         dp[i + j] = x[i + j] * (dp[i + j] - d[j]);
                     }
                 }
@@ -248,6 +273,17 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
                     for (int b = 0; b < BLOCKS; ++b) {
                         mma(dv[b], F::columns(columns + G, 32 * a + 16 * h, b), w);
                         mma(dk[b], F::columns(columns, 32 * a + 16 * h, b), ds);
+                    }
+                }
+                if (DT == NM_DT_BF16 && __any(top > LARGE)) {
+                    uint32_t again = columns;                            // (read again, not held)
+                    asm volatile("" : "+v"(again));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        take_rounded<DT>(dp, 8 * h, as_fragment<DT>(dp, 8 * h));
+                        const Frag<DT> w = as_fragment<DT>(dp, 8 * h);
+#pragma unroll
+                        for (int b = 0; b < BLOCKS; ++b) mma(dk[b], F::columns(again, 32 * a + 16 * h, b), w);
                     }
                 }
             }

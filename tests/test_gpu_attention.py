@@ -87,6 +87,17 @@ def test_scores_far_apart(dtype):
         _compare(q, k, v, g, True, 1.0)
 
 
+@pytest.mark.parametrize("T,K,D,spread", [(900, 2, 32, 5.0), (300, 2, 128, 4.0)])
+def test_rows_that_look_at_few_keys(T, K, D, spread):
+    """bf16: 2-norms of dq's and dk's errors.  The result's rounding is 0.166 % (half a step, 2^-9 to 2^-8 of a value, over sqrt(3), over a binade); what rounding P for o adds, and dS where P
+    is small, is allowed as much again, sqrt(2) times that; dS rounded everywhere would be as much a third time"""
+    q, k, v, g = inputs(2, T, T, 4, K, D, BF16, seed=15, spread=spread)
+    got, want = _all(q, k, v, g, True, D ** -0.5), reference(q, k, v, g, True, D ** -0.5)
+    for name in ("dq", "dk"):
+        w = want[name][0]
+        assert float((got[name].double().cpu() - w).norm() / w.norm()) < 0.0024, name
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_gradients_against_differences(dtype):
     """the sum of g o along a direction, by central differences in binary64 around the rounded inputs"""
