@@ -207,18 +207,23 @@ template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(c
     if (p.lse && e == 0) p.lse[at] = (base + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
-// how many rows a workgroup takes, and in how many parts the keys go
-struct Plan { int waves, keys, splits, parts; int64_t row_tiles; };
+// How many rows a workgroup takes, and in how many parts the keys go.
+// A block of rows (single tokens): a workgroup of one wave with small tiles, or, where keys are many, of four, three of which only load and store: 16 x 1 token over 8192 keys, 64 heads of 128 over 8,
+// 110 us with one and 106 with four, 1 x 1 over 32768, 32 heads over 8, 54 and 35, in binary32 8 x 1 over 8192 363 and 229; but 1 x 1 over 1000 keys 10.8 and 13.9 (binary32 20 and 34), 8 x 1 over 2000,
+// 32 heads of 64, 28.6 and 31.6, over 3000 to 4000 as much either way.
+// Parts: until there are workgroups for every CU, of keys enough to be worth their place in the join.  Unsplit: 353, 198 and 46 us where it is 106, 35 and 11.  Parts of at least 64 and 256 keys: 1 x 1 over 1000 10.8 us
+// (128: 12.5, 256: 18.6), 2 x 100 over 3000, 8 heads of 128, 21 (512: 24, 1024: 34); 32 parts at most, since one thread joins all parts of its elements (2 x 4 over 4000, 32 heads over 4: 16.8, with 63 parts 23).
+struct Plan { int waves, splits, parts; int64_t row_tiles; };
 inline Plan plan_of(const AttnArg &a)
 {
     Plan p;
     const int64_t total = (int64_t)a.Tq * a.group, heads = (int64_t)a.B * a.Hk;
-    p.waves = total <= 32 ? 1 : 4;
-    p.keys = p.waves == 1 ? 32 : a.dt == NM_DT_F32 ? 32 : 64;
+    const bool one = total <= 32;
+    p.waves = one && a.Tk < 4000 ? 1 : 4;
     p.row_tiles = (total + 32 * p.waves - 1) / (32 * p.waves);
-    const int64_t wgs = heads * p.row_tiles, want = (p.waves == 1 ? 8 : 2) * NM_CUS;
-    const int64_t least = p.waves == 1 ? 128 : 512;                     // keys to a part
-    p.splits = wgs >= want / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, (a.Tk + least - 1) / least, 64}));
+    const int64_t wgs = heads * p.row_tiles, want = (p.waves == 1 ? 8 : one ? 4 : 2) * NM_CUS;
+    const int64_t least = p.waves == 1 ? 64 : 256;                      // keys to a part
+    p.splits = wgs >= want / 2 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({want / wgs, (a.Tk + least - 1) / least, 32}));
     // two waves to a block of rows where a CU has one workgroup at most, in binary32 (full attention, one wave and two, in us: 8 x 197 tokens of 12 heads of 64 17.6 and 15.4,
     // 2 x 1000 of 4 heads on one 37.7 and 29.9; with two workgroups to a CU, 2 x 1333 of 12 on one of 48, 74 and 77).  In bf16, where a tile is a third of the work, there is nothing
     // in it (8 x 197: 9.5 and 9.5, 6 x 256 of 16 of 128: 14.5 and 15.3)
