@@ -2,7 +2,8 @@
 // neighbours (interleaved) or lie half of `part` apart.  The gradient is the same with the angle negated (sign).
 //
 // The angle is formed in binary64 turns and brought into half a turn before it is rounded: at position 10^6 a binary32 angle would be off by 0.06.  Cosines and sines are
-// made once for a token, in LDS, and serve all its heads; a thread then turns 8 pairs (two vectors of 8 elements), or 4 interleaved ones, at a time, fewer at the end of the part.  Bound: HBM.
+// made once for a token, in LDS, and serve all its heads; a thread then turns 8 pairs (two vectors of 8 elements), or 4 interleaved ones, at a time, fewer at the end of the part.  Bound: HBM: 32768
+// tokens of 72 heads of 128 in bf16 219 us, 5.5 TB/s; a flat list of vectors with four heads' to a thread 246.  Few tokens: a launch, 2.9 us for 8.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
