@@ -350,12 +350,14 @@ template <int DT, int BLOCKS, bool WIDE> struct KeyPlan {
     static constexpr int dt = DT, blocks = BLOCKS;
     // How many parts the rows go in where keys are few, and how long one is: rows divided evenly where every key is seen, so that a key's part is as long whether many
     // rows see it or few (parts that nothing is left for end at once).  Twice as many workgroups as have room, since they are all as long: 6 x up to 1333 tokens, 12 heads of
-    // 80 over 1, causal: 125 us with as many as have room, 80 with twice, 79 with three and four times.
+    // 80 over 1, causal: 125 us with as many as have room, 80 with twice, 79 with three and four times.  A part has eight tiles at least, or three where
+    // that still leaves half of the room: all gradients, 1 x 375 tokens of 2 heads of 40 29 us and 22, 3 x 247 of 4 over 1 of 56 31 and 23, 2 x 1150 of one of 40 in binary32 96 and 88; with the room full, 10 x 221 of 42
+    // over 21 of 88 75 and 100.
     static void plan(AttnArg &a)
     {
         const int64_t keys = 32 * W::waves, wgs = (int64_t)a.B * a.Hk * ((a.Tk + keys - 1) / keys), tiles = ((int64_t)a.Tq * a.group + KEY_ROWS - 1) / KEY_ROWS;
         const int64_t room = (int64_t)NM_CUS * W::per_simd * 4 / W::waves;
-        a.splits = wgs >= room || wgs == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({room * (a.causal ? 4 : 2) / wgs, tiles / 8, 32}));
+        a.splits = wgs >= room || wgs == 0 ? 1 : (int)std::max<int64_t>({1, std::min<int64_t>({room * (a.causal ? 4 : 2) / wgs, tiles / 8, 32}), std::min<int64_t>({room / 2 / wgs, tiles / 3, 32})});
         a.chunk = (int)std::max<int64_t>(1, (tiles + a.splits - 1) / a.splits);
     }
 };
