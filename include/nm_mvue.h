@@ -494,7 +494,7 @@ int nm_rotary(const nm_heads *x, const nm_heads *y, int dtype, int64_t B, int64_
  * holds, and o, dq, dk and dv are zeros there.  (Lengths beyond the tensors count as the tensors'.)  causal: query i of n sees the keys j <= i + m - n of m, so that the last query
  * sees the last key.  A query that sees no key: o = 0, lse = -infinity, and it adds nothing to any gradient.  What a query does not see of its own sequence has to be finite.
  * lse: binary32 [B][Hq][Tq], the logarithm of the sum of the exponentials; NULL: not wanted; the gradients need it, and o as the forward pass left it.
- * rest: bf16 [B][Tq][Hq][D], contiguous, on a 4-byte boundary: what rounding took from a bf16 o.  With it the gradients of queries that look at few keys are as exact as others';
+ * rest: words of 4 bytes [D / 2][B][Hq][Tq]: what rounding took from a bf16 o, as bf16, elements 2 w and 2 w + 1 in word w.  With it the gradients of queries that look at few keys are as exact as others';
  * NULL: not wanted, or not at hand.  Binary32 tensors have none.
  * scale > 0.  Scores, probabilities and all sums are binary32; with bf16 tensors probabilities (not those of the sum) and their gradients are rounded to bf16 for the
  * products that follow.  The gradients recompute the probabilities; no sum's order depends on anything but the sizes.

@@ -1099,7 +1099,8 @@ def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool
     query the last key, so that one query over a cache of keys sees all of them.  q_lens, k_lens (int32 or int64 [batch], on the GPU): the tokens of each sequence, from
     the front; what lies behind counts for nothing, and the result is zero there, as for a query that sees no key.
     want_lse: (o, lse).  lse[0] is float32 [batch x heads x queries], the logarithm of the sum of exponentials; for bfloat16 lse has D / 2 planes more, whose bits are
-    what rounding took from o (bfloat16 [batch x queries x heads x D]).  nm_attention_grad reads all of it."""
+    what rounding took from o: element [1 + w, b, h, i] as two bfloat16, those of o[b, i, h, 2 w] and o[b, i, h, 2 w + 1].  nm_attention_grad reads all of it; cut along sequences,
+    heads or queries, as the other tensors are, it stays what it is."""
     lib = load()
     scale = _scale_of(scale, q)
     r = _native_result(_native.attention(q, k, v, causal, scale, q_lens, k_lens, want_lse))

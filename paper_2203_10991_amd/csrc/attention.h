@@ -240,26 +240,53 @@ template <int DT, int BLOCKS> __device__ __forceinline__ void load_fragments(Fra
         }
     }
 }
-// the product of row x with y + rest (null: none), element by element, added up over this lane's elements
-template <int DT, int BLOCKS> __device__ __forceinline__ float row_product(const char *x, const char *y, const char *rest, int D, int lane)
+// What rounding took from a bf16 o: word w of a row holds elements 2 w and 2 w + 1, and stands with word w of all rows, which lie as in lse.  (A cut of lse and of these planes
+// beside each other is then what the cut tensors' call would leave.  32 rows of one head write, or read, 128 bytes in a run, those of a group shorter ones: 6 x up to 1333 tokens, 12 heads of 80 over
+// 1, forward 40.5 us with a row's words in a run and 43.4 so, dq 53.5 and 55.2; 32 x 512, 16 heads of 64, 50 and 50, 73 and 65.)  at: the row's first word, null: none
+struct Rest { uint32_t *at; int64_t apart; };
+__device__ __forceinline__ Rest rest_at(const AttnArg &p, int64_t row) { return Rest{p.rest ? (uint32_t *)p.rest + row : nullptr, (int64_t)p.B * p.Hq * p.Tq}; }
+
+// The product of a row x with y + rest, element by element, added up over this lane's elements.  f: x's fragments, zeros behind D (and where the row is not there; what y holds
+// then does not count).  bf16: all loads first, none behind a choice: a row's words lie in as many places as it has pairs, and waiting for some of them before the next are on
+// their way took dq of 32 x 512 tokens, 16 heads of 64, from 73 to 84 us
+template <int DT, int BLOCKS> __device__ __forceinline__ float row_product(const Frag<DT> (&f)[2 * BLOCKS], const char *x, const char *y, const Rest &rest, int D, int lane)
 {
     const int hi = lane >> 5;
     float sum = 0.0f;
+    if constexpr (DT == NM_DT_BF16) {
+        u32x4 o[2 * BLOCKS], d[2 * BLOCKS];
 #pragma unroll
-    for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
-        const int e = 16 * kk + 8 * hi;
-        if (e >= D) continue;
-        if constexpr (DT == NM_DT_BF16) {
-            const bf16x8 a = *(const bf16x8 *)(x + e * 2), b = *(const bf16x8 *)(y + e * 2);
+        for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+            const int e = 16 * kk + 8 * hi;
+            o[kk] = *(const u32x4 *)(y + (e < D ? e : 0) * 2);
+        }
+        if (rest.at) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)a[j], (float)b[j], sum);
-            if (rest) {
-                typedef bf16x8 any __attribute__((aligned(4)));
-                const bf16x8 d = *(const any *)(rest + e * 2);
+            for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+                const int e = 16 * kk + 8 * hi;
+                const uint32_t *from = rest.at + (e < D ? e / 2 : 0) * rest.apart;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)a[j], (float)d[j], sum);
+                for (int j = 0; j < 4; ++j) d[kk][j] = from[j * rest.apart];
             }
         } else {
+#pragma unroll
+            for (int kk = 0; kk < 2 * BLOCKS; ++kk) d[kk] = u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+            const bf16x8 a = f[kk].v[0], b = __builtin_bit_cast(bf16x8, o[kk]), c = __builtin_bit_cast(bf16x8, d[kk]);
+            if (16 * kk + 8 * hi < D) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)a[j], (float)b[j], sum);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)a[j], (float)c[j], sum);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int kk = 0; kk < 2 * BLOCKS; ++kk) {
+            const int e = 16 * kk + 8 * hi;
+            if (e >= D) continue;
 #pragma unroll
             for (int h = 0; h < 8; h += 4) {
                 const f32x4 a = *(const f32x4 *)(x + (e + h) * 4), b = *(const f32x4 *)(y + (e + h) * 4);
@@ -309,18 +336,16 @@ template <int DT, int BLOCKS, int ROWS, int THREADS> struct Stage {
     }
 };
 
-__device__ __forceinline__ const char *rest_at(const AttnArg &p, int b, int t, int h) { return p.rest ? (const char *)p.rest + (((int64_t)b * p.Tq + t) * p.Hq + h) * p.D * 2 : nullptr; }
-
-// four elements of a row, and (bf16, rest not null) what rounding took from them
-template <int DT> __device__ __forceinline__ void store_four(char *to, char *rest, int e, const f32x4 &x)
+// four elements of a row, and (bf16) what rounding took from them
+template <int DT> __device__ __forceinline__ void store_four(char *to, const Rest &rest, int e, const f32x4 &x)
 {
     if constexpr (DT == NM_DT_BF16) {
         const u32x2 w = {pack_bf16_rne(x[0], x[1]), pack_bf16_rne(x[2], x[3])};
         *(u32x2 *)(to + e * 2) = w;
-        if (rest) {
-            typedef u32x2 any __attribute__((aligned(4)));
-            *(any *)(rest + e * 2) = u32x2{pack_bf16_rne(x[0] - __uint_as_float(w[0] << 16), x[1] - __uint_as_float(w[0] & 0xffff0000u)),
-                                           pack_bf16_rne(x[2] - __uint_as_float(w[1] << 16), x[3] - __uint_as_float(w[1] & 0xffff0000u))};
+        if (rest.at) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                rest.at[(e / 2 + j) * rest.apart] = pack_bf16_rne(x[2 * j] - __uint_as_float(w[j] << 16), x[2 * j + 1] - __uint_as_float(w[j] & 0xffff0000u));
         }
     } else *(f32x4 *)(to + e * 4) = x;
 }
@@ -333,7 +358,7 @@ __device__ __forceinline__ void join_halves(uint32_t &first, uint32_t &second)
 }
 // a column of D blocks (an output row of D elements) times `by`, to memory.  A lane holds 4 of every 8 elements of its row and lane + 32 the others; in bf16 they exchange
 // every other 4, so that each writes 16 bytes.
-template <int DT, int BLOCKS> __device__ __forceinline__ void store_column(char *to, const f32x16 (&d)[BLOCKS], float by, int D, int lane, char *rest = nullptr)
+template <int DT, int BLOCKS> __device__ __forceinline__ void store_column(char *to, const f32x16 (&d)[BLOCKS], float by, int D, int lane, const Rest &rest = Rest{nullptr, 0})
 {
     const int hi = lane >> 5;
 #pragma unroll
@@ -354,11 +379,10 @@ template <int DT, int BLOCKS> __device__ __forceinline__ void store_column(char 
                 join_halves(w[0], w[2]);
                 join_halves(w[1], w[3]);
                 if (e < D) *(u32x4 *)(to + e * 2) = u32x4{w[0], w[1], w[2], w[3]};
-                if (rest) {
-                    typedef u32x4 any __attribute__((aligned(4)));
-                    join_halves(r[0], r[2]);
-                    join_halves(r[1], r[3]);
-                    if (e < D) *(any *)(rest + e * 2) = u32x4{r[0], r[1], r[2], r[3]};
+                if (rest.at) {                                           // (as they lie: 4 elements from the first eight, 4 from the second)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (32 * b + 2 * i + 4 * (j & 2) < D) rest.at[(16 * b + i + 4 * (j >> 1) + 2 * hi + (j & 1)) * rest.apart] = r[j];
                 }
             }
         } else {

@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * WAVES * PARTS, DT == NM_DT_F32 && BLOCKS + (WA
     }
     const int64_t at = ((int64_t)s.b * p.Hq + head) * p.Tq + query;
     if (p.splits == 1) {
-        store_column<DT, BLOCKS>((char *)row_at(p.o, p.so, s.b, query, head, ES), o, rounded != 0.0f ? 1.0f / rounded : 0.0f, p.D, lane, (char *)rest_at(p, s.b, query, head));
+        store_column<DT, BLOCKS>((char *)row_at(p.o, p.so, s.b, query, head, ES), o, rounded != 0.0f ? 1.0f / rounded : 0.0f, p.D, lane, rest_at(p, at));
         if (p.lse && hi == 0) p.lse[at] = (m + __builtin_amdgcn_logf(sum)) * LN2;             // (log2; -infinity of a sum of zero)
     } else {
         // O, m and the sums of this part of the keys
@@ -205,7 +205,7 @@ template <int DT> __global__ __launch_bounds__(256) void attention_join_kernel(c
     }
     const float by = rounded != 0.0f ? 1.0f / rounded : 0.0f;
     char *to = (char *)row_at(p.o, p.so, b, query, head, DT == NM_DT_BF16 ? 2 : 4);
-    store_four<DT>(to, (char *)rest_at(p, b, query, head), e, f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by});
+    store_four<DT>(to, rest_at(p, at), e, f32x4{o[0] * by, o[1] * by, o[2] * by, o[3] * by});
     if (p.lse && e == 0) p.lse[at] = (base + __builtin_amdgcn_logf(sum)) * LN2;
 }
 

@@ -255,7 +255,7 @@ struct AttnArg {
     AttnStride sq, sk, sv, so;
     void *o;
     float *lse;                               // [B][Hq][Tq], may be null in the forward pass
-    void *rest;                               // bf16 [B][Tq][Hq][D], what rounding took from a bf16 o; may be null
+    void *rest;                               // words [D / 2][B][Hq][Tq], what rounding took from a bf16 o, two elements each; may be null
     const int *q_lens, *k_lens;               // may be null
     int B, Tq, Tk, Hq, Hk, D, dt, causal;
     int group;                                // Hq / Hk, and r / group as r * group_mul >> group_shift
