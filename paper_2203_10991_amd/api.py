@@ -993,7 +993,13 @@ def rotary_freqs(width: int, base: float = 10000.0, scaling: Optional[str] = Non
         raise ValueError("width is an even number from 2 on, base and factor are positive")
     if scaling == "base" and width > 2:
         base = base * factor ** (width / (width - 2))
-    f = base ** (-torch.arange(0, width, 2, dtype=torch.float64) / width)
+    with torch.inference_mode(False):                                       # (constants that a later training step may save as well)
+        f = _rotary_freqs_on_host(width, base, scaling, factor, original_length, slow, fast)
+        return f.to(torch.get_default_device() if device is None else device)
+
+
+def _rotary_freqs_on_host(width, base, scaling, factor, original_length, slow, fast) -> torch.Tensor:
+    f = base ** (-torch.arange(0, width, 2, dtype=torch.float64, device="cpu") / width)
     if scaling == "linear":
         f = f / factor
     elif scaling == "parts":
@@ -1004,7 +1010,7 @@ def rotary_freqs(width: int, base: float = 10000.0, scaling: Optional[str] = Non
         f = f * keep + f / factor * (1 - keep)
     elif scaling not in (None, "base"):
         raise ValueError(f'scaling is None, "linear", "base" or "parts", got {scaling!r}')
-    return f.to(device) if device is not None else f
+    return f
 
 
 def _heads(t: torch.Tensor) -> _Heads:

@@ -491,15 +491,27 @@ class NMSelfAttention(torch.nn.Module):
             raise ValueError(f"an even number of a head's {self.head} elements is turned, got {rotary}")
         kw = dict(bias=bias, cfg=cfg, device=device, dtype=dtype)
         self.qkv, self.proj = NMLinear(width, (heads + 2 * kv_heads) * self.head, **kw), NMLinear(width, width, **kw)
-        # (a plain attribute: a module's .to(dtype) would round a buffer's binary64)
-        self._freqs = api.rotary_freqs(rotary, **(rotary_options or {})) if rotary else None
+        # (a plain attribute: a module's .to(dtype) would round a buffer's binary64, and a module built on the meta device would lose its values)
+        self._freqs = api.rotary_freqs(rotary, **{**(rotary_options or {}), "device": "cpu"}) if rotary else None
         self._freqs_on = {}
+        self._place()
+
+    def _place(self):
+        """The frequencies where the weights are, in front of any call: a copy from the host cannot be captured into a graph."""
+        if self.qkv.weight.is_cuda:
+            self._frequencies(self.qkv.weight.device)
+
+    def _apply(self, fn, recurse=True):
+        super()._apply(fn, recurse)
+        self._place()
+        return self
 
     def _frequencies(self, device):
         if self._freqs is None:
             return None
         if device not in self._freqs_on:
-            self._freqs_on[device] = self._freqs.to(device)
+            with torch.inference_mode(False):                                # (a copy that a call under inference_mode made could not be saved for a gradient later)
+                self._freqs_on[device] = self._freqs.to(device)
         return self._freqs_on[device]
 
     def forward(self, x, positions: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None):

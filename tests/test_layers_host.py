@@ -56,3 +56,16 @@ def test_convolution_knows_the_dense_products():
     layer.cfg.dense = "i4"
     with pytest.raises(ValueError, match="dense"):
         layer(x)
+
+
+def test_self_attention_built_on_the_meta_device():
+    """frequencies are values, not a shape; rotary_freqs itself goes to the default device as torch's own factories do, and what a call under inference_mode makes can be saved for a gradient"""
+    import paper_2203_10991_amd as nm
+    from paper_2203_10991_amd.autograd import NMSelfAttention
+    with torch.device("meta"):
+        layer = NMSelfAttention(64, 4, rotary_options={"base": 500.0})
+        assert nm.rotary_freqs(16, device="cpu").device.type == "cpu" and nm.rotary_freqs(16).is_meta
+    layer = layer.to_empty(device="cpu")
+    assert layer.qkv.weight.device.type == "cpu" and torch.equal(layer._frequencies(torch.device("cpu")), nm.rotary_freqs(16, 500.0))
+    with torch.inference_mode():
+        assert not nm.rotary_freqs(16).is_inference() and not NMSelfAttention(64, 4)._freqs.is_inference()
