@@ -76,7 +76,7 @@ __device__ __forceinline__ void terms_of(float x, float y, uint32_t (&w)[3])
 }
 
 // Where a lane's fragments lie in LDS: the turns of rows and chunks are exclusive-ors, so the address of row r + r', chunk c + c' is the lane's own (r, c) with
-// (c' ^ turn(r')) << 4 turned in, plus r' rows, as long as no bits meet.  Two registers and an exclusive-or before a read then take the place of a register for every
+// (c' ^ turn(r')) << 4 turned in, plus r' rows, as long as no bits meet: tiles start at multiples of a row.  Two registers and an exclusive-or before a read then take the place of a register for every
 // read, which the kernels do not have: held in registers, addresses of 128-element heads made 27 to 45 spills in the dk dv kernel, whose reloads wait for the tiles on
 // their way (2 x 8192 tokens, 64 heads over 8: 8.1 to 12.8 ms).
 typedef __attribute__((address_space(3))) char lds_char;
@@ -87,6 +87,9 @@ template <typename T> __device__ __forceinline__ T lds_read(uint32_t at) { retur
 template <int DT, int BLOCKS, int ROWS> struct Lane {
     typedef Tile<BLOCKS> L;
     static constexpr uint32_t TERM = ROWS * L::ROW, BYTES = TERMS<DT> * TERM;      // from a term's tile to the next one's, and of all of them
+    // a tile starts with a row: `moved` turns bits of whole addresses, which are a row's own only then
+    static constexpr uint32_t ALIGN = L::ROW;
+    static_assert(TERM % ALIGN == 0 && BYTES % ALIGN == 0 && (ALIGN & (ALIGN - 1)) == 0 && ALIGN == 16 * L::CHUNKS, "tiles one behind the other start with a row each");
     uint32_t row, col;               // relative to a tile
     __device__ __forceinline__ Lane(int lane)
     {

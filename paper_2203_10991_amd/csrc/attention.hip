@@ -27,7 +27,7 @@ __global__ __launch_bounds__(64 * WAVES * PARTS, DT == NM_DT_F32 && BLOCKS + (WA
 {
     typedef Lane<DT, BLOCKS, KEYS> F;
     constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, THREADS = 64 * WAVES * PARTS, ROWS = 32 * WAVES, SB = KEYS / 32 / PARTS;
-    __shared__ __align__(16) char lds[2][2][F::BYTES];
+    __shared__ __align__(F::ALIGN) char lds[2][2][F::BYTES];
     const int lane = (int)threadIdx.x & 63, wave = ((int)threadIdx.x >> 6) % WAVES, part = ((int)threadIdx.x >> 6) / WAVES, hi = lane >> 5;
     // the tiles of a head side by side, those with most keys first
     const Place place(p, row_tiles, p.splits, DT == NM_DT_BF16 || BLOCKS < 3);

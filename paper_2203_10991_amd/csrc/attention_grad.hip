@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256 * PARTS, DT == NM_DT_F32 && BLOCKS > 2 ? 1 : DT
 {
     typedef Lane<DT, BLOCKS, KEYS> F;
     constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, ROWS = 128, SB = KEYS / 32 / PARTS;
-    __shared__ __align__(16) char lds[2][2][F::BYTES];
+    __shared__ __align__(F::ALIGN) char lds[2][2][F::BYTES];
     const int lane = (int)threadIdx.x & 63, wave = ((int)threadIdx.x >> 6) % 4, part = ((int)threadIdx.x >> 6) / 4, hi = lane >> 5;
     const Place place(p, row_tiles, 1, DT == NM_DT_BF16 || BLOCKS < 3);
     const uint32_t bh = place.bh;
@@ -173,9 +173,9 @@ __global__ __launch_bounds__(64 * WAVES, PER_SIMD) void attention_dkdv_kernel(co
     typedef Lane<DT, BLOCKS, 32 * WAVES> FV;
     constexpr int ES = DT == NM_DT_BF16 ? 2 : 4, KEYS = 32 * WAVES, SB = ROWS / 32, THREADS = 64 * WAVES;
     constexpr uint32_t G = F::BYTES;                                     // from q's tile to g's
-    __shared__ __align__(16) char lds[BUFFERS][2][F::BYTES];
-    __shared__ __align__(16) char v_lds[VL ? FV::BYTES : 16];
-    __shared__ float lse_of[BUFFERS][ROWS], delta_of[BUFFERS][ROWS];
+    __shared__ __align__(F::ALIGN) char lds[BUFFERS][2][F::BYTES];
+    __shared__ __align__(FV::ALIGN) char v_lds[VL ? FV::BYTES : 16];
+    __shared__ __align__(16) float lse_of[BUFFERS][ROWS], delta_of[BUFFERS][ROWS];          // (read four at a time)
     __shared__ int seen_of[BUFFERS][ROWS];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, hi = lane >> 5;
     const Place place(p, key_tiles, p.splits, PER_SIMD * 4 >= 2 * WAVES);
