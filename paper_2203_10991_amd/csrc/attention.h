@@ -28,9 +28,10 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// Binary32 operands go through the bf16 instructions as three terms, x = x1 + x2 + x3 of 8 bits each, cut off one after another, which is exact; a product takes the six
-// products of terms down to 2^-16 of the first (what is left out is below 2^-23 of a product, half of it in the mean).  The binary32 instructions have a sixteenth of the bf16 ones'
-// rate, six products an eighth of work to sixteen.  An infinity becomes NaN.
+// Binary32 operands go through the bf16 instructions as three terms, x = x1 + x2 + x3, the first two rounded to nearest, the third what is left, which is exact: |x2| <= 2^-8, |x3| <= 2^-17
+// of x's power of two.  A product takes the six products of terms down to 2^-16 of the first; x2 y3 + x3 y2 + x3 y3, which it leaves out, is 2^-24 of it at most, of either sign (cut off instead
+// of rounded, the terms have x's sign and up to two and four times the size: what is left out is then up to 2^-21, always of the product's sign, and adds up over a sum.  Rounding costs
+// nothing at 2 x 4096 tokens of 8 heads of 64, 1 to 2 % at 8 x 197 of 12, 3 to 4 % with heads of 32).  The binary32 instructions have a sixteenth of the bf16 ones' rate, six products an eighth of work to sixteen.  An infinity becomes NaN.
 template <int DT> constexpr int TERMS = DT == NM_DT_BF16 ? 1 : 3;
 
 // rows of D = 32 BLOCKS or fewer elements in LDS as bf16 (binary32: three tiles of terms), each in a power of two of 16-byte chunks; chunk c of row r lies at c ^ turn(r):
@@ -65,14 +66,15 @@ template <int DT> __device__ __forceinline__ void mma(f32x16 &d, const Frag<DT> 
 
 // the upper halves of two words in one
 __device__ __forceinline__ uint32_t upper(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
-// the terms of two values: word k holds term k of both
-__device__ __forceinline__ void terms_of(float x, float y, uint32_t (&w)[3])
+// the terms of two values: word k holds term k of both.  WHOLE: up to the largest binary32 numbers (what would round to an infinity becomes the largest bf16 number, with a second
+// term as large as a step of it), for the tensors' own values; without it from 2^128 - 2^119 on NaN, for probabilities and their gradients
+template <bool WHOLE> __device__ __forceinline__ void terms_of(float x, float y, uint32_t (&w)[3])
 {
-    const float x1 = __uint_as_float(__float_as_uint(x) & 0xffff0000u), y1 = __uint_as_float(__float_as_uint(y) & 0xffff0000u), rx = x - x1, ry = y - y1;
-    const float x2 = __uint_as_float(__float_as_uint(rx) & 0xffff0000u), y2 = __uint_as_float(__float_as_uint(ry) & 0xffff0000u);
-    w[0] = upper(x, y);
-    w[1] = upper(rx, ry);
-    w[2] = upper(rx - x2, ry - y2);
+    constexpr float MOST = 3.38953139e38f;
+    w[0] = WHOLE ? pack_bf16_rne(__builtin_amdgcn_fmed3f(x, -MOST, MOST), __builtin_amdgcn_fmed3f(y, -MOST, MOST)) : pack_bf16_rne(x, y);
+    const float rx = x - __uint_as_float(w[0] << 16), ry = y - __uint_as_float(w[0] & 0xffff0000u);
+    w[1] = pack_bf16_rne(rx, ry);
+    w[2] = upper(rx - __uint_as_float(w[1] << 16), ry - __uint_as_float(w[1] & 0xffff0000u));
 }
 
 // Where a lane's fragments lie in LDS: the turns of rows and chunks are exclusive-ors, so the address of row r + r', chunk c + c' is the lane's own (r, c) with
@@ -128,7 +130,7 @@ template <int DT, int BLOCKS, int ROWS> struct Lane {
 
 // eight values of a D block as a B fragment.  bf16: probabilities and their gradients are rounded to the operands' own type for the second product, to nearest; sums of
 // probabilities take them before that
-template <int DT> __device__ __forceinline__ Frag<DT> as_fragment(const f32x16 &d, int first)
+template <int DT, bool WHOLE = false> __device__ __forceinline__ Frag<DT> as_fragment(const f32x16 &d, int first)
 {
     u32x4 w[TERMS<DT>];
 #pragma unroll
@@ -136,7 +138,7 @@ template <int DT> __device__ __forceinline__ Frag<DT> as_fragment(const f32x16 &
         if constexpr (DT == NM_DT_BF16) w[0][j] = pack_bf16_rne(d[first + 2 * j], d[first + 2 * j + 1]);
         else {
             uint32_t t[3];
-            terms_of(d[first + 2 * j], d[first + 2 * j + 1], t);
+            terms_of<WHOLE>(d[first + 2 * j], d[first + 2 * j + 1], t);
 #pragma unroll
             for (int n = 0; n < 3; ++n) w[n][j] = t[n];
         }
@@ -239,7 +241,7 @@ template <int DT, int BLOCKS> __device__ __forceinline__ void load_fragments(Fra
             f32x16 x;
 #pragma unroll
             for (int j = 0; j < 4; ++j) { x[j] = a[j]; x[4 + j] = b[j]; }
-            f[kk] = as_fragment<DT>(x, 0);
+            f[kk] = as_fragment<DT, true>(x, 0);
         }
     }
 }
@@ -330,8 +332,8 @@ template <int DT, int BLOCKS, int ROWS, int THREADS> struct Stage {
             if constexpr (DT == NM_DT_BF16) *(u32x4 *)(tile + L::at(r, c)) = w;
             else {
                 uint32_t lo[3], hi[3];
-                terms_of(__uint_as_float(w[0]), __uint_as_float(w[1]), lo);
-                terms_of(__uint_as_float(w[2]), __uint_as_float(w[3]), hi);
+                terms_of<true>(__uint_as_float(w[0]), __uint_as_float(w[1]), lo);
+                terms_of<true>(__uint_as_float(w[2]), __uint_as_float(w[3]), hi);
 #pragma unroll
                 for (int k = 0; k < 3; ++k) *(u32x2 *)(tile + k * ROWS * L::ROW + L::at(r, c >> 1) + (c & 1) * 8) = u32x2{lo[k], hi[k]};
             }
