@@ -473,7 +473,8 @@ size_t nm_layer_norm_grad_workspace(int64_t R, int64_t C);
 
 /*
  * Heads [B][T][H][D] of a batch: a base and the strides, in elements, of a sequence, a token and a head; a head's elements lie side by side.  A stride does not count
- * where its size is 1.  Inputs may have strides of 0; outputs have no element twice.
+ * where its size is 1.  Inputs may have strides of 0; outputs have no element twice.  Outputs may lie between one another, or between what a call reads, as parts of one tensor with the
+ * same strides do; where strides differ, a tensor counts as all bytes from its first to its last.
  */
 typedef struct { void *data; int64_t batch, token, head; } nm_heads;
 

@@ -34,17 +34,39 @@ inline bool is_float(int dt) { return dt == NM_F32 || dt == NM_BF16; }
 inline int64_t esize(int dt) { return dt == NM_BF16 ? 2 : 4; }
 inline bool aligned(const void *p, int64_t to) { return (uintptr_t)p % (uintptr_t)to == 0; }
 
-// What a call reads or writes: bytes lo .. hi - 1, of which the parts [lo + k step, lo + k step + part) where step > 0
-struct Range { uintptr_t lo, hi; int64_t step, part; };
-inline Range range_of(const void *p, int64_t bytes) { return Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)(p && bytes > 0 ? bytes : 0), 0, 0}; }
+// What a call reads or writes: bytes lo .. hi - 1, and in them runs of `run` bytes that come again every step[0] bytes, all of those every step[1], and so on (steps rise; a
+// step that appears less often than would fit counts as if it went on)
+struct Range { uintptr_t lo, hi; int64_t run; int dims; int64_t step[3], span[4]; };      // span[i]: from the first to the last byte of what steps below i make
+inline Range range_of(const void *p, int64_t bytes) { const int64_t n = p && bytes > 0 ? bytes : 0; return Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)n, n, 0, {}, {n}}; }
+// n[i] times s[i] bytes apart
+inline Range range_of(const void *p, int64_t run, const int64_t (&n)[3], const int64_t (&s)[3])
+{
+    Range r = range_of(p, run);
+    int64_t count[3];
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] < 2 || s[i] == 0) continue;
+        int at = r.dims++;
+        for (; at > 0 && r.step[at - 1] > s[i]; --at) { r.step[at] = r.step[at - 1]; count[at] = count[at - 1]; }
+        r.step[at] = s[i];
+        count[at] = n[i];
+    }
+    for (int i = 0; i < r.dims; ++i) r.span[i + 1] = r.span[i] + (count[i] - 1) * r.step[i];
+    r.hi = r.lo + (uintptr_t)r.span[r.dims];
+    return r;
+}
+// do the lower n steps of a, from byte x on, and the lower m steps of b, from byte y on, meet?  Only where both come in the same outermost step, which holds what lies within it, is that looked
+// at more closely than from the first to the last byte: of a's repetitions at k step and b's at y - x + k step, one and its next can meet.
+inline bool meet(const Range &a, int n, int64_t x, const Range &b, int m, int64_t y)
+{
+    if (x + a.span[n] <= y || y + b.span[m] <= x) return false;
+    if (n == 0 || m == 0 || a.step[n - 1] != b.step[m - 1] || a.span[n - 1] > a.step[n - 1] || b.span[m - 1] > b.step[m - 1]) return true;
+    const int64_t step = a.step[n - 1], off = ((y - x) % step + step) % step;
+    return meet(a, n - 1, 0, b, m - 1, off) || meet(a, n - 1, step, b, m - 1, off);
+}
 inline bool overlap(const Range &a, const Range &b)
 {
     if (a.lo >= b.hi || b.lo >= a.hi || a.lo == a.hi || b.lo == b.hi) return false;
-    if (a.step <= 0 || a.step != b.step) return true;
-    // both come in parts the same step apart: side by side within a step?
-    const Range &l = a.lo < b.lo ? a : b, &u = a.lo < b.lo ? b : a;
-    const uintptr_t off = (u.lo - l.lo) % (uintptr_t)a.step;
-    return off < (uintptr_t)l.part || off + (uintptr_t)u.part > (uintptr_t)a.step;
+    return a.lo < b.lo ? meet(a, a.dims, 0, b, b.dims, (int64_t)(b.lo - a.lo)) : meet(a, a.dims, (int64_t)(a.lo - b.lo), b, b.dims, 0);
 }
 
 constexpr int64_t LIM = (int64_t)1 << 56, STRIDE_MOST = (int64_t)1 << 40, SIZE_MOST = 0x7fffffff;
@@ -60,7 +82,11 @@ int check_matrix(const char *fn, const char *what, const void *p, int64_t R, int
     if (!aligned(p, esize(dt))) return fail(NM_ERR_ALIGN, "%s: %s is not on its elements' boundary", fn, what);
     return NM_OK;
 }
-inline Range matrix_range(const void *p, int64_t R, int64_t C, int64_t ld, int dt) { return range_of(p, R > 0 && C > 0 ? ((R - 1) * ld + C) * esize(dt) : 0); }
+inline Range matrix_range(const void *p, int64_t R, int64_t C, int64_t ld, int dt)
+{
+    if (R < 1 || C < 1) return range_of(nullptr, 0);
+    return range_of(p, C * esize(dt), {R, 1, 1}, {R > 1 ? ld * esize(dt) : 0, 0, 0});
+}
 
 constexpr int64_t NORM_MOST = 32768;
 int check_norm(const char *fn, int64_t R, int64_t C, int x_dtype, int w_dtype)
@@ -100,12 +126,8 @@ int check_heads(const char *fn, const char *what, const nm_heads *p, int64_t B, 
 inline Range heads_range(const nm_heads *p, int64_t B, int64_t T, int64_t H, int64_t D, int dt)
 {
     if (B < 1 || T < 1 || H < 1 || D < 1) return range_of(nullptr, 0);
-    const int64_t part = ((H - 1) * (H > 1 ? p->head : 0) + D) * esize(dt);
-    Range r = range_of(p->data, (B - 1) * (B > 1 ? p->batch : 0) * esize(dt) + (T - 1) * (T > 1 ? p->token : 0) * esize(dt) + part);
-    // a token's heads in one run, tokens and sequences whole steps apart
-    const int64_t step = T > 1 ? p->token * esize(dt) : B > 1 ? p->batch * esize(dt) : 0;
-    if (step > 0 && part <= step && (B < 2 || p->batch * esize(dt) % step == 0)) { r.step = step; r.part = part; }
-    return r;
+    const int64_t e = esize(dt);
+    return range_of(p->data, D * e, {B, T, H}, {B > 1 ? p->batch * e : 0, T > 1 ? p->token * e : 0, H > 1 ? p->head * e : 0});
 }
 inline nm::AttnStride strides_of(const nm_heads *p, int64_t B, int64_t T, int64_t H) { return nm::AttnStride{B > 1 ? p->batch : 0, T > 1 ? p->token : 0, H > 1 ? p->head : 0}; }
 

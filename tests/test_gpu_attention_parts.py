@@ -53,3 +53,32 @@ def test_parts_joined():
         assert torch.equal(torch.cat(parts, dim).view(torch.int32), whole.view(torch.int32))
     parts = [nm.nm_attention(p, k, v, want_lse=True)[1] for p in (q[:, :128], q[:, 128:])]
     assert torch.equal(torch.cat(parts, 3).view(torch.int32), whole.view(torch.int32))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("order", [(0, 1, 2), (1, 0, 2), (0, 2, 1), (2, 0, 1), (1, 2, 0), (2, 1, 0)])
+def test_gradients_into_parts_of_one_tensor(order, dtype):
+    """dq, dk and dv as heads of one tensor whose sequences, tokens and heads lie in any order; what is between them stays as it was"""
+    import paper_2203_10991_amd as nm
+    B, T, H, K, D = 3, 70, 4, 2, 32
+    q, k, v, g = (t.to(DEV) for t in inputs(B, T, T, H, K, D, dtype, seed=23))
+    o, lse = nm.nm_attention(q, k, v, causal=True, want_lse=True)
+    want = nm.nm_attention_grad(g, q, k, v, o, lse, causal=True)
+    sizes, back = (B, T, H + 2 * K + 1), [order.index(i) for i in range(3)]
+    held = torch.full((*(sizes[i] for i in order), D), 7.0, dtype=dtype, device=DEV).permute(*back, 3)
+    assert held.shape == (*sizes, D)
+    out = held[:, :, :H], held[:, :, H + 1:H + 1 + K], held[:, :, H + 1 + K:]
+    nm.nm_attention_grad(g, q, k, v, o, lse, causal=True, out=out)
+    assert all(torch.equal(a, b) for a, b in zip(out, want)) and bool((held[:, :, H] == 7).all())
+    with pytest.raises(nm.NmError):
+        nm.nm_attention_grad(g, q, k, v, o, lse, causal=True, out=(out[0], out[1], held[:, :, H + K:-1]))
+
+
+def test_heads_turned_into_other_parts():
+    """rotary positions of one part of a sequence-first tensor into another"""
+    import paper_2203_10991_amd as nm
+    held = torch.randn(11, 3, 6, 32, device=DEV).transpose(0, 1)
+    freqs = nm.rotary_freqs(32, device=DEV)
+    kept = held.clone()
+    nm.nm_rotary(held[:, :, :3], freqs, out=held[:, :, 3:])
+    assert torch.equal(held[:, :, :3], kept[:, :, :3]) and torch.equal(held[:, :, 3:], nm.nm_rotary(kept[:, :, :3], freqs))
