@@ -214,3 +214,36 @@ def test_refusals():
                  lambda: nm.nm_layer_norm(torch.zeros(1, 0, device=DEV))):
         with pytest.raises(nm.NmError):
             call()
+
+
+@pytest.mark.parametrize("xt", [BF16, F32])
+@pytest.mark.parametrize("R,C", [(2700, 1030), (1400, 2500), (1300, 5000), (1283, 9000), (530, 16384), (1290, 16391), (260, 32768)])
+def test_workgroups_with_several_rows(R, C, xt):
+    """rows of several waves, more of them than the forward pass (1280) and the gradients (256 or 512) have workgroups: statistics exchanged row after row, the next row on its way, sums over rows"""
+    import paper_2203_10991_amd as nm
+    x, w, b, g = _inputs(R, C, xt, F32)
+    got = _compare(x, w, b, g)
+    # every row's result is what the row alone gives
+    xd = x.to(DEV)
+    for at in (0, R // 2, R - 1):
+        assert torch.equal(got[0][at:at + 1], nm.nm_layer_norm(xd[at:at + 1], w.to(DEV), b.to(DEV), EPS))
+
+
+@pytest.mark.parametrize("C", [1500, 4000, 9000, 20000])
+def test_rows_of_several_waves_again_and_again(C):
+    """the same bits from every call, for rows that differ by far from one to the next"""
+    import paper_2203_10991_amd as nm
+    gen = torch.Generator(device=DEV).manual_seed(C)
+    x = torch.randn(3000, C, generator=gen, device=DEV) * torch.exp2(torch.randint(-20, 20, (3000, 1), generator=gen, device=DEV).float()) + torch.randn(3000, 1, generator=gen, device=DEV) * 1000
+    w, g = torch.rand(C, generator=gen, device=DEV) + 0.5, torch.randn(3000, C, generator=gen, device=DEV)
+
+    def both():
+        y, mean, rstd = nm.nm_layer_norm(x, w, want_stats=True)
+        return y, mean, rstd, *nm.nm_layer_norm_grad(g, x, w, mean, rstd)
+    first = both()
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(first, both()))
+    # (rows in another order: results move with them)
+    order = torch.randperm(3000, generator=gen, device=DEV)
+    y, mean, rstd = nm.nm_layer_norm(x[order], w, want_stats=True)
+    assert torch.equal(y, first[0][order]) and torch.equal(mean, first[1][order]) and torch.equal(rstd, first[2][order])
