@@ -1,9 +1,10 @@
 // Rotary positions: pairs (a, b) of a head's first `part` elements become s (a cos - b sin, a sin + b cos), the angle being position times the pair's frequency; pairs are
 // neighbours (interleaved) or lie half of `part` apart.  The gradient is the same with the angle negated (sign).
 //
-// The angle is formed in binary64 turns and brought into half a turn before it is rounded: at position 10^6 a binary32 angle would be off by 0.06.  Cosines and sines are
-// made once for a token, in LDS, and serve all its heads; a thread then turns 8 pairs (two vectors of 8 elements), or 4 interleaved ones, at a time, fewer at the end of the part.  Bound: HBM: 32768
-// tokens of 72 heads of 128 in bf16 219 us, 5.5 TB/s; a flat list of vectors with four heads' to a thread 246.  Few tokens: a launch, 2.9 us for 8.
+// The angle is formed in binary64 turns and brought into half a turn, and what rounding it to binary32 takes goes into cosine and sine: at position 10^6 a binary32 angle would be off by
+// 0.06, a binary32 fraction of a turn by up to 1.6 half steps of one, more than the functions' own errors.  Cosines and sines are made once for a token, in LDS, and serve all its heads; a
+// thread then turns 8 pairs (two vectors of 8 elements), or 4 interleaved ones, at a time, fewer at the end of the part.  Bound: HBM: 32768 tokens of 72 heads of 128 in bf16 219 us,
+// 5.5 TB/s; a flat list of vectors with four heads' to a thread 246.  Few tokens: a launch, 2.9 us for 8.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -48,9 +49,14 @@ template <int DT, bool INTERLEAVED> __global__ __launch_bounds__(256) void rotar
         if (first + k >= n) break;
         const uint32_t at = (uint32_t)(first + k), kb = at / (uint32_t)p.T, kt = at - kb * (uint32_t)p.T;
         const int64_t pos = !p.positions ? (int64_t)kt : p.wide ? ((const int64_t *)p.positions)[kb * p.pos_b + kt] : ((const int32_t *)p.positions)[kb * p.pos_b + kt];
-        const double turn = (double)pos * (p.freqs[j] * 0.15915494309189533577);
+        // (the fraction of a turn as two binary32 numbers: the library's functions take the first, and what the second one turns, 2^-23 at most, is their first derivative's share)
+        const double turn = (double)pos * (p.freqs[j] * 0.15915494309189533577), part_of_turn = turn - rint(turn);
+        const float first_part = (float)part_of_turn, d = (float)(part_of_turn - (double)first_part) * 6.28318530717958647693f;
         float sn, cs;
-        sincospif(2.0f * (float)(turn - rint(turn)), &sn, &cs);
+        sincospif(2.0f * first_part, &sn, &cs);
+        const float sn1 = sn;
+        sn = __builtin_fmaf(cs, d, sn);
+        cs = __builtin_fmaf(-sn1, d, cs);
         turns[i] = make_float2(cs * p.scale, sn * p.scale * p.sign);
     }
     __syncthreads();

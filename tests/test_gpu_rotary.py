@@ -152,3 +152,23 @@ def test_refusals():
                  lambda: nm.nm_rotary(torch.zeros(1, 1, 1, 1026, device=DEV), freqs), lambda: nm.nm_rotary(x, freqs, out=wide[:, :, :1].expand(2, 5, 3, 16))):
         with pytest.raises(nm.NmError):
             call()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_cosines_and_sines_of_unrounded_angles(interleaved):
+    """Pairs (1, 0), which become the cosine and the sine themselves.  The 2-norm of their errors stays below that of exact functions of a fraction of a turn rounded to binary32, rounded once:
+    whatever rounds the fraction has that error, and its functions' own beside it"""
+    import paper_2203_10991_amd as nm
+    T, part = 4000, 64
+    freqs = nm.rotary_freqs(part, 300.0)
+    pos = torch.arange(T) * 261 + 7
+    x = torch.zeros(1, T, 1, part)
+    x[..., 0::2 if interleaved else 1][..., :part // 2] = 1.0
+    y = nm.nm_rotary(x.to(DEV), freqs.to(DEV), pos.to(DEV), interleaved).cpu().double()[0, :, 0]
+    got = torch.stack((y[:, 0::2], y[:, 1::2]) if interleaved else (y[:, :part // 2], y[:, part // 2:]))
+    angle = pos.double()[:, None] * freqs
+    want = torch.stack((angle.cos(), angle.sin()))
+    turn = angle / (2 * math.pi)
+    rounded = (turn - turn.round()).float().double() * 2 * math.pi
+    limit = (torch.stack((rounded.cos(), rounded.sin())).float().double() - want).norm()
+    assert float((got - want).norm()) < float(limit), float((got - want).norm() / limit)
