@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_plan.h"           // NM_CUS
 #include "nm_internal.h"
@@ -272,9 +273,10 @@ template <int WT> __global__ __launch_bounds__(1024) void layer_norm_sum_kernel(
 }
 
 template <int T, int N, bool LEAN = false> struct Shape { static constexpr int t = T, n = N, threads = T < NORM_T ? NORM_T : T, rows = threads / T; static constexpr bool lean = LEAN; };
-// Threads to a row and pieces to a thread: part of a wave up to 256 elements, a wave up to 1024.  200000 rows of 64 in bf16: 60 us with a wave to a row, 12 with 8 threads.  lean: the
-// gradients of binary32 rows of 8193 to 16384 elements (4096 x 16384: 251 us with 512 threads and 94 spills, 196 lean; in bf16 101 and 128).
-template <typename F> auto with_shape(int64_t C, bool lean, F &&f)
+// Threads to a row and pieces to a thread: part of a wave up to 256 elements, a wave up to 1024.  200000 rows of 64 in bf16: 60 us with a wave to a row, 12 with 8 threads.  LEAN: the
+// gradients of binary32 rows of 8193 to 16384 elements (4096 x 16384: 251 us with 512 threads and 94 spills, 196 lean; in bf16 101 and 128).  Gradients of wider rows spill 32 to 74 registers
+// of the 128 that 1024 threads have: 2048 x 32768 in bf16 169 us, 3.2 TB/s.
+template <bool LEAN, typename F> auto with_shape(int64_t C, F &&f)
 {
     if (C <= 64) return f(Shape<8, 1>{});
     if (C <= 128) return f(Shape<16, 1>{});
@@ -284,13 +286,13 @@ template <typename F> auto with_shape(int64_t C, bool lean, F &&f)
     if (C <= 2048) return f(Shape<256, 1>{});
     if (C <= 4096) return f(Shape<256, 2>{});
     if (C <= 8192) return f(Shape<256, 4>{});
-    if (C <= 16384) return lean ? f(Shape<1024, 2, true>{}) : f(Shape<512, 4>{});
+    if (C <= 16384) return f(std::conditional_t<LEAN, Shape<1024, 2, true>, Shape<512, 4>>{});
     return f(Shape<1024, 4, true>{});
 }
 // (a workgroup's sums are 8 C bytes out and in again: 512 rows of 16384 in 512 workgroups take 37 us, in 256 25)
 inline int64_t grad_workgroups(int64_t R, int64_t C)
 {
-    const int64_t rows = with_shape(C, false, [](auto s) { return (int64_t)decltype(s)::rows; }), wgs = (R + rows - 1) / rows;
+    const int64_t rows = with_shape<false>(C, [](auto s) { return (int64_t)decltype(s)::rows; }), wgs = (R + rows - 1) / rows;
     return std::min<int64_t>(wgs, (C > 16384 || wgs < 4 * NM_CUS ? 1 : 2) * NM_CUS);
 }
 
@@ -299,7 +301,7 @@ inline int64_t grad_workgroups(int64_t R, int64_t C)
 hipError_t launch_layer_norm(const NormArg &a, hipStream_t st)
 {
     if (a.R <= 0) return hipSuccess;
-    return with_shape(a.C, false, [&](auto s) {
+    return with_shape<false>(a.C, [&](auto s) {
         typedef decltype(s) S;
         const unsigned wgs = (unsigned)std::min<int64_t>((a.R + S::rows - 1) / S::rows, 5 * NM_CUS);
         const dim3 threads(S::threads);
@@ -318,15 +320,18 @@ hipError_t launch_layer_norm_grad(const NormGradArg &a, hipStream_t st)
 {
     const int64_t wgs = grad_workgroups(a.R, a.C);
     hipError_t e = hipSuccess;
-    if (wgs > 0)
-        e = with_shape(a.C, a.x_dt == NM_DT_F32, [&](auto s) {
+    if (wgs > 0 && a.x_dt == NM_DT_BF16)
+        e = with_shape<false>(a.C, [&](auto s) {
             typedef decltype(s) S;
-            const dim3 threads(S::threads);
-            if (a.x_dt == NM_DT_BF16) {
-                if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_BF16, NM_DT_BF16, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
-                else layer_norm_grad_kernel<NM_DT_BF16, NM_DT_F32, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
-            } else if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_F32, NM_DT_BF16, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
-            else layer_norm_grad_kernel<NM_DT_F32, NM_DT_F32, S::t, S::n, S::lean><<<(unsigned)wgs, threads, 0, st>>>(a);
+            if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_BF16, NM_DT_BF16, S::t, S::n, S::lean><<<(unsigned)wgs, S::threads, 0, st>>>(a);
+            else layer_norm_grad_kernel<NM_DT_BF16, NM_DT_F32, S::t, S::n, S::lean><<<(unsigned)wgs, S::threads, 0, st>>>(a);
+            return hipGetLastError();
+        });
+    else if (wgs > 0)
+        e = with_shape<true>(a.C, [&](auto s) {
+            typedef decltype(s) S;
+            if (a.w_dt == NM_DT_BF16) layer_norm_grad_kernel<NM_DT_F32, NM_DT_BF16, S::t, S::n, S::lean><<<(unsigned)wgs, S::threads, 0, st>>>(a);
+            else layer_norm_grad_kernel<NM_DT_F32, NM_DT_F32, S::t, S::n, S::lean><<<(unsigned)wgs, S::threads, 0, st>>>(a);
             return hipGetLastError();
         });
     if (e != hipSuccess || !a.part) return e;
