@@ -509,10 +509,11 @@ class NMSelfAttention(torch.nn.Module):
     def _frequencies(self, device):
         if self._freqs is None:
             return None
-        if device not in self._freqs_on:
+        held = self._freqs_on.get(device)
+        if held is None or held.device != device:                            # (a saved module may have been loaded onto another device than it was saved from)
             with torch.inference_mode(False):                                # (a copy that a call under inference_mode made could not be saved for a gradient later)
-                self._freqs_on[device] = self._freqs.to(device)
-        return self._freqs_on[device]
+                held = self._freqs_on[device] = self._freqs.to(device)
+        return held
 
     def forward(self, x, positions: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None):
         B, T, width = x.shape

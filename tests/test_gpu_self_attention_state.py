@@ -65,3 +65,18 @@ def test_the_first_call_captured():
             torch.cuda.synchronize()
             assert torch.equal(held, want)
             x.copy_(torch.randn(x.shape, device=DEV))
+
+
+def test_saved_and_loaded_onto_the_host():
+    """(a file of this test's own) ... and moved back"""
+    import io
+    x = torch.randn(1, 9, 64, device=DEV).to(BF16)
+    layer = _layer()
+    want = _train(layer, x)
+    file = io.BytesIO()
+    torch.save(layer, file)
+    file.seek(0)
+    again = torch.load(file, map_location="cpu", weights_only=False)
+    assert again.qkv.weight.device.type == "cpu"
+    # (the configuration's state travels with the module; its seed's step is the same)
+    assert all(torch.equal(a, b) for a, b in zip(_train(again.to(DEV), x), want))
