@@ -1103,7 +1103,7 @@ def nm_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool
     """softmax(scale q k^T) v for each head.  q [batch x queries x heads x D], k and v [batch x keys x kv_heads x D], float32 or bfloat16 of one type, D a multiple of
     8 up to 128; heads / kv_heads heads of q in a row share one of k and v.  scale: D ** -0.5 by default.  causal: query i of n sees the keys up to i + m - n of m, the last
     query the last key, so that one query over a cache of keys sees all of them.  q_lens, k_lens (int32 or int64 [batch], on the GPU): the tokens of each sequence, from
-    the front; what lies behind counts for nothing, and the result is zero there, as for a query that sees no key.
+    the front; what lies behind counts for nothing, and the result is zero there, as for a query that sees no key.  What a causal query does not see of its own sequence has to be finite.
     want_lse: (o, lse).  lse[0] is float32 [batch x heads x queries], the logarithm of the sum of exponentials; for bfloat16 lse has D / 2 planes more, whose bits are
     what rounding took from o: element [1 + w, b, h, i] as two bfloat16, those of o[b, i, h, 2 w] and o[b, i, h, 2 w + 1].  nm_attention_grad reads all of it; cut along sequences,
     heads or queries, as the other tensors are, it stays what it is."""

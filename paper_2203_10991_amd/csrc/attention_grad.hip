@@ -6,8 +6,8 @@
 //   dq      a wave keeps 32 rows (attention.h) of q and g as columns: S^T = K Q^T, dP^T = V G^T, dQ^T += K^T dS^T over tiles of keys; delta comes from its own rows first
 //   dk dv   a wave keeps 32 keys as columns: S = Q K^T, dP = G V^T, dV^T += G^T P, dK^T += Q^T dS over tiles of the rows of all heads that share the keys
 // Both recompute S and dP: seven products instead of five, and neither atomics nor a matrix in memory (dS of a pair, written and read in bf16, would take 4 bytes
-// at about 5 TB/s against 4 D operations).  Bound: as the forward pass.  2 x 8192 tokens, 64 heads of 128 over 8, causal: dq 3.4 ms (970 TFLOP/s of its three products), dk dv 4.6 (950
-// of four); 32 x 512, 16 heads of 64: 74 and 81 us (350 and 420); 6 x up to 1333, 12 heads of 80 over 1: 53 and 82, and 12 for the sum of the parts.
+// at about 5 TB/s against 4 D operations).  Bound: as the forward pass.  2 x 8192 tokens, 64 heads of 128 over 8, causal: dq 3.3 ms (1000 TFLOP/s of its three products), dk dv 4.6 (950
+// of four); 32 x 512, 16 heads of 64: 67 and 82 us (385 and 420); 6 x up to 1333, 12 heads of 80 over 1: 55 and 82, and 12 for the sum of the parts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
